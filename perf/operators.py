@@ -69,6 +69,13 @@ def _log(rng, lo, hi):
     return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
 
 
+def _fitting(case):
+    """No more work than the largest listed case has: shorter rows where it is."""
+    while work(case)["bytes"] > 1.2e9 or case["batch"] * case["seqlen"] * case.get("heads", 1) > (1 << 20):
+        case["seqlen"] //= 2
+    return case
+
+
 def draw(rng):
     kind = rng.choice(["fwd", "fwd", "fwd", "bwd", "bwd", "bwd", "step", "step", "norm", "normb"])
     dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
@@ -76,10 +83,8 @@ def draw(rng):
         groups = rng.choice([1, 1, 8, 24])
         dim = groups * _log(rng, 8 if groups > 1 else 64, 4096 // groups)
         batch, seqlen = _log(rng, 1, 64), rng.choice([1, _log(rng, 2, 4096)])
-        while batch * seqlen * dim > 8 * 4096 * 4096:
-            batch, seqlen = max(1, batch // 2), max(1, seqlen // 2)
-        return dict(kind=kind, batch=batch, seqlen=seqlen, dim=dim, groups=groups, dtype=dtype,
-                    gate_first=rng.random() < 0.5)
+        return _fitting(dict(kind=kind, batch=batch, seqlen=seqlen, dim=dim, groups=groups, dtype=dtype,
+                             gate_first=rng.random() < 0.5))
     heads = _log(rng, 1, 64)
     groups = rng.choice([1, heads, max(g for g in range(1, heads + 1) if heads % g == 0 and g * g <= heads)])
     # head sizes: mostly those that models have, sometimes any
@@ -88,11 +93,8 @@ def draw(rng):
                 dtype=dtype, fixed=rng.random() < 0.3)
     if kind == "step":
         return case
-    seqlen = _log(rng, 1, 16384)
-    while case["batch"] * seqlen * heads > (1 << 20):
-        seqlen //= 2
-    mean = rng.uniform(math.log(8), math.log(4096))
-    return dict(case, seqlen=max(1, seqlen), states=rng.random() < 0.5, mean=math.exp(mean))
+    mean = math.exp(rng.uniform(math.log(8), math.log(4096)))
+    return _fitting(dict(case, seqlen=_log(rng, 1, 16384), states=rng.random() < 0.5, mean=mean))
 
 
 def work(case):
