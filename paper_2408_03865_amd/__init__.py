@@ -34,6 +34,7 @@ __all__ = [
     "check_position_indices", "saved_states_size", "chunk_states", "segments", "pack_plan",
     "pack_positions",
     "rmsnorm_fwd", "rmsnorm_bwd",
+    "linear_attention_fwd", "linear_attention_bwd", "linear_attention_step", "gated_rmsnorm_fwd", "gated_rmsnorm_bwd",
     "padding_rate", "PackMambaError", "load", "F32", "BF16",
     "STATE_STRIDE", "BF16_F32OUT",
 ]
@@ -305,3 +306,7 @@ def padding_rate(pieces, n_rows: int, seqlen: int) -> float:
     """Fraction of the rows' tokens that hold no sequence."""
     import numpy as np
     return 1.0 - float(np.asarray(pieces)[:, 3].sum()) / float(max(1, n_rows * seqlen))
+
+
+from .linear import (gated_rmsnorm_bwd, gated_rmsnorm_fwd, linear_attention_bwd, linear_attention_fwd,  # noqa: E402
+                     linear_attention_step)

@@ -35,6 +35,19 @@ EXPORTS = (
     "packmamba_causal_conv1d_bwd_noalloc",
 )
 
+# Every symbol of include/packmamba_linear.h, with its arguments (p: pointer, s: size, l: 64-bit, i: 32-bit,
+# f: float) and whether it returns a size.
+LINEAR_EXPORTS = {
+    "packmamba_linear_attention_fwd_workspace_size": ("llllll", True),
+    "packmamba_linear_attention_fwd": ("ppppppfppps" + "llllll" + "iip", False),
+    "packmamba_linear_attention_bwd_workspace_size": ("llllll", True),
+    "packmamba_linear_attention_bwd": ("ppppppf" + "ppppppp" + "ps" + "llllll" + "iip", False),
+    "packmamba_linear_attention_step": ("ppppppfp" + "lllll" + "iip", False),
+    "packmamba_gated_rmsnorm_fwd": ("pppfpp" + "llll" + "iip", False),
+    "packmamba_gated_rmsnorm_bwd_workspace_size": ("llll", True),
+    "packmamba_gated_rmsnorm_bwd": ("pppppppp" + "ps" + "llll" + "iip", False),
+}
+
 PACK_SEQUENTIAL, PACK_GREEDY, PACK_CUT = 0, 1, 2
 
 
@@ -102,6 +115,12 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
                  "packmamba_selective_scan_fwd", "packmamba_selective_scan_bwd",
                  "packmamba_check_position_indices", "packmamba_rmsnorm_fwd", "packmamba_rmsnorm_bwd"):
         getattr(lib, name).restype = ctypes.c_int
+    kinds = {"p": vp, "s": sz, "l": i64, "i": i32, "f": ctypes.c_float}
+    for name, (args, size) in LINEAR_EXPORTS.items():
+        fn = getattr(lib, name, None)        # a build of the other header's host layer alone lacks them
+        if fn is not None:
+            fn.argtypes = [kinds[c] for c in args]
+            fn.restype = sz if size else ctypes.c_int
     if lib.packmamba_abi_version() != ABI_VERSION:
         raise RuntimeError("libpackmamba ABI version mismatch")
     if path == LIB_PATH:

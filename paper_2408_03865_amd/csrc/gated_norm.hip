@@ -1,0 +1,304 @@
+// gated_norm.hip -- the gated RMSNorm of (batch, dim, seqlen) activations, forward and backward: each group
+// of consecutive features is normed by itself at every token, of a = x silu(z) (gate first) or of x, whose
+// normed value silu(z) then multiplies.
+//
+// A block owns the features of one group at a tile of consecutive tokens: GROUPS lanes side by side, each with a
+// 16-byte vector of tokens, and THREADS / GROUPS slices of the features.  A thread keeps what it
+// read of its first KEPT features in registers from the sum over the features to the second sweep; features
+// beyond those are read again.  Bound by HBM: three tensors in the forward, five in the backward.
+#include "common.hpp"
+#include "launch.hpp"
+#include "linear.hpp"
+
+namespace pm {
+namespace {
+
+// Sum over the slices of each token's value, in a fixed order; every thread gets its own tokens' sums.
+template <int GROUPS, int THREADS, int TOK>
+__device__ __forceinline__ void slices_sum(float (&v)[TOK], float (*red)[GROUPS * TOK], int grp) {
+#pragma unroll
+    for (int m = GROUPS; m < 64; m *= 2)
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) v[k] += __shfl_xor(v[k], m);
+    if ((int)(threadIdx.x & 63) < GROUPS) {
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) red[threadIdx.x >> 6][grp * TOK + k] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < TOK; ++k) v[k] = red[0][grp * TOK + k];
+    for (int w = 1; w < THREADS / 64; ++w)
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) v[k] += red[w][grp * TOK + k];
+}
+
+template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST>
+__global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
+    constexpr int TOK = Storage<T>::kPerVec, SL = THREADS / GROUPS;
+    __shared__ float red[THREADS / 64][GROUPS * TOK];
+    const int grp = threadIdx.x % GROUPS, sl = threadIdx.x / GROUPS;
+    const int64_t L = a.seqlen, tiles = (L + GROUPS * TOK - 1) / (GROUPS * TOK);
+    const int64_t bg = blockIdx.x / tiles, t0 = (blockIdx.x - bg * tiles) * (GROUPS * TOK);
+    const int per = (int)(a.dim / a.groups);
+    const bool whole = t0 + GROUPS * TOK <= L || L % TOK == 0;     // no vector crosses the row end
+    const bool live = t0 + grp * TOK < L;
+    const int64_t l0 = whole && !live ? t0 : t0 + grp * TOK;
+    const int64_t base = bg * per * L;
+    const T* x = static_cast<const T*>(a.x) + base;
+    const T* z = static_cast<const T*>(a.z) + base;
+    TO* out = static_cast<TO*>(a.out) + base;
+    const float* w = a.w + (bg % a.groups) * per;
+    const auto body = [&](auto full_tag) {
+        constexpr bool FULL = decltype(full_tag)::value;
+        constexpr int C = FULL ? KEPT : 0;
+        RawRun<T, TOK> xr[KEPT], zr[KEPT];
+        float kept[FIRST ? KEPT : 1][TOK];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            xr[i] = zr[i] = RawRun<T, TOK>{};
+            const int f = sl + i * SL;
+            if (f < per) {
+                xr[i] = load_raw<T, TOK>(x + (int64_t)f * L, l0);
+                zr[i] = load_raw<T, TOK>(z + (int64_t)f * L, l0);
+            }
+        }
+        float s[TOK] = {};
+        const auto value = [&](const float (&xv)[TOK], const float (&zv)[TOK], float (&v)[TOK]) {
+#pragma unroll
+            for (int k = 0; k < TOK; ++k) {
+                v[k] = FIRST ? xv[k] * (zv[k] * sigmoid_f(zv[k])) : xv[k];
+                s[k] = fmaf(v[k], v[k], s[k]);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            float xv[TOK], zv[TOK], v[TOK];
+            unpack_run(xr[i], xv);
+            unpack_run(zr[i], zv);
+            value(xv, zv, v);
+            if constexpr (FIRST) {
+#pragma unroll
+                for (int k = 0; k < TOK; ++k) kept[i][k] = v[k];
+            }
+        }
+        for (int f = sl + C * SL; f < per; f += SL) {
+            float xv[TOK], zv[TOK], v[TOK];
+            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, xv);
+            if constexpr (FIRST) load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
+            value(xv, zv, v);
+        }
+        slices_sum<GROUPS, THREADS, TOK>(s, red, grp);
+        float r[TOK];
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) r[k] = 1.0f / sqrtf(s[k] / (float)per + a.eps);
+        if (sl == 0) {
+#pragma unroll
+            for (int k = 0; k < TOK; ++k)
+                if (FULL ? live : l0 + k < L) a.rstd_out[bg * L + l0 + k] = r[k];
+        }
+        const auto put = [&](float (&v)[TOK], const float (&zv)[TOK], int f) {
+            const float wv = w[f];
+#pragma unroll
+            for (int k = 0; k < TOK; ++k) {
+                v[k] = v[k] * r[k] * wv;
+                if constexpr (!FIRST) v[k] *= zv[k] * sigmoid_f(zv[k]);
+            }
+            if (!FULL || live) store_run<TO, TOK, FULL>(out + (int64_t)f * L, l0, L, v);
+        };
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int f = sl + i * SL;
+            float v[TOK], zv[TOK];
+            if constexpr (FIRST) {
+#pragma unroll
+                for (int k = 0; k < TOK; ++k) v[k] = kept[i][k];
+            } else {
+                unpack_run(xr[i], v);
+                unpack_run(zr[i], zv);
+            }
+            if (f < per) put(v, zv, f);
+        }
+        for (int f = sl + C * SL; f < per; f += SL) {
+            float v[TOK], zv[TOK];
+            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, v);
+            load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
+            if constexpr (FIRST) {
+#pragma unroll
+                for (int k = 0; k < TOK; ++k) v[k] *= zv[k] * sigmoid_f(zv[k]);
+            }
+            put(v, zv, f);
+        }
+    };
+    if (whole) body(std::true_type{});
+    else body(std::false_type{});
+}
+
+// With up the gradient of a rstd (dout weight, or dout weight gate) and m the mean of up a over the group,
+//   da = rstd (up - a rstd^2 m), and from it dx and dz; partial[b, tile, f] = the tile's sum for dweight.
+template <typename T, typename TO, int THREADS, int KEPT, bool FIRST>
+__global__ __launch_bounds__(THREADS) void gated_bwd_kernel(GatedArgs a) {
+    constexpr int TOK = Storage<T>::kPerVec, GROUPS = (int)kRmsTile / TOK, SL = THREADS / GROUPS;
+    __shared__ float red[THREADS / 64][GROUPS * TOK];
+    const int grp = threadIdx.x % GROUPS, sl = threadIdx.x / GROUPS;
+    const int64_t L = a.seqlen, tiles = (L + kRmsTile - 1) / kRmsTile;
+    const int64_t bg = blockIdx.x / tiles, tile = blockIdx.x - bg * tiles, t0 = tile * kRmsTile;
+    const int64_t b = bg / a.groups;
+    const int per = (int)(a.dim / a.groups), first = (int)(bg - b * a.groups) * per;
+    const bool whole = t0 + kRmsTile <= L || L % TOK == 0;
+    const bool live = t0 + grp * TOK < L;
+    const int64_t l0 = whole && !live ? t0 : t0 + grp * TOK;
+    const int64_t base = bg * per * L;
+    const T* x = static_cast<const T*>(a.x) + base;
+    const T* z = static_cast<const T*>(a.z) + base;
+    const T* g = static_cast<const T*>(a.dout) + base;
+    TO* dx = static_cast<TO*>(a.out) + base;
+    TO* dz = static_cast<TO*>(a.dz) + base;
+    const float* w = a.w + first;
+    float* part = a.partial + (b * tiles + tile) * a.dim + first;
+    const auto body = [&](auto full_tag) {
+        constexpr bool FULL = decltype(full_tag)::value;
+        constexpr int C = FULL ? KEPT : 0;
+        RawRun<T, TOK> xr[KEPT], zr[KEPT], gr[KEPT];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            xr[i] = zr[i] = gr[i] = RawRun<T, TOK>{};
+            const int f = sl + i * SL;
+            if (f < per) {
+                xr[i] = load_raw<T, TOK>(x + (int64_t)f * L, l0);
+                zr[i] = load_raw<T, TOK>(z + (int64_t)f * L, l0);
+                gr[i] = load_raw<T, TOK>(g + (int64_t)f * L, l0);
+            }
+        }
+        float s[TOK] = {};
+        const auto dot = [&](const float (&xv)[TOK], const float (&zv)[TOK], const float (&gv)[TOK], float wv) {
+#pragma unroll
+            for (int k = 0; k < TOK; ++k) s[k] = fmaf(gv[k] * wv * (zv[k] * sigmoid_f(zv[k])), xv[k], s[k]);
+        };
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            float xv[TOK], zv[TOK], gv[TOK];
+            unpack_run(xr[i], xv);
+            unpack_run(zr[i], zv);
+            unpack_run(gr[i], gv);
+            const int f = sl + i * SL;
+            if (f < per) dot(xv, zv, gv, w[f]);
+        }
+        for (int f = sl + C * SL; f < per; f += SL) {
+            float xv[TOK], zv[TOK], gv[TOK];
+            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, xv);
+            load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
+            load_run<T, TOK, FULL>(g + (int64_t)f * L, l0, L, gv);
+            dot(xv, zv, gv, w[f]);
+        }
+        float r[TOK], c[TOK];
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) r[k] = (FULL || l0 + k < L) ? a.rstd[bg * L + l0 + k] : 0.0f;
+        slices_sum<GROUPS, THREADS, TOK>(s, red, grp);
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) c[k] = r[k] * r[k] * (s[k] / (float)per);
+        const auto grad = [&](const float (&xv)[TOK], const float (&zv)[TOK], const float (&gv)[TOK], int f) {
+            const float wv = w[f];
+            float ox[TOK], oz[TOK], pw = 0.0f;
+#pragma unroll
+            for (int k = 0; k < TOK; ++k) {
+                const float sig = sigmoid_f(zv[k]), gate = zv[k] * sig, dgate = sig * fmaf(zv[k], 1.0f - sig, 1.0f);
+                if constexpr (FIRST) {
+                    const float av = xv[k] * gate, da = r[k] * (gv[k] * wv - av * c[k]);
+                    ox[k] = da * gate;
+                    oz[k] = da * xv[k] * dgate;
+                    pw = fmaf(gv[k] * av, r[k], pw);
+                } else {
+                    ox[k] = r[k] * (gv[k] * wv * gate - xv[k] * c[k]);
+                    const float n = gv[k] * xv[k] * r[k];
+                    oz[k] = n * wv * dgate;
+                    pw = fmaf(n, gate, pw);
+                }
+            }
+            if (FULL && !live) pw = 0.0f;
+            if (!FULL || live) {
+                store_run<TO, TOK, FULL>(dx + (int64_t)f * L, l0, L, ox);
+                store_run<TO, TOK, FULL>(dz + (int64_t)f * L, l0, L, oz);
+            }
+#pragma unroll
+            for (int m = 1; m < GROUPS; m *= 2) pw += __shfl_xor(pw, m, GROUPS);
+            if (grp == 0) part[f] = pw;
+        };
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            float xv[TOK], zv[TOK], gv[TOK];
+            unpack_run(xr[i], xv);
+            unpack_run(zr[i], zv);
+            unpack_run(gr[i], gv);
+            const int f = sl + i * SL;
+            if (f < per) grad(xv, zv, gv, f);
+        }
+        for (int f = sl + C * SL; f < per; f += SL) {
+            float xv[TOK], zv[TOK], gv[TOK];
+            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, xv);
+            load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
+            load_run<T, TOK, FULL>(g + (int64_t)f * L, l0, L, gv);
+            grad(xv, zv, gv, f);
+        }
+    };
+    if (whole) body(std::true_type{});
+    else body(std::false_type{});
+}
+
+template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST>
+hipError_t fwd_one(const GatedArgs& a, hipStream_t s) {
+    constexpr int64_t kTile = GROUPS * Storage<T>::kPerVec;
+    const int64_t blocks = a.batch * a.groups * ((a.seqlen + kTile - 1) / kTile);
+    hipLaunchKernelGGL((gated_fwd_kernel<T, TO, GROUPS, THREADS, KEPT, FIRST>), dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, typename TO, bool FIRST>
+hipError_t fwd_t(const GatedArgs& a, hipStream_t s) {
+    const int64_t per = a.dim / a.groups;
+    if (per <= 256) return fwd_one<T, TO, 8, 256, 8, FIRST>(a, s);
+    if (per <= 512) return fwd_one<T, TO, 8, 512, 8, FIRST>(a, s);
+    return fwd_one<T, TO, 8, 1024, 8, FIRST>(a, s);
+}
+
+template <typename T, typename TO, int THREADS, int KEPT, bool FIRST>
+hipError_t bwd_one(const GatedArgs& a, hipStream_t s) {
+    const int64_t tiles = (a.seqlen + kRmsTile - 1) / kRmsTile;
+    hipLaunchKernelGGL((gated_bwd_kernel<T, TO, THREADS, KEPT, FIRST>), dim3((unsigned)(a.batch * a.groups * tiles)),
+                       dim3(THREADS), 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_partial_rows_sum(a.partial, a.dw, a.batch * tiles, a.dim, s);
+}
+
+template <typename T, typename TO, bool FIRST>
+hipError_t bwd_t(const GatedArgs& a, hipStream_t s) {
+    const int64_t per = a.dim / a.groups;
+    if (per <= 128) return bwd_one<T, TO, 256, 4, FIRST>(a, s);
+    if (per <= 256) return bwd_one<T, TO, 512, 4, FIRST>(a, s);
+    return bwd_one<T, TO, 1024, 4, FIRST>(a, s);
+}
+
+template <bool FIRST>
+hipError_t fwd_d(const GatedArgs& a, hipStream_t s) {
+    switch (a.dtype) {
+        case 1: return fwd_t<bf16_t, bf16_t, FIRST>(a, s);
+        case 2: return fwd_t<bf16_t, float, FIRST>(a, s);
+        default: return fwd_t<float, float, FIRST>(a, s);
+    }
+}
+template <bool FIRST>
+hipError_t bwd_d(const GatedArgs& a, hipStream_t s) {
+    switch (a.dtype) {
+        case 1: return bwd_t<bf16_t, bf16_t, FIRST>(a, s);
+        case 2: return bwd_t<bf16_t, float, FIRST>(a, s);
+        default: return bwd_t<float, float, FIRST>(a, s);
+    }
+}
+
+}  // namespace
+
+int64_t gated_bwd_partial_rows(int64_t batch, int64_t seqlen) { return batch * ((seqlen + kRmsTile - 1) / kRmsTile); }
+
+hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s) { return a.gate_first ? fwd_d<true>(a, s) : fwd_d<false>(a, s); }
+hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) { return a.gate_first ? bwd_d<true>(a, s) : bwd_d<false>(a, s); }
+
+}  // namespace pm

@@ -60,6 +60,8 @@ struct RmsArgs {
 };
 hipError_t launch_rmsnorm_fwd(const RmsArgs& a, hipStream_t s);
 hipError_t launch_rmsnorm_bwd(const RmsArgs& a, hipStream_t s);
+// out[f] = sum over the rows of partial (rows, dim), in a fixed order
+hipError_t launch_partial_rows_sum(const float* partial, float* out, int64_t rows, int64_t dim, hipStream_t s);
 
 // The conv backward runs one wave per (row, segment); a row is cut into segments of
 // whole 512-token steps when batch x dim alone gives fewer than kConvBwdWaves waves.

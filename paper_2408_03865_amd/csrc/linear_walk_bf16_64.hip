@@ -1,0 +1,6 @@
+// The linear-attention walks of heads whose contracted features number up to 64: bf16_t in, bf16_t out.
+#include "linear_walk.hpp"
+
+namespace pm {
+template hipError_t launch_walk_kc<bf16_t, bf16_t, 64>(const WalkArgs&, WalkMode, bool, hipStream_t);
+}  // namespace pm

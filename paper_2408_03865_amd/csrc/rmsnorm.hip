@@ -393,6 +393,12 @@ hipError_t bwd_t(const RmsArgs& a, hipStream_t s) {
 
 }  // namespace
 
+hipError_t launch_partial_rows_sum(const float* partial, float* out, int64_t rows, int64_t dim, hipStream_t s) {
+    hipLaunchKernelGGL(rmsnorm_bwd_finalize, dim3((unsigned)((dim + kFinFeat - 1) / kFinFeat)), dim3(kFinFeat * kFinRows),
+                       0, s, partial, out, rows, dim);
+    return hipGetLastError();
+}
+
 hipError_t launch_rmsnorm_fwd(const RmsArgs& a, hipStream_t s) {
     switch (a.dtype) {
         case 1: return fwd_t<bf16_t, bf16_t>(a, s);
