@@ -20,8 +20,8 @@
  *             A value of -104 or less (exp of it is 0 in 32 bits; -infinity too) cuts as a start
  *             does.  Values above 0 make the state grow and are taken as they are.
  *   states    (batch, heads, dk, dv) float
- * dk, dv in [1, 128]; heads a multiple of groups; batch * heads at most 2^23, and batch * heads *
- * max(dk, dv) * seqlen at most 2^33.
+ * dk, dv in [1, 128]; heads a multiple of groups; seqlen at most 2^22, batch * heads at most 2^23, and
+ * batch * heads * max(dk, dv) * seqlen at most 2^33.
  * Arithmetic: products accumulate in 32 bits and the state is held in 32 bits.  With bf16 inputs the
  * products inside a chunk of 64 tokens (q . k, weighted) and the copy of the state that q is
  * multiplied with are rounded to bf16 once, also where PACKMAMBA_BF16_F32OUT returns 32 bits: out

@@ -40,15 +40,18 @@ __global__ void walk_chain(float* __restrict__ seg, const float* __restrict__ se
     }
 }
 
+template <typename T, int KC, int VP>
+hipError_t aggregate_vp(const WalkArgs& a, hipStream_t s) {
+    constexpr int NS = Mat<T>::kSplit ? 3 : 1;
+    const dim3 grid((unsigned)((int64_t)a.batch * a.heads * (a.nseg - 1))), block(walk_threads<T, KC, VP>());
+    if (a.rev) hipLaunchKernelGGL((walk_aggregate<T, KC, VP, true, NS>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((walk_aggregate<T, KC, VP, false, NS>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
 template <typename T, int KC>
 hipError_t aggregate_kc(const WalkArgs& a, hipStream_t s) {
-    constexpr int NS = Mat<T>::kSplit ? 3 : 1;
-    const dim3 grid((unsigned)((int64_t)a.batch * a.heads * (a.nseg - 1)));
-    if (a.z.rows <= 64)
-        hipLaunchKernelGGL((walk_aggregate<T, KC, 64, NS>), grid, dim3(kWalkThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((walk_aggregate<T, KC, 128, NS>), grid, dim3(kWalkThreads), 0, s, a);
-    return hipGetLastError();
+    return a.z.rows <= 64 ? aggregate_vp<T, KC, 64>(a, s) : aggregate_vp<T, KC, 128>(a, s);
 }
 
 template <typename T>

@@ -11,6 +11,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxRows = (int64_t)1 << 23;      // (batch, head) pairs: one block each
+constexpr int64_t kMaxSeqlen = (int64_t)1 << 22;    // 64 rows of it in fp32 are an offset of 32 bits in the walks
 constexpr int64_t kMaxElems = (int64_t)1 << 33;     // of a tensor, heads' copies of q and k included
 
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
@@ -31,7 +32,7 @@ int check_heads(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_
     if (batch <= 0 || heads <= 0 || groups <= 0 || dk <= 0 || dv <= 0 || seqlen <= 0) return PACKMAMBA_ERR_SHAPE;
     if (heads > kMaxRows || batch > kMaxRows / heads || heads % groups) return PACKMAMBA_ERR_SHAPE;
     if (dk > PACKMAMBA_LINEAR_MAX_HEAD || dv > PACKMAMBA_LINEAR_MAX_HEAD) return PACKMAMBA_ERR_UNSUPPORTED;
-    if (seqlen > INT32_MAX / 2 || seqlen > kMaxElems / (batch * heads * (dk > dv ? dk : dv))) return PACKMAMBA_ERR_SHAPE;
+    if (seqlen > kMaxSeqlen || seqlen > kMaxElems / (batch * heads * (dk > dv ? dk : dv))) return PACKMAMBA_ERR_SHAPE;
     return PACKMAMBA_OK;
 }
 

@@ -17,12 +17,12 @@
 // pairs inside a chunk are summed from the 32-bit products; a pair's contributions to r_i and r_j
 // cancel to rounding.  Boundaries every 512 tokens keep those sums short.
 //
-// Mapping.  One block of 4 waves walks a row (or a segment of it) of one head; activations are
-// (features, tokens), tokens innermost.  A chunk's tiles sit in LDS as they do in memory.  Products
+// Mapping.  One block walks a row (or a segment of it) of one head; activations are (features, tokens),
+// tokens innermost.  A chunk's tiles sit in LDS as they do in memory.  Products
 // over tokens (z and the update) read their operands directly, four tokens a lane; products over
 // features (x . y and x . S) read them transposed (ds_read_b64_tr_b16 in bf16).  The waves share the
 // 64 x 64 products of x and y by strips of 16 x's and pass them, weighted and rounded to T, through
-// LDS.  Each wave owns 16 or 32 of z's features: its part of S stays in registers, in the layout
+// LDS.  Each wave owns 16 of z's features: its part of S stays in registers, in the layout
 // that an MFMA result has and, four rows of it a lane, an MFMA operand takes.
 // Rounding in bf16: the weighted products x . y and, in plain walks, the copy of S that is
 // multiplied with x are rounded to bf16 once (each enters bf16 outputs only); what S itself adds is
@@ -42,28 +42,49 @@ namespace pm {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kWalkThreads = 256, kWalkWaves = 4, kC = (int)kLinChunk;
+constexpr int kC = (int)kLinChunk;
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// v, as a value that is new here: what is computed from it stays where it is used, and takes no
+// registers elsewhere.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// The same where HIDE, for offsets that a kernel short of registers computes anew in each phase.
+template <bool HIDE>
+__device__ __forceinline__ int fresh(int v) {
+    if constexpr (HIDE) return here(v);
+    else return v;
+}
 
 // A decay below this multiplies by 0 in 32 bits (exp(-104) < 2^-150): the token is taken for a start.
 constexpr float kDecayCut = -104.0f;
 
 // --------------------------------------------------------------------------------------------
 // matrix operands: four values of the contracted index a lane, 4 (lane / 16) .. + 3 of 16, for
-// row or column lane % 16 -- also the layout of a 16 x 16 result, contracted along its rows
+// row or column lane % 16 -- also the layout of a 16 x 16 result, contracted along its rows.
+// Tiles in LDS are rows of 64 tokens without padding; the 16-byte pieces of row r are permuted by
+// an exclusive or with swz(r), so that 16 rows by 16 tokens, read either way, take every bank once.
 // --------------------------------------------------------------------------------------------
 template <typename T> struct Mat;
 
 template <> struct Mat<bf16_t> {
     typedef u32x2 Frag;
-    static constexpr int kStride = kC + 8;          // of a tile's rows: 144 bytes spread 16 rows over all banks
     static constexpr bool kSplit = true;
-    __device__ static Frag direct(const bf16_t* p) { return *reinterpret_cast<const u32x2*>(p); }
-    // rows 0..15 of p (kStride apart), token lane % 16 of 16
-    __device__ static Frag transposed(const bf16_t* p) {
-        const int l = lane_id();
-        const bf16_t* q = p + ((l >> 4) * 4 + ((l & 15) >> 2)) * kStride + (l & 3) * 4;
+    __device__ static int swz(int r) { return (r & 6) | ((r >> 3) & 1); }
+    // rows 0..15 of the tile, tokens 16 tt + 4 (lane / 16) .. + 3 of row lane % 16
+    __device__ static int direct_at(int l, int tt) {
+        const int r = l & 15, half = (l >> 5) ^ ((r >> 3) & 1);
+        return r * kC + half * 8 + ((l >> 4) & 1) * 4 + (tt ^ ((r >> 1) & 3)) * 16;
+    }
+    __device__ static Frag direct(int l, const bf16_t* p, int tt) { return *reinterpret_cast<const u32x2*>(p + direct_at(l, tt)); }
+    // rows 4 (lane / 16) .. + 3 of the tile, token 16 tt + lane % 16
+    __device__ static Frag transposed(int l, const bf16_t* p, int tt) {
+        const int r = (l >> 4) * 4 + ((l & 15) >> 2), half = ((l >> 1) & 1) ^ ((r >> 3) & 1);
+        const bf16_t* q = p + r * kC + half * 8 + (l & 1) * 4 + (tt ^ ((r >> 1) & 3)) * 16;
         const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (__attribute__((address_space(3))) s16x4*)(const_cast<bf16_t*>(q)));
         return __builtin_bit_cast(u32x2, v);
@@ -98,23 +119,31 @@ template <> struct Mat<bf16_t> {
     __device__ static uint32_t high2(float a, float b) {
         return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
     }
-    __device__ static bool finite(const u32x4& w) {
-        uint32_t t = 0;
+    // 0 times every value, added up: NaN if one is infinite or NaN
+    __device__ static float zero_sum(const u32x4& w, float v) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t |= (w[i] & 0x7f807f80u) + 0x00800080u;
-        return (t & 0x80008000u) == 0;
+        for (int i = 0; i < 4; ++i)
+            v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, uint32_t(w[i])), bf16x2{0, 0}, v, false);
+        return v;
     }
 };
 
 template <> struct Mat<float> {
     typedef f32x4 Frag;
-    static constexpr int kStride = kC + 4;
     static constexpr bool kSplit = false;
-    __device__ static Frag direct(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-    __device__ static Frag transposed(const float* p) {
-        const int l = lane_id();
-        const float* q = p + (l >> 4) * 4 * kStride + (l & 15);
-        return Frag{q[0], q[kStride], q[2 * kStride], q[3 * kStride]};
+    __device__ static int swz(int r) { return r & 15; }
+    __device__ static int direct_at(int l, int tt) {
+        const int r = l & 15;
+        return r * kC + ((l >> 4) ^ (r & 3)) * 4 + (tt ^ (r >> 2)) * 16;
+    }
+    __device__ static Frag direct(int l, const float* p, int tt) { return *reinterpret_cast<const f32x4*>(p + direct_at(l, tt)); }
+    __device__ static Frag transposed(int l, const float* p, int tt) {
+        const int g = l >> 4;
+        const float* q = p + g * 4 * kC + (tt ^ g) * 16 + (l & 3);
+        Frag v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = q[e * kC + (((l >> 2) & 3) ^ e) * 4];
+        return v;
     }
     __device__ static Frag round(const f32x4& v) { return v; }
     __device__ static f32x4 mma(const Frag& a0, const Frag& a1, const Frag& b0, const Frag& b1, f32x4 c) {
@@ -127,22 +156,28 @@ template <> struct Mat<float> {
     __device__ static f32x4 widen(const Frag& f) { return f; }
     template <int N>
     __device__ static void split(const f32x4& v, Frag* out) { out[0] = v; }
-    __device__ static bool finite(const u32x4& w) {
-        bool ok = true;
+    __device__ static float zero_sum(const u32x4& w, float v) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ok = ok && (w[i] & 0x7f800000u) != 0x7f800000u;
-        return ok;
+        for (int i = 0; i < 4; ++i) v = fmaf(__uint_as_float(w[i]), 0.0f, v);
+        return v;
     }
 };
+
+// The value of row r at token t of a tile.
+template <typename T>
+__device__ __forceinline__ float tile_value(const T* tile, int r, int t) {
+    constexpr int kPer = Storage<T>::kPerVec;
+    return Storage<T>::load1(tile + r * kC + ((t / kPer) ^ Mat<T>::swz(r)) * kPer + t % kPer);
+}
 
 // --------------------------------------------------------------------------------------------
 // a chunk's decays
 // --------------------------------------------------------------------------------------------
 struct __attribute__((aligned(16))) ChunkDecay {
     float hi[kC], lo[kC];       // G in log2 units, as a sum of two floats
-    float in[kC], up[kC];       // -1: left out
+    float in[kC], up[kC];       // scaled; 0 where the term is left out
     int32_t start[kC];          // the last start up to the token, -1: none in the chunk
-    float a;                    // -1: cut
+    float a;                    // -1: a start in the chunk
     int32_t bad[1];             // an infinity or a NaN in y or z
 };
 
@@ -166,9 +201,26 @@ __device__ __forceinline__ float pair_decay(float hi, float lo, float hj, float 
     return fast_exp2((hi - hj) + (lo - lj));
 }
 
+// Whether token t takes the state that enters the chunk (enters), and whether it adds to the one that
+// leaves it (leaves), in a forward walk; a reverse walk has the two the other way round.
+template <bool REV>
+__device__ __forceinline__ bool enters(const ChunkDecay& c, int t) {
+    return REV ? t >= c.start[kC - 1] : c.start[t] < 0;
+}
+template <bool REV>
+__device__ __forceinline__ bool leaves(const ChunkDecay& c, int t) {
+    return enters<!REV>(c, t);
+}
+// Whether x's out takes y.
+template <bool REV>
+__device__ __forceinline__ bool takes(const ChunkDecay& c, int x, int y) {
+    return REV ? x <= y && c.start[y] <= x : y <= x && c.start[x] <= y;
+}
+
 // One wave, lane = token.  The sum is kept in 64 bits and starts anew at each start, so that no
 // sequence's decays reach another's.
-__device__ __forceinline__ void chunk_decay(const TokenDecay& d, bool rev, ChunkDecay& c) {
+template <bool REV>
+__device__ __forceinline__ void chunk_decay(const TokenDecay& d, ChunkDecay& c, float iscale, float uscale) {
     const int l = lane_id();
     bool cut = d.pos == 0 || d.g <= kDecayCut;
     double v = cut ? 0.0 : (double)d.g * 1.4426950408889634;
@@ -185,86 +237,123 @@ __device__ __forceinline__ void chunk_decay(const TokenDecay& d, bool rev, Chunk
     const float hi = (float)v, lo = (float)(v - (double)hi);
     const float ehi = __shfl(hi, 63), elo = __shfl(lo, 63);
     const int estart = __shfl(start, 63);
-    const float first = start < 0 ? fast_exp2(hi + lo) : -1.0f;
-    const float last = l >= estart ? pair_decay(ehi, elo, hi, lo) : -1.0f;
+    const float first = start < 0 ? fast_exp2(hi + lo) : 0.0f;
+    const float last = l >= estart ? pair_decay(ehi, elo, hi, lo) : 0.0f;
     c.hi[l] = hi;
     c.lo[l] = lo;
     c.start[l] = start;
-    c.in[l] = rev ? last : first;
-    c.up[l] = rev ? first : last;
-    if (l == 63) c.a = first;
+    c.in[l] = (REV ? last : first) * iscale;
+    c.up[l] = (REV ? first : last) * uscale;
+    if (l == 63) c.a = start < 0 ? first : -1.0f;
 }
 
 // --------------------------------------------------------------------------------------------
 // tiles: ROWS features x 64 tokens through registers into LDS; features and tokens that the tensor
 // lacks are 0
 // --------------------------------------------------------------------------------------------
-template <typename T, int ROWS>
+__device__ const u32x4 walk_zero = {0, 0, 0, 0};
+
+template <typename T, int ROWS, int THREADS>
 struct TileRegs {
-    static constexpr int kPer = Storage<T>::kPerVec, kLanes = kC / kPer, kRowsPass = kWalkThreads / kLanes;
+    static constexpr int kPer = Storage<T>::kPerVec, kLanes = kC / kPer, kRowsPass = THREADS / kLanes;
     static constexpr int kPasses = ROWS / kRowsPass;
+    static_assert(kRowsPass % 16 == 0 && ROWS % kRowsPass == 0, "a thread's rows are permuted alike");
     u32x4 w[kPasses];
 
-    __device__ void load(const T* p, int rows, int64_t t0, int64_t L) {
-        const int tok = (threadIdx.x % kLanes) * kPer, row0 = threadIdx.x / kLanes;
-        const bool whole = t0 + kC <= L;
+    // Every lane loads whole vectors from inside its row, a row that the tensor has, whatever it needs: a branch
+    // here would make the kernel wait for the loads at once.  settle() puts right what the last chunk of a row
+    // and heads of fewer features need, when the values are used.  One 32-bit offset a lane for all its rows.
+    __device__ void load(int tid, const T* p, int rows, int64_t t0, int64_t L) {
+        const int row0 = tid / kLanes, tok = (tid % kLanes) * kPer;
+        const int64_t from = min(t0, L - kPer);             // of the row's vectors the last starts at L - kPer
+        const T* base = L < kPer ? reinterpret_cast<const T*>(&walk_zero) : p + from;
+        const uint32_t t = L < kPer ? 0 : (uint32_t)(min(t0 + tok, L - kPer) - from) * sizeof(T);
+        const uint32_t at = L < kPer ? 0 : (uint32_t)row0 * (uint32_t)L * sizeof(T) + t;
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) {
-            const int row = row0 + i * kRowsPass;
-            w[i] = u32x4{0, 0, 0, 0};
-            if (row < rows) {
-                const T* src = p + (int64_t)row * L + t0 + tok;
-                if (whole || t0 + tok + kPer <= L) {
-                    w[i] = load_vec<T, kPer>(src);
-                } else {
-                    float v[kPer];
-#pragma unroll
-                    for (int k = 0; k < kPer; ++k) v[k] = t0 + tok + k < L ? Storage<T>::load1(src + k) : 0.0f;
-                    w[i] = Storage<T>::pack(v);
-                }
-            }
+            const T* row = i * kRowsPass < rows && L >= kPer ? base + i * kRowsPass * L : base;
+            const uint32_t off = row0 + i * kRowsPass < rows ? at : t;
+            w[i] = load_vec<T, kPer>(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + off));
         }
     }
-    __device__ void store(T* tile) const {
-        const int tok = (threadIdx.x % kLanes) * kPer, row0 = threadIdx.x / kLanes;
+    __device__ void settle(int tid, const T* p, int rows, int64_t t0, int64_t L) {
+        const int row0 = tid / kLanes, tok = (tid % kLanes) * kPer;
+        if (rows < ROWS) {
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i)
-            *reinterpret_cast<u32x4*>(tile + (row0 + i * kRowsPass) * Mat<T>::kStride + tok) = w[i];
+            for (int i = 0; i < kPasses; ++i)
+                if (row0 + i * kRowsPass >= rows) w[i] = u32x4{0, 0, 0, 0};
+        }
+        if (t0 + kC <= L) return;
+        if (L < kPer) {                     // rows shorter than a vector
+#pragma unroll 1
+            for (int i = 0; i < kPasses; ++i) {
+                const int row = row0 + i * kRowsPass;
+                u32x4 v = {0, 0, 0, 0};
+#pragma unroll 1
+                for (int k = 0; k < kPer; ++k) push(v, row < rows && tok + k < L ? p[row * L + tok + k] : T{});
+#pragma unroll
+                for (int j = 0; j < kPasses; ++j)
+                    if (j == i) w[j] = v;
+            }
+            return;
+        }
+        const int64_t over = t0 + tok + kPer - L;           // elements that the vector was read too early
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            u32x4 v = over >= kPer ? u32x4{0, 0, 0, 0} : w[i];
+#pragma unroll
+            for (int k = 1; k < kPer; ++k) {
+                u32x4 u = v;
+                push(u, T{});
+                v = over >= k && over < kPer ? u : v;
+            }
+            w[i] = v;
+        }
     }
-    __device__ bool finite() const {
-        bool ok = true;
+    // v after the last of the vector's elements, whose first leaves
+    __device__ static void push(u32x4& w, bf16_t v) {
+        w = u32x4{__builtin_amdgcn_alignbit(w.y, w.x, 16), __builtin_amdgcn_alignbit(w.z, w.y, 16),
+                  __builtin_amdgcn_alignbit(w.w, w.z, 16), __builtin_amdgcn_alignbit(v.bits, w.w, 16)};
+    }
+    __device__ static void push(u32x4& w, float v) { w = u32x4{w.y, w.z, w.w, __float_as_uint(v)}; }
+    __device__ void store(int tid, T* tile) const {
+        const int row0 = tid / kLanes;
+        T* p = tile + row0 * kC + ((tid % kLanes) ^ Mat<T>::swz(row0)) * kPer;
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) ok = Mat<T>::finite(w[i]) && ok;
-        return ok;
+        for (int i = 0; i < kPasses; ++i) *reinterpret_cast<u32x4*>(p + i * kRowsPass * kC) = w[i];
+    }
+    __device__ float zero_sum(float v) const {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) v = Mat<T>::zero_sum(w[i], v);
+        return v;
     }
 };
 
 template <typename T>
 __device__ __forceinline__ const T* head_base(const WalkTensor& t, int64_t b, int64_t h, int heads, int64_t L) {
-    return static_cast<const T*>(t.p) + ((b * t.heads + h / (heads / t.heads)) * t.rows) * L;
+    return static_cast<const T*>(t.p) + ((b * t.heads + (uint32_t)h / (uint32_t)(heads / t.heads)) * t.rows) * L;
 }
 
 // The block's place: heads that share tensors run on one XCD, whose L2 then holds them (blocks go to
 // the 8 XCDs in turn).
-__device__ __forceinline__ int64_t walk_block(int64_t n) {
-    const int64_t id = blockIdx.x, per = n / 8;
+__device__ __forceinline__ uint32_t walk_block(uint32_t n) {
+    const uint32_t id = blockIdx.x, per = n / 8;
     return id < per * 8 ? (id % 8) * per + id / 8 : id;
 }
 
 // --------------------------------------------------------------------------------------------
-// the state: KT x DT tiles of 16 x features by 16 z features; wave w owns z features 16 DT w .. + 16 DT - 1
+// the state: 16 z features a wave, and of the x features all or half: KF tiles of 16 by 16
 // --------------------------------------------------------------------------------------------
-template <int KT, int DT>
+template <int KF>
 struct State {
-    f32x4 s[KT][DT];
+    f32x4 s[KF];
+    int xf, zf;                         // the wave's first x and z feature
 
     template <typename F>
-    __device__ void each(F f) {         // f(x feature of the tile's row 0, z feature, its four values)
-        const int l = lane_id(), w = wave_id();
+    __device__ void each(F f) {         // f(x feature of the lane's first value, z feature, its four values)
+        const int l = here(lane_id());
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) f(k * 16 + (l >> 4) * 4, (w * DT + d) * 16 + (l & 15), s[k][d]);
+        for (int k = 0; k < KF; ++k) f(xf + k * 16 + (l >> 4) * 4, zf + (l & 15), s[k]);
     }
     __device__ void load(const float* p, const WalkArgs& a) {
         each([&](int xf, int zf, f32x4& v) {
@@ -280,148 +369,183 @@ struct State {
                 if (xf + r < a.x.rows && zf < a.z.rows) p[(int64_t)(xf + r) * a.s_x + (int64_t)zf * a.s_z] = v[r];
         });
     }
-    __device__ void decay(float a) {
+    __device__ void decay(bool cut, float a) {      // both the same for the whole wave
+        if (cut) {
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
+            for (int k = 0; k < KF; ++k) s[k] = f32x4{0, 0, 0, 0};
+        } else {
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-                s[k][d] = a < 0.0f ? f32x4{0, 0, 0, 0} : s[k][d] * a;
+            for (int k = 0; k < KF; ++k) s[k] *= a;
+        }
     }
 };
 
-// S <- A S + sum_j up_j y_j z_j^T; zf: the wave's z, four tokens a lane, for each of the four token tiles
-template <typename T, int NS, int KT, int DT>
-__device__ __forceinline__ void update(State<KT, DT>& S, const T* ys, const T* zs, const ChunkDecay& c, float uscale) {
+__device__ __forceinline__ float uniform(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
+// S <- A S + sum_j up_j y_j z_j^T
+template <typename T, bool REV, int NS, bool HIDE, int KF>
+__device__ __forceinline__ void update(State<KF>& S, const T* ys, const T* zs, const ChunkDecay& c, bool cut, bool bad) {
     using M = Mat<T>;
-    const int l = lane_id(), w = wave_id(), row = l & 15, tok = (l >> 4) * 4;
-    S.decay(c.a);
-    if (c.bad[0]) {
+    const int l = fresh<HIDE>(lane_id()), four = (l >> 4) * 4;
+    ys += S.xf * kC;
+    zs += S.zf * kC;
+    S.decay(cut, uniform(c.a));
+    if (bad) {
+        const int lb = here(l);
 #pragma unroll 1
         for (int j = 0; j < kC; ++j) {
-            const float up = c.up[j];
-            if (up < 0.0f) continue;
+            if (!leaves<REV>(c, j)) continue;
+            const float zv = tile_value(zs, lb & 15, j) * c.up[j];
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
+            for (int k = 0; k < KF; ++k) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const float zv = Storage<T>::load1(zs + ((w * DT + d) * 16 + row) * M::kStride + j) * (up * uscale);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        S.s[k][d][r] = fmaf(Storage<T>::load1(ys + (k * 16 + tok + r) * M::kStride + j), zv, S.s[k][d][r]);
-                }
+                for (int r = 0; r < 4; ++r) S.s[k][r] = fmaf(tile_value(ys + k * 16 * kC, (lb >> 4) * 4 + r, j), zv, S.s[k][r]);
+                __builtin_amdgcn_sched_barrier(0);      // few values at a time: registers count, not speed
+            }
         }
         return;
     }
 #pragma unroll
     for (int p = 0; p < 2; ++p) {                               // 32 tokens
-        typename M::Frag zw[2][DT][NS];
+        typename M::Frag zw[2][NS];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const int t0 = (2 * p + q) * 16 + tok;
-            f32x4 up = *reinterpret_cast<const f32x4*>(&c.up[t0]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) up[r] = up[r] < 0.0f ? 0.0f : up[r] * uscale;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-                M::template split<NS>(M::widen(M::direct(zs + ((w * DT + d) * 16 + row) * M::kStride + t0)) * up, zw[q][d]);
+            const f32x4 up = *reinterpret_cast<const f32x4*>(&c.up[(2 * p + q) * 16 + four]);
+            M::template split<NS>(M::widen(M::direct(l, zs, 2 * p + q)) * up, zw[q]);
         }
 #pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            const T* y = ys + (k * 16 + row) * M::kStride + 2 * p * 16 + tok;
-            const typename M::Frag y0 = M::direct(y), y1 = M::direct(y + 16);
+        for (int k = 0; k < KF; ++k) {
+            const typename M::Frag y0 = M::direct(l, ys + k * 16 * kC, 2 * p), y1 = M::direct(l, ys + k * 16 * kC, 2 * p + 1);
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int n = 0; n < NS; ++n) S.s[k][d] = M::mma(y0, y1, zw[0][d][n], zw[1][d][n], S.s[k][d]);
+            for (int n = 0; n < NS; ++n) S.s[k] = M::mma(y0, y1, zw[0][n], zw[1][n], S.s[k]);
         }
     }
 }
 
-__device__ __forceinline__ float sum16(float v) {       // over the 16 lanes of a row, to all of them
-#pragma unroll
-    for (int m = 1; m < 16; m *= 2) v += __shfl_xor(v, m, 16);
-    return v;
+// The four values' sums over the 16 lanes of a row: lane 7 has those of x and z, lane 15 of y and w.
+__device__ __forceinline__ f32x2 sum16(const f32x4& v) {
+    return f32x2{row_sum2_to_7_15(v.x, v.y), row_sum2_to_7_15(v.z, v.w)};
+}
+// and their place: two floats of four consecutive ones, from lanes 7 and 15
+__device__ __forceinline__ void store_sum16(int l, float* four, const f32x2& s) {
+    if ((l & 7) == 7) {
+        float* p = four + ((l >> 3) & 1);
+        p[0] = s.x;
+        p[2] = s.y;
+    }
 }
 
-template <typename T, int KC, int VP, int MODE>
+// bf16: the x features are split over two waves, so that twice the waves share a chunk's latencies; the
+// state that x is multiplied with then passes through LDS, rounded, or where it is split into terms in 32 bits.
+template <typename T, int KC, int VP>
+constexpr int walk_parts() {
+    return sizeof(T) == 2 && KC >= VP ? 2 : 1;
+}
+template <typename T, int NO>
+using WalkCopy = std::conditional_t<NO == 1, typename Mat<T>::Frag, f32x4>;
+
+template <typename T, int KC, int VP, int MODE, int NO>
 struct WalkSmem {
-    static constexpr int kS = Mat<T>::kStride;
-    __attribute__((aligned(16))) T x[KC * kS];
-    __attribute__((aligned(16))) T y[KC * kS];
-    __attribute__((aligned(16))) T z[VP * kS];
-    __attribute__((aligned(16))) T e[MODE != kWalkPlain ? VP * kS : 8];
-    __attribute__((aligned(16))) T p[kC * kS];          // x's rows
+    static constexpr int kParts = walk_parts<T, KC, VP>(), kWaves = VP / 16 * kParts;
+    __attribute__((aligned(16))) T x[KC * kC];
+    __attribute__((aligned(16))) T y[KC * kC];
+    __attribute__((aligned(16))) T z[VP * kC];
+    __attribute__((aligned(16))) T e[MODE != kWalkPlain ? VP * kC : 8];
+    __attribute__((aligned(16))) T p[kC * kC];          // x's rows
+    __attribute__((aligned(16))) WalkCopy<T, NO> s[kParts == 2 ? KC * VP / 4 : 1];     // the operands of the lanes
     ChunkDecay c[2];
-    __attribute__((aligned(16))) float rsum[MODE == kWalkDq ? kC : 4];
-    __attribute__((aligned(16))) float csum[MODE == kWalkDq ? kWalkWaves : 1][kC];
-    __attribute__((aligned(16))) float dot[MODE != kWalkPlain ? kWalkWaves : 1][kC];
-    float xdot[kWalkWaves];
+    __attribute__((aligned(16))) float rsum[MODE == kWalkDq ? kWaves / 4 : 1][kC];
+    __attribute__((aligned(16))) float csum[MODE == kWalkDq ? 4 : 1][kC];
+    __attribute__((aligned(16))) float dot[MODE != kWalkPlain ? VP / 16 : 1][kC];
+    float xdot[kWaves];
 };
 
-template <typename T, typename TO, int KC, int VP, int MODE, int NS, int NO>
-__global__ __launch_bounds__(kWalkThreads) void walk_kernel(WalkArgs a) {
+// Waves of a SIMD that the registers are to leave room for.
+template <typename T, int KC, int VP, int MODE>
+constexpr int walk_waves() {
+    if (sizeof(T) == 4) return VP == 64 ? 1 : 2;
+    return 4;
+}
+template <typename T, int KC, int VP>
+constexpr int walk_threads() {
+    return VP * 4 * walk_parts<T, KC, VP>();
+}
+
+// Wave (z tile, part): 16 of z's features, and of the x features and the out's tokens all or, of two waves,
+// half.  All waves share the products of x and y by strips of 16 x's and parts of the y's.
+template <typename T, typename TO, int KC, int VP, int MODE, bool REV, int NS, int NO>
+__global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP, MODE>())) void walk_kernel(WalkArgs a) {
     using M = Mat<T>;
     using Frag = typename M::Frag;
-    constexpr int KT = KC / 16, DT = VP / (16 * kWalkWaves), VT = VP / 16, kS = M::kStride;
+    constexpr int KT = KC / 16, VT = VP / 16, kParts = walk_parts<T, KC, VP>(), KF = KT / kParts, XT = 4 / kParts;
+    constexpr int kWaves = VT * kParts, kThreads = kWaves * 64, kYParts = kWaves / 4, kYTiles = 4 / kYParts;
     constexpr bool kAhead = sizeof(T) == 2;             // the next chunk's tiles are loaded during a chunk
-    __shared__ WalkSmem<T, KC, VP, MODE> sm;
-    const int l = lane_id(), w = wave_id(), col = l & 15, four = (l >> 4) * 4;
+    constexpr bool kTight = MODE != kWalkPlain || VP > KC;
+    __shared__ WalkSmem<T, KC, VP, MODE, NO> sm;
+    const int l = lane_id(), w = wave_id();
     const int64_t L = a.seqlen;
-    const int64_t id = walk_block((int64_t)a.batch * a.heads * a.nseg);
-    const int64_t bh = id / a.nseg, seg = id - bh * a.nseg;
-    const int64_t b = bh / a.heads, h = bh - b * a.heads;
-    const bool rev = a.rev != 0;
+    const uint32_t id = walk_block((uint32_t)a.batch * a.heads * a.nseg);       // at most 2^23 of them
+    const uint32_t row = id / (uint32_t)a.nseg, bat = row / (uint32_t)a.heads;
+    const int64_t bh = row, b = bat, h = row - bat * a.heads, seg = id - row * a.nseg;
     const int chunks = (int)((L + kC - 1) / kC);
     const int first = (int)seg * a.seg_chunks, last = min(chunks, first + a.seg_chunks) - 1;
     const T* xp = head_base<T>(a.x, b, h, a.heads, L);
     const T* yp = head_base<T>(a.y, b, h, a.heads, L);
     const T* zp = head_base<T>(a.z, b, h, a.heads, L);
     const T* ep = MODE != kWalkPlain ? head_base<T>(a.e, b, h, a.heads, L) : nullptr;
-    TO* op = static_cast<TO*>(a.out) + bh * a.z.rows * L;
+    const int part = w / VT, ztile = w % VT;
+    TO* op = static_cast<TO*>(a.out) + (bh * a.z.rows + ztile * 16) * L;        // the wave's first z feature
 
-    State<KT, DT> S;
+    State<KF> S;
+    S.xf = part * KF * 16;
+    S.zf = ztile * 16;
     const int64_t sz = (int64_t)a.x.rows * a.z.rows;
     S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a);
 
-    constexpr int64_t kBound = (int64_t)KT * DT * 4 * kWalkThreads;
     // boundary n of the row: the state there, stored (dq) or multiplied with the one that dq stored (dk)
+    const auto bound_at = [&](int64_t n) {
+        return a.bound + ((bh * (a.nb + 1) + n) * KF * kThreads + here(threadIdx.x)) * 4;
+    };
     const auto bound_store = [&](int64_t n) {
-        float* p = a.bound + (bh * (a.nb + 1) + n) * kBound + threadIdx.x * 4;
+        float* p = bound_at(n);
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p + (k * DT + d) * 4 * kWalkThreads) = S.s[k][d];
+        for (int k = 0; k < KF; ++k) *reinterpret_cast<f32x4*>(p + k * 4 * kThreads) = S.s[k];
     };
     const auto bound_dot = [&](int64_t n) {              // block-uniform
-        const float* p = a.bound + (bh * (a.nb + 1) + n) * kBound + threadIdx.x * 4;
+        const float* p = bound_at(n);
         float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
+        for (int k = 0; k < KF; ++k) {
+            const f32x4 o = *reinterpret_cast<const f32x4*>(p + k * 4 * kThreads);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const f32x4 o = *reinterpret_cast<const f32x4*>(p + (k * DT + d) * 4 * kWalkThreads);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v = fmaf(o[r], S.s[k][d][r], v);
-            }
+            for (int r = 0; r < 4; ++r) v = fmaf(o[r], S.s[k][r], v);
+        }
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
         __syncthreads();
         if (l == 0) sm.xdot[w] = v;
         __syncthreads();
-        if (threadIdx.x == 0)
-            a.dot[bh * (a.nb + 1) + n] = (sm.xdot[0] + sm.xdot[1]) + (sm.xdot[2] + sm.xdot[3]);
+        if (threadIdx.x == 0) {
+            v = sm.xdot[0];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i) v += sm.xdot[i];
+            a.dot[bh * (a.nb + 1) + n] = v;
+        }
     };
 
-    TileRegs<T, KC> xr, yr;
-    TileRegs<T, VP> zr, er;
+    TileRegs<T, KC, kThreads> xr, yr;
+    TileRegs<T, VP, kThreads> zr, er;
     TokenDecay td{0.0f, 1};
-    const int coef_wave = rev ? kWalkWaves - 1 : 0;     // the wave with the fewest products of x and y
+    const int coef_wave = REV ? 3 : kYParts > 1 ? 4 : 0;    // a wave with the fewest products of x and y
     const auto load = [&](int chunk) {
+        const int tid = fresh<kTight>(threadIdx.x);
         const int64_t t0 = (int64_t)chunk * kC;
-        xr.load(xp, a.x.rows, t0, L);
-        yr.load(yp, a.y.rows, t0, L);
-        zr.load(zp, a.z.rows, t0, L);
-        if constexpr (MODE != kWalkPlain) er.load(ep, a.e.rows, t0, L);
+        xr.load(tid, xp, a.x.rows, t0, L);
+        yr.load(tid, yp, a.y.rows, t0, L);
+        zr.load(tid, zp, a.z.rows, t0, L);
+        if constexpr (MODE != kWalkPlain) er.load(tid, ep, a.e.rows, t0, L);
     };
     const auto load_td = [&](int chunk) {
         if (w == coef_wave) td = load_decay(a, b, h, (int64_t)chunk * kC + l);
@@ -431,33 +555,51 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(WalkArgs a) {
         if constexpr (MODE != kWalkPlain) {
             const int64_t t = (int64_t)chunk * kC + threadIdx.x;
             if (threadIdx.x < kC && t < L) {
-                float v = (sm.dot[0][threadIdx.x] + sm.dot[1][threadIdx.x]) + (sm.dot[2][threadIdx.x] + sm.dot[3][threadIdx.x]);
+                const int i = threadIdx.x;
+                float v = sm.dot[0][i];
+#pragma unroll
+                for (int n = 1; n < VT; ++n) v += sm.dot[n][i];
                 if constexpr (MODE == kWalkDq) {
-                    const int i = threadIdx.x;
-                    v += sm.rsum[i] - ((sm.csum[0][i] + sm.csum[1][i]) + (sm.csum[2][i] + sm.csum[3][i]));
+#pragma unroll
+                    for (int n = 0; n < kYParts; ++n) v += sm.rsum[n][i];
+                    v -= (sm.csum[0][i] + sm.csum[1][i]) + (sm.csum[2][i] + sm.csum[3][i]);
                 }
                 a.r[bh * L + t] = v;
             }
         }
     };
 
-    const int step = rev ? -1 : 1, begin = rev ? last : first, n = last - first + 1;
+    constexpr int step = REV ? -1 : 1;
+    const int begin = REV ? last : first, n = last - first + 1;
     if (threadIdx.x == 0) sm.c[0].bad[0] = sm.c[1].bad[0] = 0;
     load_td(begin);
     if (kAhead) load(begin);
-    if (w == coef_wave) chunk_decay(td, rev, sm.c[0]);
+    if (w == coef_wave) chunk_decay<REV>(td, sm.c[0], a.iscale, a.uscale);
     if (n > 1) load_td(begin + step);
     for (int it = 0; it < n; ++it) {
-        const int chunk = begin + it * step;
+        const int chunk = begin + it * step, tid = fresh<kTight>(threadIdx.x);
         ChunkDecay& c = sm.c[it & 1];
         __syncthreads();                                // the tiles of the chunk before are read
         if (it > 0) flush_r(chunk - step);
         if (!kAhead) load(chunk);
-        xr.store(sm.x);
-        yr.store(sm.y);
-        zr.store(sm.z);
-        if constexpr (MODE != kWalkPlain) er.store(sm.e);
-        if (!(yr.finite() && zr.finite())) c.bad[0] = 1;
+        const int64_t ct = (int64_t)chunk * kC;
+        xr.settle(tid, xp, a.x.rows, ct, L);
+        yr.settle(tid, yp, a.y.rows, ct, L);
+        zr.settle(tid, zp, a.z.rows, ct, L);
+        if constexpr (MODE != kWalkPlain) er.settle(tid, ep, a.e.rows, ct, L);
+        xr.store(tid, sm.x);
+        yr.store(tid, sm.y);
+        zr.store(tid, sm.z);
+        if constexpr (MODE != kWalkPlain) er.store(tid, sm.e);
+        if constexpr (kParts == 2) {
+#pragma unroll
+            for (int k = 0; k < KF; ++k) {
+                auto& copy = sm.s[((part * KF + k) * VT + ztile) * 64 + l];
+                if constexpr (NO == 1) copy = M::round(S.s[k]);
+                else copy = S.s[k];
+            }
+        }
+        if (zr.zero_sum(yr.zero_sum(0.0f)) != 0.0f) c.bad[0] = 1;
         if constexpr (MODE == kWalkDq) {
             if (chunk > 0 && chunk % a.bound_chunks == 0) bound_store(chunk / a.bound_chunks);
         }
@@ -469,171 +611,169 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(WalkArgs a) {
         __syncthreads();
         if (kAhead && it + 1 < n) load(chunk + step);
 
-        // products of x and y, weighted: strip w of 16 x's
+        const bool cut = __builtin_amdgcn_readfirstlane(__float_as_int(c.a)) < 0;      // a sequence starts in the chunk
+        // products of x and y, weighted: 16 x's by all y's, or a part of them
         {
+            const int l = fresh<kTight>(lane_id()), col = l & 15, four = (l >> 4) * 4;
             if (w == coef_wave && it + 1 < n) {
                 ChunkDecay& cn = sm.c[(it + 1) & 1];
-                chunk_decay(td, rev, cn);
+                chunk_decay<REV>(td, cn, a.iscale, a.uscale);
                 if (l == 0) cn.bad[0] = 0;
                 if (it + 2 < n) load_td(chunk + 2 * step);
             }
+            const int strip = w % 4, ypart = w / 4;
             Frag xf[KT];
 #pragma unroll
-            for (int k = 0; k < KT; ++k) xf[k] = M::transposed(sm.x + k * 16 * kS + w * 16);
-            const int xt = w * 16 + col;
+            for (int k = 0; k < KT; ++k) xf[k] = M::transposed(l, sm.x + k * 16 * kC, strip);
+            const int xt = strip * 16 + col;
             const float xhi = c.hi[xt], xlo = c.lo[xt];
-            const int xstart = c.start[xt];
             float rs = 0.0f;
-#pragma unroll
-            for (int yt = 0; yt < 4; ++yt) {
+#pragma unroll 1
+            for (int i = 0; i < kYTiles; ++i) {
+                const int yt = ypart * kYTiles + i;
                 f32x4 d = {0, 0, 0, 0};
-                T* pp = sm.p + xt * kS + yt * 16 + four;
-                const bool needed = rev ? yt >= w : yt <= w;
-                float cs[4] = {0, 0, 0, 0};
-                if (needed) {
+                Frag* pp = reinterpret_cast<Frag*>(sm.p + strip * 16 * kC + M::direct_at(l, yt));
+                f32x4 cs = {0, 0, 0, 0};
+                if (REV ? yt >= strip : yt <= strip) {
 #pragma unroll
                     for (int k = 0; k < KT; k += 2)
-                        d = M::mma(M::transposed(sm.y + k * 16 * kS + yt * 16), M::transposed(sm.y + (k + 1) * 16 * kS + yt * 16),
-                                   xf[k], xf[k + 1], d);
+                        d = M::mma(M::transposed(l, sm.y + k * 16 * kC, yt), M::transposed(l, sm.y + (k + 1) * 16 * kC, yt), xf[k],
+                                   xf[k + 1], d);
                     const int y0 = yt * 16 + four;
                     const f32x4 yhi = *reinterpret_cast<const f32x4*>(&c.hi[y0]), ylo = *reinterpret_cast<const f32x4*>(&c.lo[y0]);
                     f32x4 p;
-                    bool on[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int y = y0 + r;
-                        on[r] = rev ? xt <= y && c.start[y] <= xt : y <= xt && xstart <= y;
-                        const float dec = rev ? pair_decay(yhi[r], ylo[r], xhi, xlo) : pair_decay(xhi, xlo, yhi[r], ylo[r]);
-                        p[r] = on[r] ? d[r] * (dec * a.pscale) : 0.0f;
+                    for (int r = 0; r < 4; ++r)
+                        p[r] = d[r] * ((REV ? pair_decay(yhi[r], ylo[r], xhi, xlo) : pair_decay(xhi, xlo, yhi[r], ylo[r])) * a.pscale);
+                    const bool masked = cut || yt == strip;
+                    bool on[4] = {true, true, true, true};
+                    if (masked) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            on[r] = takes<REV>(c, xt, y0 + r);
+                            p[r] = on[r] ? p[r] : 0.0f;
+                        }
                     }
                     if constexpr (MODE == kWalkDq) {
                         f32x4 d2 = {0, 0, 0, 0};
+                        __builtin_amdgcn_sched_barrier(0);      // not both products' operands at once
 #pragma unroll
                         for (int k = 0; k < VT; k += 2)
-                            d2 = M::mma(M::transposed(sm.z + k * 16 * kS + yt * 16), M::transposed(sm.z + (k + 1) * 16 * kS + yt * 16),
-                                        M::transposed(sm.e + k * 16 * kS + w * 16), M::transposed(sm.e + (k + 1) * 16 * kS + w * 16), d2);
+                            d2 = M::mma(M::transposed(l, sm.z + k * 16 * kC, yt), M::transposed(l, sm.z + (k + 1) * 16 * kC, yt),
+                                        M::transposed(l, sm.e + k * 16 * kC, strip), M::transposed(l, sm.e + (k + 1) * 16 * kC, strip), d2);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            const float wv = on[r] ? p[r] * d2[r] : 0.0f;
-                            rs += wv;
-                            cs[r] = sum16(wv);
+                            cs[r] = on[r] ? p[r] * d2[r] : 0.0f;
+                            rs += cs[r];
                         }
                     }
-                    *reinterpret_cast<Frag*>(pp) = M::round(p);
-                } else if (rev ? (w & 1) && yt == w - 1 : !(w & 1) && yt == w + 1) {
-                    *reinterpret_cast<Frag*>(pp) = M::round(d);      // the other half of a step of 32 tokens
+                    *pp = M::round(p);
+                } else if (REV ? (strip & 1) && yt == strip - 1 : !(strip & 1) && yt == strip + 1) {
+                    *pp = M::round(d);      // the other half of a step of 32 tokens
                 }
                 if constexpr (MODE == kWalkDq) {
-                    if (col == 0) *reinterpret_cast<f32x4*>(&sm.csum[w][yt * 16 + four]) = f32x4{cs[0], cs[1], cs[2], cs[3]};
+                    store_sum16(l, &sm.csum[strip][yt * 16 + four], sum16(cs));
                 }
             }
             if constexpr (MODE == kWalkDq) {
                 rs += __shfl_xor(rs, 16);
                 rs += __shfl_xor(rs, 32);
-                if (l < 16) sm.rsum[xt] = rs;
+                if (l < 16) sm.rsum[ypart][xt] = rs;
             }
         }
         __syncthreads();
 
         // out, from the state that enters the chunk and from the chunk's own products
+        const bool bad = __builtin_amdgcn_readfirstlane(c.bad[0]) != 0;
         {
-            f32x4 o[4][DT];
+            const int l = fresh<kTight>(lane_id()), col = l & 15, four = (l >> 4) * 4;
+            // the wave's token tiles: all, or the first and the last, or the two between
+            const auto token_tile = [&](int i) { return kParts == 1 ? i : part ? 1 + i : 3 * i; };
+            f32x4 os[XT];
 #pragma unroll
-            for (int xt = 0; xt < 4; ++xt)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[xt][d] = f32x4{0, 0, 0, 0};
-#pragma unroll
+            for (int i = 0; i < XT; ++i) os[i] = f32x4{0, 0, 0, 0};
+#pragma unroll (kParts == 1 || NO == 1 ? KT / 2 : 1)
             for (int k = 0; k < KT; k += 2) {
-                Frag s0[DT][NO], s1[DT][NO];
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    M::template split<NO>(S.s[k][d], s0[d]);
-                    M::template split<NO>(S.s[k + 1][d], s1[d]);
+                Frag s0[NO], s1[NO];
+                if constexpr (kParts == 1) {
+                    M::template split<NO>(S.s[k], s0);
+                    M::template split<NO>(S.s[k + 1], s1);
+                } else {
+                    const auto &c0 = sm.s[(k * VT + ztile) * 64 + l], &c1 = sm.s[((k + 1) * VT + ztile) * 64 + l];
+                    if constexpr (NO == 1) {
+                        s0[0] = c0;
+                        s1[0] = c1;
+                    } else {
+                        M::template split<NO>(c0, s0);
+                        M::template split<NO>(c1, s1);
+                    }
                 }
 #pragma unroll
-                for (int xt = 0; xt < 4; ++xt) {
-                    const Frag x0 = M::transposed(sm.x + k * 16 * kS + xt * 16), x1 = M::transposed(sm.x + (k + 1) * 16 * kS + xt * 16);
+                for (int i = 0; i < XT; ++i) {
+                    const Frag f0 = M::transposed(l, sm.x + k * 16 * kC, token_tile(i)), f1 = M::transposed(l, sm.x + (k + 1) * 16 * kC, token_tile(i));
 #pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int q = 0; q < NO; ++q) o[xt][d] = M::mma(x0, x1, s0[d][q], s1[d][q], o[xt][d]);
+                    for (int q = 0; q < NO; ++q) os[i] = M::mma(f0, f1, s0[q], s1[q], os[i]);
                 }
             }
-            const bool bad = c.bad[0] != 0;
+            Frag zf[4];
+            const T* zt = sm.z + ztile * 16 * kC;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) zf[i] = M::direct(l, zt, i);
             const int64_t t0 = (int64_t)chunk * kC;
 #pragma unroll
-            for (int xt = 0; xt < 4; ++xt) {
-                const int x0 = xt * 16 + four;
+            for (int i = 0; i < XT; ++i) {
+                const int xt = token_tile(i), x0 = xt * 16 + four;
+                f32x4 o = os[i];
                 const f32x4 in = *reinterpret_cast<const f32x4*>(&c.in[x0]);
-                float rd[4] = {0, 0, 0, 0};
+                o *= in;
+                if (cut) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[xt][d][r] = in[r] < 0.0f ? 0.0f : o[xt][d][r] * (in[r] * a.iscale);
-                    if constexpr (MODE != kWalkPlain) {
-                        const f32x4 ev = M::widen(M::direct(sm.e + ((w * DT + d) * 16 + col) * kS + x0));
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) rd[r] = in[r] < 0.0f ? 0.0f : fmaf(o[xt][d][r], ev[r], rd[r]);
-                    }
+                    for (int r = 0; r < 4; ++r) o[r] = enters<REV>(c, x0 + r) ? o[r] : 0.0f;
                 }
                 if constexpr (MODE != kWalkPlain) {
+                    f32x4 rd = o * M::widen(M::direct(l, sm.e + ztile * 16 * kC, xt));
+                    if (cut) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) rd[r] = sum16(rd[r]);
-                    if (col == 0)
-                        *reinterpret_cast<f32x4*>(&sm.dot[w][x0]) = MODE == kWalkDk ? f32x4{-rd[0], -rd[1], -rd[2], -rd[3]}
-                                                                                    : f32x4{rd[0], rd[1], rd[2], rd[3]};
+                        for (int r = 0; r < 4; ++r) rd[r] = enters<REV>(c, x0 + r) ? rd[r] : 0.0f;
+                    }
+                    store_sum16(l, &sm.dot[ztile][x0], sum16(MODE == kWalkDk ? -rd : rd));
                 }
                 if (!bad) {
+                    const T* pp = sm.p + xt * 16 * kC;
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        if (rev ? 2 * q + 1 < xt : 2 * q > xt) continue;
-                        const T* pp = sm.p + (xt * 16 + col) * kS + q * 32 + four;
-                        const Frag p0 = M::direct(pp), p1 = M::direct(pp + 16);
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            const T* zz = sm.z + ((w * DT + d) * 16 + col) * kS + q * 32 + four;
-                            o[xt][d] = M::mma(p0, p1, M::direct(zz), M::direct(zz + 16), o[xt][d]);
-                        }
-                    }
+                    for (int q = 0; q < 2; ++q)
+                        if (REV ? 2 * q + 1 >= xt : 2 * q <= xt)
+                            o = M::mma(M::direct(l, pp, 2 * q), M::direct(l, pp, 2 * q + 1), zf[2 * q], zf[2 * q + 1], o);
                 } else {
+                    const int lb = here(l);
 #pragma unroll 1
                     for (int y = 0; y < kC; ++y)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            const int x = x0 + r;
-                            if (!(rev ? x <= y && c.start[y] <= x : y <= x && c.start[x] <= y)) continue;
-                            const float pv = Storage<T>::load1(sm.p + x * kS + y);
-#pragma unroll
-                            for (int d = 0; d < DT; ++d)
-                                o[xt][d][r] = fmaf(pv, Storage<T>::load1(sm.z + ((w * DT + d) * 16 + col) * kS + y), o[xt][d][r]);
+                            if (takes<REV>(c, xt * 16 + (lb >> 4) * 4 + r, y))
+                                o[r] = fmaf(tile_value(sm.p + xt * 16 * kC, (lb >> 4) * 4 + r, y), tile_value(zt, lb & 15, y), o[r]);
                         }
                 }
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const int zf = (w * DT + d) * 16 + col;
-                    if (zf >= a.z.rows) continue;
-                    float v[4] = {o[xt][d].x, o[xt][d].y, o[xt][d].z, o[xt][d].w};
-                    TO* dst = op + (int64_t)zf * L;
+                if (ztile * 16 + col < a.z.rows) {
+                    TO* dst = op + col * L + t0 + x0;
                     if (t0 + x0 + 4 <= L) {
-                        if constexpr (sizeof(TO) == 2)
-                            *reinterpret_cast<u32x2_a2*>(dst + t0 + x0) = Mat<bf16_t>::round(o[xt][d]);
-                        else
-                            *reinterpret_cast<u32x4_a4*>(dst + t0 + x0) = Storage<float>::pack(v);
+                        if constexpr (sizeof(TO) == 2) *reinterpret_cast<u32x2_a2*>(dst) = Mat<bf16_t>::round(o);
+                        else *reinterpret_cast<u32x4_a4*>(dst) = __builtin_bit_cast(u32x4, o);
                     } else {
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (t0 + x0 + r < L) Storage<TO>::store1(dst + t0 + x0 + r, v[r]);
+                            if (t0 + x0 + r < L) Storage<TO>::store1(dst + r, o[r]);
                     }
                 }
             }
         }
-        update<T, NS>(S, sm.y, sm.z, c, a.uscale);
+        update<T, REV, NS, kTight>(S, sm.y, sm.z, c, cut, bad);
     }
     if constexpr (MODE != kWalkPlain) {
         __syncthreads();
         flush_r(begin + (n - 1) * step);
     }
-    const bool ends = rev ? seg == 0 : seg == a.nseg - 1;       // the state leaves the row
+    const bool ends = REV ? seg == 0 : seg == a.nseg - 1;       // the state leaves the row
     if constexpr (MODE == kWalkDq) {
         if (ends && a.bound_end) bound_store(a.nb);
     }
@@ -646,62 +786,67 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(WalkArgs a) {
 // --------------------------------------------------------------------------------------------
 template <typename T, int KC, int VP>
 struct AggSmem {
-    __attribute__((aligned(16))) T y[KC * Mat<T>::kStride];
-    __attribute__((aligned(16))) T z[VP * Mat<T>::kStride];
+    __attribute__((aligned(16))) T y[KC * kC];
+    __attribute__((aligned(16))) T z[VP * kC];
     ChunkDecay c[2];
 };
 
-template <typename T, int KC, int VP, int NS>
-__global__ __launch_bounds__(kWalkThreads) void walk_aggregate(WalkArgs a) {
-    constexpr int KT = KC / 16, DT = VP / (16 * kWalkWaves);
+template <typename T, int KC, int VP, bool REV, int NS>
+__global__ __launch_bounds__((walk_threads<T, KC, VP>())) void walk_aggregate(WalkArgs a) {
+    constexpr int VT = VP / 16, KF = KC / 16 / walk_parts<T, KC, VP>(), kThreads = walk_threads<T, KC, VP>();
     __shared__ AggSmem<T, KC, VP> sm;
     const int l = lane_id(), w = wave_id();
     const int64_t L = a.seqlen;
     // the segment that nothing enters after it is left out
-    const int64_t id = walk_block((int64_t)a.batch * a.heads * (a.nseg - 1));
-    const int64_t bh = id / (a.nseg - 1);
-    const bool rev = a.rev != 0;
-    const int64_t seg = id - bh * (a.nseg - 1) + (rev ? 1 : 0);
-    const int64_t b = bh / a.heads, h = bh - b * a.heads;
+    const uint32_t id = walk_block((uint32_t)a.batch * a.heads * (a.nseg - 1));
+    const uint32_t row = id / (uint32_t)(a.nseg - 1), bat = row / (uint32_t)a.heads;
+    const int64_t bh = row, b = bat, h = row - bat * a.heads, seg = id - row * (a.nseg - 1) + (REV ? 1 : 0);
     const int chunks = (int)((L + kC - 1) / kC);
     const int first = (int)seg * a.seg_chunks, last = min(chunks, first + a.seg_chunks) - 1;
     const T* yp = head_base<T>(a.y, b, h, a.heads, L);
     const T* zp = head_base<T>(a.z, b, h, a.heads, L);
-    State<KT, DT> S;
+    State<KF> S;
+    S.xf = w / VT * KF * 16;
+    S.zf = w % VT * 16;
     S.load(nullptr, a);
     float all = 1.0f;
-    TileRegs<T, KC> yr;
-    TileRegs<T, VP> zr;
-    const int step = rev ? -1 : 1, begin = rev ? last : first, n = last - first + 1;
+    TileRegs<T, KC, kThreads> yr;
+    TileRegs<T, VP, kThreads> zr;
+    constexpr int step = REV ? -1 : 1;
+    const int begin = REV ? last : first, n = last - first + 1;
     if (threadIdx.x == 0) sm.c[0].bad[0] = sm.c[1].bad[0] = 0;
     TokenDecay td{0.0f, 1};
     if (w == 0) {
         td = load_decay(a, b, h, (int64_t)begin * kC + l);
-        chunk_decay(td, rev, sm.c[0]);
+        chunk_decay<REV>(td, sm.c[0], a.iscale, a.uscale);
         if (n > 1) td = load_decay(a, b, h, (int64_t)(begin + step) * kC + l);
     }
-    yr.load(yp, a.y.rows, (int64_t)begin * kC, L);
-    zr.load(zp, a.z.rows, (int64_t)begin * kC, L);
+    const int tid = threadIdx.x;
+    yr.load(tid, yp, a.y.rows, (int64_t)begin * kC, L);
+    zr.load(tid, zp, a.z.rows, (int64_t)begin * kC, L);
     for (int it = 0; it < n; ++it) {
         const int chunk = begin + it * step;
         ChunkDecay& c = sm.c[it & 1];
         __syncthreads();
-        yr.store(sm.y);
-        zr.store(sm.z);
-        if (!(yr.finite() && zr.finite())) c.bad[0] = 1;
+        yr.settle(tid, yp, a.y.rows, (int64_t)chunk * kC, L);
+        zr.settle(tid, zp, a.z.rows, (int64_t)chunk * kC, L);
+        yr.store(tid, sm.y);
+        zr.store(tid, sm.z);
+        if (zr.zero_sum(yr.zero_sum(0.0f)) != 0.0f) c.bad[0] = 1;
         __syncthreads();
         if (it + 1 < n) {
-            yr.load(yp, a.y.rows, (int64_t)(chunk + step) * kC, L);
-            zr.load(zp, a.z.rows, (int64_t)(chunk + step) * kC, L);
+            yr.load(tid, yp, a.y.rows, (int64_t)(chunk + step) * kC, L);
+            zr.load(tid, zp, a.z.rows, (int64_t)(chunk + step) * kC, L);
             if (w == 0) {
                 ChunkDecay& cn = sm.c[(it + 1) & 1];
-                chunk_decay(td, rev, cn);
+                chunk_decay<REV>(td, cn, a.iscale, a.uscale);
                 if (l == 0) cn.bad[0] = 0;
                 if (it + 2 < n) td = load_decay(a, b, h, (int64_t)(chunk + 2 * step) * kC + l);
             }
         }
-        update<T, NS>(S, sm.y, sm.z, c, a.uscale);
-        all = c.a < 0.0f || all < 0.0f ? -1.0f : all * c.a;
+        const bool cut = __builtin_amdgcn_readfirstlane(__float_as_int(c.a)) < 0;
+        update<T, REV, NS, false>(S, sm.y, sm.z, c, cut, __builtin_amdgcn_readfirstlane(c.bad[0]) != 0);
+        all = cut || all < 0.0f ? -1.0f : all * c.a;
     }
     const int64_t sz = (int64_t)a.x.rows * a.z.rows;
     S.store(a.seg + (bh * a.nseg + seg) * sz, a);
@@ -711,10 +856,11 @@ __global__ __launch_bounds__(kWalkThreads) void walk_aggregate(WalkArgs a) {
 // --------------------------------------------------------------------------------------------
 // launches: one T, TO and KC in each translation unit
 // --------------------------------------------------------------------------------------------
-template <typename T, typename TO, int KC, int VP, int MODE, int NS, int NO>
+template <typename T, typename TO, int KC, int VP, int MODE, bool REV, int NS, int NO>
 hipError_t launch_walk_one(const WalkArgs& a, hipStream_t s) {
     const int64_t blocks = (int64_t)a.batch * a.heads * a.nseg;
-    hipLaunchKernelGGL((walk_kernel<T, TO, KC, VP, MODE, NS, NO>), dim3((unsigned)blocks), dim3(kWalkThreads), 0, s, a);
+    hipLaunchKernelGGL((walk_kernel<T, TO, KC, VP, MODE, REV, NS, NO>), dim3((unsigned)blocks), dim3(walk_threads<T, KC, VP>()),
+                       0, s, a);
     return hipGetLastError();
 }
 
@@ -722,11 +868,14 @@ template <typename T, typename TO, int KC, int VP>
 hipError_t launch_walk_vp(const WalkArgs& a, WalkMode mode, bool exact, hipStream_t s) {
     constexpr int kAll = Mat<T>::kSplit ? 3 : 1, kSome = Mat<T>::kSplit ? 2 : 1;
     switch (mode) {
-        case kWalkDq: return launch_walk_one<T, TO, KC, VP, kWalkDq, kAll, kAll>(a, s);
-        case kWalkDk: return launch_walk_one<T, TO, KC, VP, kWalkDk, kAll, kAll>(a, s);
+        case kWalkDq: return launch_walk_one<T, TO, KC, VP, kWalkDq, false, kAll, kAll>(a, s);
+        case kWalkDk: return launch_walk_one<T, TO, KC, VP, kWalkDk, true, kAll, kAll>(a, s);
         default:
-            if (exact) return launch_walk_one<T, TO, KC, VP, kWalkPlain, kAll, 1>(a, s);
-            return launch_walk_one<T, TO, KC, VP, kWalkPlain, kSome, 1>(a, s);
+            if (a.rev)
+                return exact ? launch_walk_one<T, TO, KC, VP, kWalkPlain, true, kAll, 1>(a, s)
+                             : launch_walk_one<T, TO, KC, VP, kWalkPlain, true, kSome, 1>(a, s);
+            return exact ? launch_walk_one<T, TO, KC, VP, kWalkPlain, false, kAll, 1>(a, s)
+                         : launch_walk_one<T, TO, KC, VP, kWalkPlain, false, kSome, 1>(a, s);
     }
 }
 
