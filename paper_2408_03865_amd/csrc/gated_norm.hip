@@ -13,6 +13,35 @@
 namespace pm {
 namespace {
 
+// Offsets of a group's elements: 32 bits, added to a base that is the same for all lanes, where its bytes allow
+// that (all but rows of 2^30 and more elements), else 64.  64-bit addresses of a thread's features took the
+// registers of a whole feature's values.
+template <bool FAR>
+using Offset = std::conditional_t<FAR, int64_t, uint32_t>;
+template <typename T, typename O>
+__device__ __forceinline__ const T* at(const T* base, O off) {
+    return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + off * sizeof(T));
+}
+template <typename T, typename O>
+__device__ __forceinline__ T* at(T* base, O off) {
+    return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + off * sizeof(T));
+}
+bool far(const GatedArgs& a) { return a.dim / a.groups * a.seqlen >= (int64_t)1 << 30; }
+
+// The same raw values, unknown to the compiler: what it computed from them for the sum is computed again after it
+// and not kept, which would take several times their registers.
+template <typename T, int K>
+__device__ __forceinline__ void forget(RawRun<T, K>& r) {
+#pragma unroll
+    for (int i = 0; i < RawRun<T, K>::kVecs; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t v = r.w[i][k];
+            asm volatile("" : "+v"(v));
+            r.w[i][k] = v;
+        }
+}
+
 // Sum over the slices of each token's value, in a fixed order; every thread gets its own tokens' sums.
 template <int GROUPS, int THREADS, int TOK>
 __device__ __forceinline__ void slices_sum(float (&v)[TOK], float (*red)[GROUPS * TOK], int grp) {
@@ -32,7 +61,7 @@ __device__ __forceinline__ void slices_sum(float (&v)[TOK], float (*red)[GROUPS 
         for (int k = 0; k < TOK; ++k) v[k] += red[w][grp * TOK + k];
 }
 
-template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST>
+template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST, bool FAR>
 __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
     constexpr int TOK = Storage<T>::kPerVec, SL = THREADS / GROUPS;
     __shared__ float red[THREADS / 64][GROUPS * TOK];
@@ -51,6 +80,8 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
     const auto body = [&](auto full_tag) {
         constexpr bool FULL = decltype(full_tag)::value;
         constexpr int C = FULL ? KEPT : 0;
+        const int64_t left = L - l0;                            // tokens from the lane's first
+        const auto off = [&](int f) { return (Offset<FAR>)f * (Offset<FAR>)L + (Offset<FAR>)l0; };
         RawRun<T, TOK> xr[KEPT], zr[KEPT];
         float kept[FIRST ? KEPT : 1][TOK];
 #pragma unroll
@@ -58,8 +89,8 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
             xr[i] = zr[i] = RawRun<T, TOK>{};
             const int f = sl + i * SL;
             if (f < per) {
-                xr[i] = load_raw<T, TOK>(x + (int64_t)f * L, l0);
-                zr[i] = load_raw<T, TOK>(z + (int64_t)f * L, l0);
+                xr[i] = load_raw<T, TOK>(at(x, off(f)), 0);
+                zr[i] = load_raw<T, TOK>(at(z, off(f)), 0);
             }
         }
         float s[TOK] = {};
@@ -83,8 +114,8 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
         }
         for (int f = sl + C * SL; f < per; f += SL) {
             float xv[TOK], zv[TOK], v[TOK];
-            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, xv);
-            if constexpr (FIRST) load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
+            load_run<T, TOK, FULL>(at(x, off(f)), 0, left, xv);
+            if constexpr (FIRST) load_run<T, TOK, FULL>(at(z, off(f)), 0, left, zv);
             value(xv, zv, v);
         }
         slices_sum<GROUPS, THREADS, TOK>(s, red, grp);
@@ -103,7 +134,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
                 v[k] = v[k] * r[k] * wv;
                 if constexpr (!FIRST) v[k] *= zv[k] * sigmoid_f(zv[k]);
             }
-            if (!FULL || live) store_run<TO, TOK, FULL>(out + (int64_t)f * L, l0, L, v);
+            if (!FULL || live) store_run<TO, TOK, FULL>(at(out, off(f)), 0, left, v);
         };
 #pragma unroll
         for (int i = 0; i < C; ++i) {
@@ -113,6 +144,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
 #pragma unroll
                 for (int k = 0; k < TOK; ++k) v[k] = kept[i][k];
             } else {
+                forget(xr[i]);
                 unpack_run(xr[i], v);
                 unpack_run(zr[i], zv);
             }
@@ -120,8 +152,8 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
         }
         for (int f = sl + C * SL; f < per; f += SL) {
             float v[TOK], zv[TOK];
-            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, v);
-            load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
+            load_run<T, TOK, FULL>(at(x, off(f)), 0, left, v);
+            load_run<T, TOK, FULL>(at(z, off(f)), 0, left, zv);
             if constexpr (FIRST) {
 #pragma unroll
                 for (int k = 0; k < TOK; ++k) v[k] *= zv[k] * sigmoid_f(zv[k]);
@@ -133,18 +165,86 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
     else body(std::false_type{});
 }
 
+// The forward of single tokens (seqlen 1): a group's features are consecutive in memory, so the lanes take
+// vectors of features.
+template <typename T, typename TO, int THREADS, int KEPT, bool FIRST>
+__global__ __launch_bounds__(THREADS) void gated_fwd_token(GatedArgs a) {
+    constexpr int PV = Storage<T>::kPerVec;
+    __shared__ float red[THREADS / 64];
+    const int per = (int)(a.dim / a.groups);
+    const int64_t bg = blockIdx.x, base = bg * per;
+    const T* x = static_cast<const T*>(a.x) + base;
+    const T* z = static_cast<const T*>(a.z) + base;
+    TO* out = static_cast<TO*>(a.out) + base;
+    const float* w = a.w + (bg % a.groups) * per;
+    RawRun<T, PV> xr[KEPT], zr[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+        const int f = (threadIdx.x + i * THREADS) * PV;
+        xr[i] = load_part<T, PV, false>(x, f, per);
+        zr[i] = load_part<T, PV, false>(z, f, per);
+    }
+    float s = 0.0f;
+    const auto value = [&](const RawRun<T, PV>& xw, const RawRun<T, PV>& zw, int f, float (&v)[PV], float (&gate)[PV]) {
+        unpack_part<T, PV, false>(xw, x, f, per, v);
+        unpack_part<T, PV, false>(zw, z, f, per, gate);
+#pragma unroll
+        for (int k = 0; k < PV; ++k) {
+            gate[k] *= sigmoid_f(gate[k]);
+            if constexpr (FIRST) v[k] *= gate[k];
+        }
+    };
+    const auto sum = [&](const RawRun<T, PV>& xw, const RawRun<T, PV>& zw, int f) {
+        float v[PV], gate[PV];
+        value(xw, zw, f, v, gate);
+#pragma unroll
+        for (int k = 0; k < PV; ++k) s = fmaf(v[k], v[k], s);       // 0 beyond the group
+    };
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) sum(xr[i], zr[i], (threadIdx.x + i * THREADS) * PV);
+    for (int f = (threadIdx.x + KEPT * THREADS) * PV; f < per; f += THREADS * PV)
+        sum(load_part<T, PV, false>(x, f, per), load_part<T, PV, false>(z, f, per), f);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) s += __shfl_xor(s, m);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = red[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) s += red[i];
+    const float r = 1.0f / sqrtf(s / (float)per + a.eps);
+    if (threadIdx.x == 0) a.rstd_out[bg] = r;
+    const auto put = [&](const RawRun<T, PV>& xw, const RawRun<T, PV>& zw, int f) {
+        if (f >= per) return;
+        float v[PV], gate[PV], wv[PV];
+        load_run<float, PV>(w, f, per, wv);
+        value(xw, zw, f, v, gate);
+#pragma unroll
+        for (int k = 0; k < PV; ++k) {
+            v[k] = v[k] * r * wv[k];
+            if constexpr (!FIRST) v[k] *= gate[k];
+        }
+        store_run<TO, PV, false, false>(out, f, per, v);
+    };
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) put(xr[i], zr[i], (threadIdx.x + i * THREADS) * PV);
+    for (int f = (threadIdx.x + KEPT * THREADS) * PV; f < per; f += THREADS * PV)
+        put(load_part<T, PV, false>(x, f, per), load_part<T, PV, false>(z, f, per), f);
+}
+
 // With up the gradient of a rstd (dout weight, or dout weight gate) and m the mean of up a over the group,
 //   da = rstd (up - a rstd^2 m), and from it dx and dz; partial[b, tile, f] = the tile's sum for dweight.
-template <typename T, typename TO, int THREADS, int KEPT, bool FIRST>
-__global__ __launch_bounds__(THREADS) void gated_bwd_kernel(GatedArgs a) {
-    constexpr int TOK = Storage<T>::kPerVec, GROUPS = (int)kRmsTile / TOK, SL = THREADS / GROUPS;
+// A tile is kRmsTile tokens, or fewer that hold the whole row: partial has one row for kRmsTile tokens.
+template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST, bool FAR>
+__global__ __launch_bounds__(THREADS, (THREADS >= 512 ? 4 : THREADS / 128)) void gated_bwd_kernel(GatedArgs a) {
+    constexpr int TOK = Storage<T>::kPerVec, SL = THREADS / GROUPS;
     __shared__ float red[THREADS / 64][GROUPS * TOK];
     const int grp = threadIdx.x % GROUPS, sl = threadIdx.x / GROUPS;
-    const int64_t L = a.seqlen, tiles = (L + kRmsTile - 1) / kRmsTile;
-    const int64_t bg = blockIdx.x / tiles, tile = blockIdx.x - bg * tiles, t0 = tile * kRmsTile;
+    constexpr int kTile = GROUPS * TOK;
+    const int64_t L = a.seqlen, tiles = (L + kTile - 1) / kTile;
+    const int64_t bg = blockIdx.x / tiles, tile = blockIdx.x - bg * tiles, t0 = tile * kTile;
     const int64_t b = bg / a.groups;
     const int per = (int)(a.dim / a.groups), first = (int)(bg - b * a.groups) * per;
-    const bool whole = t0 + kRmsTile <= L || L % TOK == 0;
+    const bool whole = t0 + kTile <= L || L % TOK == 0;
     const bool live = t0 + grp * TOK < L;
     const int64_t l0 = whole && !live ? t0 : t0 + grp * TOK;
     const int64_t base = bg * per * L;
@@ -158,15 +258,17 @@ __global__ __launch_bounds__(THREADS) void gated_bwd_kernel(GatedArgs a) {
     const auto body = [&](auto full_tag) {
         constexpr bool FULL = decltype(full_tag)::value;
         constexpr int C = FULL ? KEPT : 0;
+        const int64_t left = L - l0;                            // tokens from the lane's first
+        const auto off = [&](int f) { return (Offset<FAR>)f * (Offset<FAR>)L + (Offset<FAR>)l0; };
         RawRun<T, TOK> xr[KEPT], zr[KEPT], gr[KEPT];
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             xr[i] = zr[i] = gr[i] = RawRun<T, TOK>{};
             const int f = sl + i * SL;
             if (f < per) {
-                xr[i] = load_raw<T, TOK>(x + (int64_t)f * L, l0);
-                zr[i] = load_raw<T, TOK>(z + (int64_t)f * L, l0);
-                gr[i] = load_raw<T, TOK>(g + (int64_t)f * L, l0);
+                xr[i] = load_raw<T, TOK>(at(x, off(f)), 0);
+                zr[i] = load_raw<T, TOK>(at(z, off(f)), 0);
+                gr[i] = load_raw<T, TOK>(at(g, off(f)), 0);
             }
         }
         float s[TOK] = {};
@@ -182,12 +284,13 @@ __global__ __launch_bounds__(THREADS) void gated_bwd_kernel(GatedArgs a) {
             unpack_run(gr[i], gv);
             const int f = sl + i * SL;
             if (f < per) dot(xv, zv, gv, w[f]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         for (int f = sl + C * SL; f < per; f += SL) {
             float xv[TOK], zv[TOK], gv[TOK];
-            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, xv);
-            load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
-            load_run<T, TOK, FULL>(g + (int64_t)f * L, l0, L, gv);
+            load_run<T, TOK, FULL>(at(x, off(f)), 0, left, xv);
+            load_run<T, TOK, FULL>(at(z, off(f)), 0, left, zv);
+            load_run<T, TOK, FULL>(at(g, off(f)), 0, left, gv);
             dot(xv, zv, gv, w[f]);
         }
         float r[TOK], c[TOK];
@@ -216,13 +319,19 @@ __global__ __launch_bounds__(THREADS) void gated_bwd_kernel(GatedArgs a) {
             }
             if (FULL && !live) pw = 0.0f;
             if (!FULL || live) {
-                store_run<TO, TOK, FULL>(dx + (int64_t)f * L, l0, L, ox);
-                store_run<TO, TOK, FULL>(dz + (int64_t)f * L, l0, L, oz);
+                store_run<TO, TOK, FULL>(at(dx, off(f)), 0, left, ox);
+                store_run<TO, TOK, FULL>(at(dz, off(f)), 0, left, oz);
             }
 #pragma unroll
             for (int m = 1; m < GROUPS; m *= 2) pw += __shfl_xor(pw, m, GROUPS);
             if (grp == 0) part[f] = pw;
         };
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            forget(xr[i]);
+            forget(zr[i]);
+            forget(gr[i]);
+        }
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             float xv[TOK], zv[TOK], gv[TOK];
@@ -231,12 +340,13 @@ __global__ __launch_bounds__(THREADS) void gated_bwd_kernel(GatedArgs a) {
             unpack_run(gr[i], gv);
             const int f = sl + i * SL;
             if (f < per) grad(xv, zv, gv, f);
+            __builtin_amdgcn_sched_barrier(0);          // one feature's values at a time
         }
         for (int f = sl + C * SL; f < per; f += SL) {
             float xv[TOK], zv[TOK], gv[TOK];
-            load_run<T, TOK, FULL>(x + (int64_t)f * L, l0, L, xv);
-            load_run<T, TOK, FULL>(z + (int64_t)f * L, l0, L, zv);
-            load_run<T, TOK, FULL>(g + (int64_t)f * L, l0, L, gv);
+            load_run<T, TOK, FULL>(at(x, off(f)), 0, left, xv);
+            load_run<T, TOK, FULL>(at(z, off(f)), 0, left, zv);
+            load_run<T, TOK, FULL>(at(g, off(f)), 0, left, gv);
             grad(xv, zv, gv, f);
         }
     };
@@ -248,33 +358,53 @@ template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST
 hipError_t fwd_one(const GatedArgs& a, hipStream_t s) {
     constexpr int64_t kTile = GROUPS * Storage<T>::kPerVec;
     const int64_t blocks = a.batch * a.groups * ((a.seqlen + kTile - 1) / kTile);
-    hipLaunchKernelGGL((gated_fwd_kernel<T, TO, GROUPS, THREADS, KEPT, FIRST>), dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
+    if (far(a))
+        hipLaunchKernelGGL((gated_fwd_kernel<T, TO, GROUPS, THREADS, KEPT, FIRST, true>), dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
+    else
+        hipLaunchKernelGGL((gated_fwd_kernel<T, TO, GROUPS, THREADS, KEPT, FIRST, false>), dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
+template <typename T, typename TO, int THREADS, int KEPT, bool FIRST>
+hipError_t token_one(const GatedArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL((gated_fwd_token<T, TO, THREADS, KEPT, FIRST>), dim3((unsigned)(a.batch * a.groups)), dim3(THREADS), 0, s, a);
+    return hipGetLastError();
+}
+
+constexpr int64_t kFewTokens = 8;       // rows no longer take a narrow tile: more slices of the features
+
 template <typename T, typename TO, bool FIRST>
 hipError_t fwd_t(const GatedArgs& a, hipStream_t s) {
+    constexpr int kNarrow = (int)kFewTokens / Storage<T>::kPerVec;
     const int64_t per = a.dim / a.groups;
+    if (a.seqlen == 1) return per <= 512 ? token_one<T, TO, 64, 2, FIRST>(a, s) : token_one<T, TO, 512, 2, FIRST>(a, s);
+    if (a.seqlen <= kFewTokens)
+        return per <= 512 ? fwd_one<T, TO, kNarrow, 256, 2, FIRST>(a, s) : fwd_one<T, TO, kNarrow, 1024, 4, FIRST>(a, s);
     if (per <= 256) return fwd_one<T, TO, 8, 256, 8, FIRST>(a, s);
     if (per <= 512) return fwd_one<T, TO, 8, 512, 8, FIRST>(a, s);
     return fwd_one<T, TO, 8, 1024, 8, FIRST>(a, s);
 }
 
-template <typename T, typename TO, int THREADS, int KEPT, bool FIRST>
+template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST>
 hipError_t bwd_one(const GatedArgs& a, hipStream_t s) {
-    const int64_t tiles = (a.seqlen + kRmsTile - 1) / kRmsTile;
-    hipLaunchKernelGGL((gated_bwd_kernel<T, TO, THREADS, KEPT, FIRST>), dim3((unsigned)(a.batch * a.groups * tiles)),
-                       dim3(THREADS), 0, s, a);
+    constexpr int64_t kTile = GROUPS * Storage<T>::kPerVec;
+    const int64_t tiles = (a.seqlen + kTile - 1) / kTile;
+    const dim3 grid((unsigned)(a.batch * a.groups * tiles));
+    if (far(a)) hipLaunchKernelGGL((gated_bwd_kernel<T, TO, GROUPS, THREADS, KEPT, FIRST, true>), grid, dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((gated_bwd_kernel<T, TO, GROUPS, THREADS, KEPT, FIRST, false>), grid, dim3(THREADS), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
     return launch_partial_rows_sum(a.partial, a.dw, a.batch * tiles, a.dim, s);
 }
 
 template <typename T, typename TO, bool FIRST>
 hipError_t bwd_t(const GatedArgs& a, hipStream_t s) {
+    constexpr int TOK = Storage<T>::kPerVec, kWide = (int)kRmsTile / TOK, kNarrow = (int)kFewTokens / TOK;
     const int64_t per = a.dim / a.groups;
-    if (per <= 128) return bwd_one<T, TO, 256, 4, FIRST>(a, s);
-    if (per <= 256) return bwd_one<T, TO, 512, 4, FIRST>(a, s);
-    return bwd_one<T, TO, 1024, 4, FIRST>(a, s);
+    if (a.seqlen <= kFewTokens)
+        return per <= 512 ? bwd_one<T, TO, kNarrow, 256, 2, FIRST>(a, s) : bwd_one<T, TO, kNarrow, 1024, 4, FIRST>(a, s);
+    if (per <= 128) return bwd_one<T, TO, kWide, 256, 4, FIRST>(a, s);
+    if (per <= 256) return bwd_one<T, TO, kWide, 512, 4, FIRST>(a, s);
+    return bwd_one<T, TO, kWide, 1024, 4, FIRST>(a, s);
 }
 
 template <bool FIRST>

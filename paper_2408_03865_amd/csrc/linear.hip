@@ -26,16 +26,23 @@ __global__ void walk_chain(float* __restrict__ seg, const float* __restrict__ se
     const int64_t i = (blockIdx.x - bh * parts) * blockDim.x + threadIdx.x;
     if (i >= sz) return;
     float cur = entry ? entry[bh * sz + i] : 0.0f;
-    float* p = seg + bh * nseg * sz + i;
-    const float* pa = seg_a + bh * nseg;
-    for (int k = 0; k < nseg; ++k) {
-        const int64_t s = rev ? nseg - 1 - k : k;
-        if (k + 1 < nseg) {             // nothing follows the last
-            const float added = p[s * sz], A = pa[s];
-            p[s * sz] = cur;
-            cur = A < 0.0f ? added : fmaf(A, cur, added);
-        } else {
-            p[s * sz] = cur;
+    const int64_t step = rev ? -sz : sz;
+    float* p = seg + (bh * nseg + (rev ? nseg - 1 : 0)) * sz + i;
+    const float* pa = seg_a + bh * nseg + (rev ? nseg - 1 : 0);
+    // the last segment adds to nothing; eight loads on their way at a time
+    for (int k = 0; k < nseg; k += 8) {
+        float added[8], A[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (k + j + 1 < nseg) {
+                added[j] = p[(k + j) * step];
+                A[j] = pa[rev ? -(k + j) : k + j];
+            }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (k + j >= nseg) break;
+            p[(k + j) * step] = cur;
+            if (k + j + 1 < nseg) cur = A[j] < 0.0f ? added[j] : fmaf(A[j], cur, added[j]);
         }
     }
 }
@@ -154,10 +161,12 @@ __global__ __launch_bounds__(256) void group_sum_kernel(const float* __restrict_
 // Blocks wanted of a walk: two for each CU.
 constexpr int64_t kWalkBlocks = 512;
 constexpr int32_t kBoundChunks = 8;
+// Rows of fewer chunks are walked whole: the two launches more take as long as the chunks.
+constexpr int64_t kSplitChunks = 8;
 
 LinPlan linear_plan(int64_t batch, int64_t heads, int64_t seqlen) {
     const int64_t chunks = (seqlen + kLinChunk - 1) / kLinChunk, blocks = batch * heads;
-    int64_t nseg = blocks >= kWalkBlocks / 2 ? 1 : (kWalkBlocks + blocks - 1) / blocks;
+    int64_t nseg = blocks >= kWalkBlocks / 2 || chunks < kSplitChunks ? 1 : (kWalkBlocks + blocks - 1) / blocks;
     if (nseg > chunks) nseg = chunks;
     int64_t per = (chunks + nseg - 1) / nseg;
     if (nseg > 1 && per > kBoundChunks) per = (per + kBoundChunks - 1) / kBoundChunks * kBoundChunks;

@@ -162,8 +162,8 @@ int packmamba_linear_attention_bwd(const void* q, const void* k, const void* v, 
     const pm::WalkTensor tq{q, (int32_t)dk_size, (int32_t)groups}, tk{k, (int32_t)dk_size, (int32_t)groups};
     const pm::WalkTensor tv{v, (int32_t)dv_size, (int32_t)heads}, tdo{dout, (int32_t)dv_size, (int32_t)heads};
     const bool shared = heads > groups;
-    const auto walk = [&](pm::WalkMode mode, bool exact) {
-        if (p.nseg > 1)
+    const auto walk = [&](pm::WalkMode mode, bool exact, bool segments = true) {
+        if (p.nseg > 1 && segments)
             if (int e = launch_status(pm::launch_walk_segments(a, s))) return e;
         return launch_status(pm::launch_walk(a, mode, exact, s));
     };
@@ -199,7 +199,8 @@ int packmamba_linear_attention_bwd(const void* q, const void* k, const void* v, 
     a.dtype = dtype;
     a.leave = dinitial_state;
     a.s_x = (int32_t)dv_size; a.s_z = 1;
-    if (int e = walk(pm::kWalkPlain, dinitial_state != nullptr)) return e;
+    // the states that enter the segments are those of dk, which lie in memory the same way
+    if (int e = walk(pm::kWalkPlain, dinitial_state != nullptr, false)) return e;
     if (!ddecay) return PACKMAMBA_OK;
 
     pm::LinDecayArgs d{};

@@ -628,7 +628,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
             const int xt = strip * 16 + col;
             const float xhi = c.hi[xt], xlo = c.lo[xt];
             float rs = 0.0f;
-#pragma unroll 1
+#pragma unroll (kYTiles == 2 ? 2 : 1)
             for (int i = 0; i < kYTiles; ++i) {
                 const int yt = ypart * kYTiles + i;
                 f32x4 d = {0, 0, 0, 0};

@@ -31,11 +31,11 @@ def test_sizes():
     lib = _lib()
     fwd, bwd = lib.packmamba_linear_attention_fwd_workspace_size, lib.packmamba_linear_attention_bwd_workspace_size
     assert fwd(8, 64, 8, 128, 64, 4096) == 0                    # rows and heads enough
-    assert fwd(1, 8, 8, 64, 64, 64) == 0                        # one chunk
-    assert fwd(1, 8, 8, 64, 64, 65) >= 8 * 2 * 64 * 64 * 4      # two segments
+    assert fwd(1, 8, 8, 64, 64, 7 * 64) == 0                    # few chunks
+    assert fwd(1, 8, 8, 64, 64, 7 * 64 + 1) >= 8 * 2 * 64 * 64 * 4      # segments
     assert bwd(2, 6, 2, 128, 64, 300) >= 2 * 6 * 300 * 4 * (128 + 2)
     for bad in [(0, 8, 8, 64, 64, 64), (1, 8, 3, 64, 64, 64), (1, 8, 8, 129, 64, 64), (1, 8, 8, 64, 0, 64), (1, 8, 8, 64, 64, -1),
-                (1 << 20, 64, 64, 64, 64, 64), (1, 8, 8, 64, 64, 1 << 40), (64, 64, 64, 128, 128, 1 << 17), (1 << 62, 4, 4, 8, 8, 8)]:
+                (1 << 20, 64, 64, 64, 64, 64), (1, 1, 1, 64, 64, (1 << 22) + 1), (1, 8, 8, 64, 64, 1 << 40), (64, 64, 64, 128, 128, 1 << 17), (1 << 62, 4, 4, 8, 8, 8)]:
         assert fwd(*bad) == 0 and bwd(*bad) == 0, bad
     norm = lib.packmamba_gated_rmsnorm_bwd_workspace_size
     assert norm(2, 48, 130, 3) == 2 * 3 * 48 * 4 // 256 * 256 + (256 if 2 * 3 * 48 * 4 % 256 else 0)
@@ -62,7 +62,7 @@ def test_argument_errors_before_launch():
     for i in (11, 12, 13, 14, 15, 16):
         assert fwd(**{f"_{i}": 0}) == 2 and fwd(**{f"_{i}": -1}) == 2, i
     assert fwd(_13=3) == 2 and fwd(_14=129) == 3 and fwd(_15=129) == 3 and fwd(_18=3) == 3
-    assert fwd(_11=1 << 62) == 2 and fwd(_16=1 << 31) == 2 and fwd(_9=None) == 5 and fwd(_10=100) == 5
+    assert fwd(_11=1 << 62) == 2 and fwd(_16=1 << 31) == 2 and fwd(_16=900, _9=None) == 5 and fwd(_16=900, _10=100) == 5
     # q, k, v, decay, pos, initial, scale, dout, dfinal, dq, dk, dv, ddecay, dinitial, ws, bytes, batch, ...
     good_b = [P, P, P, P, P, None, 1.0, P, None, P, P, P, P, None, P, 1 << 40, 2, 4, 2, 64, 64, 100, 1, 1, None]
 
