@@ -217,6 +217,20 @@ __device__ __forceinline__ bool takes(const ChunkDecay& c, int x, int y) {
     return REV ? x <= y && c.start[y] <= x : y <= x && c.start[x] <= y;
 }
 
+// One step of the segmented sum over lanes: a lane that has no start among those summed so far adds the sum of
+// the lane that CTRL names, and takes its start.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(double& v, int& start) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CTRL, ROWS, 0xf, false);
+    const int ps = __builtin_amdgcn_update_dpp(-1, start, CTRL, ROWS, 0xf, false);
+    if (start < 0) {
+        v += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+        start = ps;
+    }
+}
+
 // One wave, lane = token.  The sum is kept in 64 bits and starts anew at each start, so that no
 // sequence's decays reach another's.
 template <bool REV>
@@ -225,15 +239,12 @@ __device__ __forceinline__ void chunk_decay(const TokenDecay& d, ChunkDecay& c, 
     bool cut = d.pos == 0 || d.g <= kDecayCut;
     double v = cut ? 0.0 : (double)d.g * 1.4426950408889634;
     int start = cut ? l : -1;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const double pv = __shfl_up(v, m);
-        const int ps = __shfl_up(start, m);
-        if (l >= m && start < 0) {      // no start in the lanes summed so far
-            v += pv;
-            start = ps;
-        }
-    }
+    scan_step<row_shr(1), 0xf>(v, start);
+    scan_step<row_shr(2), 0xf>(v, start);
+    scan_step<row_shr(4), 0xf>(v, start);
+    scan_step<row_shr(8), 0xf>(v, start);
+    scan_step<0x142, 0xa>(v, start);     // lane 15 of rows 0 and 2 to the rows after them
+    scan_step<0x143, 0xc>(v, start);     // lane 31 to rows 2 and 3
     const float hi = (float)v, lo = (float)(v - (double)hi);
     const float ehi = __shfl(hi, 63), elo = __shfl(lo, 63);
     const int estart = __shfl(start, 63);
@@ -262,18 +273,27 @@ struct TileRegs {
 
     // Every lane loads whole vectors from inside its row, a row that the tensor has, whatever it needs: a branch
     // here would make the kernel wait for the loads at once.  settle() puts right what the last chunk of a row
-    // and heads of fewer features need, when the values are used.  One 32-bit offset a lane for all its rows.
-    __device__ void load(int tid, const T* p, int rows, int64_t t0, int64_t L) {
-        const int row0 = tid / kLanes, tok = (tid % kLanes) * kPer;
-        const int64_t from = min(t0, L - kPer);             // of the row's vectors the last starts at L - kPer
-        const T* base = L < kPer ? reinterpret_cast<const T*>(&walk_zero) : p + from;
-        const uint32_t t = L < kPer ? 0 : (uint32_t)(min(t0 + tok, L - kPer) - from) * sizeof(T);
-        const uint32_t at = L < kPer ? 0 : (uint32_t)row0 * (uint32_t)L * sizeof(T) + t;
+    // and heads of fewer features need, when the values are used.  at: offset_of(), the same for all tensors.
+    __device__ static uint32_t offset_of(int tid, int t0, int L) {
+        const int tok = (tid % kLanes) * kPer;
+        return L < kPer ? 0u : ((uint32_t)(tid / kLanes) * (uint32_t)L + (uint32_t)min(t0 + tok, L - kPer)) * (uint32_t)sizeof(T);
+    }
+    __device__ void load(int tid, uint32_t at, const T* p, int rows, int L) {
+        // said to be global memory, which the compiler cannot see of a choice of two pointers: what it then
+        // loads makes every wait for LDS wait for memory too
+        typedef const __attribute__((address_space(1))) char* Bytes;
+        typedef const __attribute__((address_space(1))) typename Storage<T>::Vec* Global;
+        const int row0 = tid / kLanes;
+        Bytes base = (Bytes)(uintptr_t)(L < kPer ? reinterpret_cast<const T*>(&walk_zero) : p);
+        const int64_t apart = L < kPer ? 0 : (int64_t)kRowsPass * L * (int64_t)sizeof(T);
+        if (rows == ROWS) {
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const T* row = i * kRowsPass < rows && L >= kPer ? base + i * kRowsPass * L : base;
-            const uint32_t off = row0 + i * kRowsPass < rows ? at : t;
-            w[i] = load_vec<T, kPer>(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + off));
+            for (int i = 0; i < kPasses; ++i) w[i] = *(Global)(base + i * apart + at);
+        } else {
+            const uint32_t first = L < kPer ? 0u : at - (uint32_t)row0 * (uint32_t)L * (uint32_t)sizeof(T);    // in the pass's first row
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i)
+                w[i] = *(Global)(base + (i * kRowsPass < rows ? i * apart : 0) + (row0 + i * kRowsPass < rows ? at : first));
         }
     }
     __device__ void settle(int tid, const T* p, int rows, int64_t t0, int64_t L) {
@@ -541,11 +561,11 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
     const int coef_wave = REV ? 3 : kYParts > 1 ? 4 : 0;    // a wave with the fewest products of x and y
     const auto load = [&](int chunk) {
         const int tid = fresh<kTight>(threadIdx.x);
-        const int64_t t0 = (int64_t)chunk * kC;
-        xr.load(tid, xp, a.x.rows, t0, L);
-        yr.load(tid, yp, a.y.rows, t0, L);
-        zr.load(tid, zp, a.z.rows, t0, L);
-        if constexpr (MODE != kWalkPlain) er.load(tid, ep, a.e.rows, t0, L);
+        const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
+        xr.load(tid, at, xp, a.x.rows, (int)L);
+        yr.load(tid, at, yp, a.y.rows, (int)L);
+        zr.load(tid, at, zp, a.z.rows, (int)L);
+        if constexpr (MODE != kWalkPlain) er.load(tid, at, ep, a.e.rows, (int)L);
     };
     const auto load_td = [&](int chunk) {
         if (w == coef_wave) td = load_decay(a, b, h, (int64_t)chunk * kC + l);
@@ -822,8 +842,12 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>())) void walk_aggregate(Wa
         if (n > 1) td = load_decay(a, b, h, (int64_t)(begin + step) * kC + l);
     }
     const int tid = threadIdx.x;
-    yr.load(tid, yp, a.y.rows, (int64_t)begin * kC, L);
-    zr.load(tid, zp, a.z.rows, (int64_t)begin * kC, L);
+    const auto load = [&](int chunk) {
+        const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
+        yr.load(tid, at, yp, a.y.rows, (int)L);
+        zr.load(tid, at, zp, a.z.rows, (int)L);
+    };
+    load(begin);
     for (int it = 0; it < n; ++it) {
         const int chunk = begin + it * step;
         ChunkDecay& c = sm.c[it & 1];
@@ -835,8 +859,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>())) void walk_aggregate(Wa
         if (zr.zero_sum(yr.zero_sum(0.0f)) != 0.0f) c.bad[0] = 1;
         __syncthreads();
         if (it + 1 < n) {
-            yr.load(tid, yp, a.y.rows, (int64_t)(chunk + step) * kC, L);
-            zr.load(tid, zp, a.z.rows, (int64_t)(chunk + step) * kC, L);
+            load(chunk + step);
             if (w == 0) {
                 ChunkDecay& cn = sm.c[(it + 1) & 1];
                 chunk_decay<REV>(td, cn, a.iscale, a.uscale);
