@@ -457,16 +457,13 @@ __device__ __forceinline__ void store_sum16(int l, float* four, const f32x2& s) 
     }
 }
 
-// bf16: the x features are split over two waves, so that twice the waves share a chunk's latencies; the
-// state that x is multiplied with then passes through LDS, rounded, or where it is split into terms in 32 bits.
+// bf16: the x features are split over two waves, so that twice the waves share a chunk's latencies; each
+// multiplies x with its half of the state for all tokens, and the sums meet in LDS.
 template <typename T, int KC, int VP>
 constexpr int walk_parts() {
     return sizeof(T) == 2 && KC >= VP ? 2 : 1;
 }
-template <typename T, int NO>
-using WalkCopy = std::conditional_t<NO == 1, typename Mat<T>::Frag, f32x4>;
-
-template <typename T, int KC, int VP, int MODE, int NO>
+template <typename T, int KC, int VP, int MODE>
 struct WalkSmem {
     static constexpr int kParts = walk_parts<T, KC, VP>(), kWaves = VP / 16 * kParts;
     __attribute__((aligned(16))) T x[KC * kC];
@@ -474,7 +471,7 @@ struct WalkSmem {
     __attribute__((aligned(16))) T z[VP * kC];
     __attribute__((aligned(16))) T e[MODE != kWalkPlain ? VP * kC : 8];
     __attribute__((aligned(16))) T p[kC * kC];          // x's rows
-    __attribute__((aligned(16))) WalkCopy<T, NO> s[kParts == 2 ? KC * VP / 4 : 1];     // the operands of the lanes
+    __attribute__((aligned(16))) f32x4 half[kParts == 2 ? kWaves * 2 * 64 : 1];        // sums for the other part's tokens
     ChunkDecay c[2];
     __attribute__((aligned(16))) float rsum[MODE == kWalkDq ? kWaves / 4 : 1][kC];
     __attribute__((aligned(16))) float csum[MODE == kWalkDq ? 4 : 1][kC];
@@ -503,7 +500,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
     constexpr int kWaves = VT * kParts, kThreads = kWaves * 64, kYParts = kWaves / 4, kYTiles = 4 / kYParts;
     constexpr bool kAhead = sizeof(T) == 2;             // the next chunk's tiles are loaded during a chunk
     constexpr bool kTight = MODE != kWalkPlain || VP > KC;
-    __shared__ WalkSmem<T, KC, VP, MODE, NO> sm;
+    __shared__ WalkSmem<T, KC, VP, MODE> sm;
     const int l = lane_id(), w = wave_id();
     const int64_t L = a.seqlen;
     const uint32_t id = walk_block((uint32_t)a.batch * a.heads * a.nseg);       // at most 2^23 of them
@@ -611,14 +608,6 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
         yr.store(tid, sm.y);
         zr.store(tid, sm.z);
         if constexpr (MODE != kWalkPlain) er.store(tid, sm.e);
-        if constexpr (kParts == 2) {
-#pragma unroll
-            for (int k = 0; k < KF; ++k) {
-                auto& copy = sm.s[((part * KF + k) * VT + ztile) * 64 + l];
-                if constexpr (NO == 1) copy = M::round(S.s[k]);
-                else copy = S.s[k];
-            }
-        }
         if (zr.zero_sum(yr.zero_sum(0.0f)) != 0.0f) c.bad[0] = 1;
         if constexpr (MODE == kWalkDq) {
             if (chunk > 0 && chunk % a.bound_chunks == 0) bound_store(chunk / a.bound_chunks);
@@ -701,40 +690,47 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
                 if (l < 16) sm.rsum[ypart][xt] = rs;
             }
         }
-        __syncthreads();
 
-        // out, from the state that enters the chunk and from the chunk's own products
+        // x and the wave's part of the state that enters the chunk, for all tokens
         const bool bad = __builtin_amdgcn_readfirstlane(c.bad[0]) != 0;
+        // the tokens whose out the wave finishes: all tiles of 16, or the first and the last, or the two between
+        const auto own_tile = [&](int i) { return kParts == 1 ? i : part ? 1 + i : 3 * i; };
+        f32x4 os[XT];
         {
-            const int l = fresh<kTight>(lane_id()), col = l & 15, four = (l >> 4) * 4;
-            // the wave's token tiles: all, or the first and the last, or the two between
-            const auto token_tile = [&](int i) { return kParts == 1 ? i : part ? 1 + i : 3 * i; };
-            f32x4 os[XT];
+            const int l = fresh<kTight>(lane_id());
+            f32x4 all[4];
 #pragma unroll
-            for (int i = 0; i < XT; ++i) os[i] = f32x4{0, 0, 0, 0};
-#pragma unroll (kParts == 1 || NO == 1 ? KT / 2 : 1)
-            for (int k = 0; k < KT; k += 2) {
+            for (int xt = 0; xt < 4; ++xt) all[xt] = f32x4{0, 0, 0, 0};
+            const T* xs = sm.x + S.xf * kC;
+#pragma unroll
+            for (int k = 0; k < KF; k += 2) {
                 Frag s0[NO], s1[NO];
-                if constexpr (kParts == 1) {
-                    M::template split<NO>(S.s[k], s0);
-                    M::template split<NO>(S.s[k + 1], s1);
-                } else {
-                    const auto &c0 = sm.s[(k * VT + ztile) * 64 + l], &c1 = sm.s[((k + 1) * VT + ztile) * 64 + l];
-                    if constexpr (NO == 1) {
-                        s0[0] = c0;
-                        s1[0] = c1;
-                    } else {
-                        M::template split<NO>(c0, s0);
-                        M::template split<NO>(c1, s1);
-                    }
-                }
+                M::template split<NO>(S.s[k], s0);
+                M::template split<NO>(S.s[k + 1], s1);
 #pragma unroll
-                for (int i = 0; i < XT; ++i) {
-                    const Frag f0 = M::transposed(l, sm.x + k * 16 * kC, token_tile(i)), f1 = M::transposed(l, sm.x + (k + 1) * 16 * kC, token_tile(i));
+                for (int xt = 0; xt < 4; ++xt) {
+                    const Frag f0 = M::transposed(l, xs + k * 16 * kC, xt), f1 = M::transposed(l, xs + (k + 1) * 16 * kC, xt);
 #pragma unroll
-                    for (int q = 0; q < NO; ++q) os[i] = M::mma(f0, f1, s0[q], s1[q], os[i]);
+                    for (int q = 0; q < NO; ++q) all[xt] = M::mma(f0, f1, s0[q], s1[q], all[xt]);
                 }
             }
+            if constexpr (kParts == 1) {
+#pragma unroll
+                for (int i = 0; i < XT; ++i) os[i] = all[i];
+            } else {
+                f32x4* half = sm.half + ((part ^ 1) * VT + ztile) * 2 * 64 + l;      // where the other part reads
+                half[0] = part ? all[0] : all[1];
+                half[64] = part ? all[3] : all[2];
+                os[0] = part ? all[1] : all[0];
+                os[1] = part ? all[2] : all[3];
+            }
+        }
+        update<T, REV, NS, kTight>(S, sm.y, sm.z, c, cut, bad);
+        __syncthreads();
+
+        // out, from those sums and the chunk's own products
+        {
+            const int l = fresh<kTight>(lane_id()), col = l & 15, four = (l >> 4) * 4;
             Frag zf[4];
             const T* zt = sm.z + ztile * 16 * kC;
 #pragma unroll
@@ -742,8 +738,9 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
             const int64_t t0 = (int64_t)chunk * kC;
 #pragma unroll
             for (int i = 0; i < XT; ++i) {
-                const int xt = token_tile(i), x0 = xt * 16 + four;
+                const int xt = own_tile(i), x0 = xt * 16 + four;
                 f32x4 o = os[i];
+                if constexpr (kParts == 2) o += sm.half[(w * 2 + i) * 64 + l];
                 const f32x4 in = *reinterpret_cast<const f32x4*>(&c.in[x0]);
                 o *= in;
                 if (cut) {
@@ -787,7 +784,6 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
                 }
             }
         }
-        update<T, REV, NS, kTight>(S, sm.y, sm.z, c, cut, bad);
     }
     if constexpr (MODE != kWalkPlain) {
         __syncthreads();
