@@ -20,7 +20,7 @@
  *             A value of -104 or less (exp of it is 0 in 32 bits; -infinity too) cuts as a start
  *             does.  Values above 0 make the state grow and are taken as they are.
  *   states    (batch, heads, dk, dv) float
- * dk, dv in [1, 128]; heads a multiple of groups; seqlen at most 2^22, batch * heads at most 2^23, and
+ * dk, dv in [1, 128]; heads a multiple of groups; seqlen at most 2^22, batch * heads at most 2^21, and
  * batch * heads * max(dk, dv) * seqlen at most 2^33.
  * Arithmetic: products accumulate in 32 bits and the state is held in 32 bits.  With bf16 inputs the
  * products inside a chunk of 64 tokens (q . k, weighted) and the copy of the state that q is
@@ -95,7 +95,8 @@ int packmamba_linear_attention_step(const void* q, const void* k, const void* v,
  *   gate_first:  a = x gate,  out = a rstd weight          rstd = 1 / sqrt(mean over the group of a^2 + eps)
  *   otherwise:   a = x,       out = a rstd weight gate
  *   x, z, out in dtype; weight (dim) float; rstd (batch, groups, seqlen) float, written for the backward.
- *   dim a multiple of groups; eps >= 0; batch * groups at most 2^20.
+ *   dim a multiple of groups; eps >= 0; batch * groups at most 2^20, batch * groups * ceil(seqlen / 32) below 2^22
+ *   and batch * dim * seqlen at most 2^33.
  */
 int packmamba_gated_rmsnorm_fwd(const void* x, const void* z, const float* weight, float eps, void* out, float* rstd,
                                 int64_t batch, int64_t dim, int64_t seqlen, int64_t groups, int32_t gate_first,

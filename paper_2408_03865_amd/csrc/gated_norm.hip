@@ -426,8 +426,6 @@ hipError_t bwd_d(const GatedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t gated_bwd_partial_rows(int64_t batch, int64_t seqlen) { return batch * ((seqlen + kRmsTile - 1) / kRmsTile); }
-
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s) { return a.gate_first ? fwd_d<true>(a, s) : fwd_d<false>(a, s); }
 hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) { return a.gate_first ? bwd_d<true>(a, s) : bwd_d<false>(a, s); }
 

@@ -158,30 +158,6 @@ __global__ __launch_bounds__(256) void group_sum_kernel(const float* __restrict_
 
 }  // namespace
 
-// Blocks wanted of a walk: two for each CU.
-constexpr int64_t kWalkBlocks = 512;
-constexpr int32_t kBoundChunks = 8;
-// Rows of fewer chunks are walked whole: the two launches more take as long as the chunks.
-constexpr int64_t kSplitChunks = 8;
-
-LinPlan linear_plan(int64_t batch, int64_t heads, int64_t seqlen) {
-    const int64_t chunks = (seqlen + kLinChunk - 1) / kLinChunk, blocks = batch * heads;
-    int64_t nseg = blocks >= kWalkBlocks / 2 || chunks < kSplitChunks ? 1 : (kWalkBlocks + blocks - 1) / blocks;
-    if (nseg > chunks) nseg = chunks;
-    int64_t per = (chunks + nseg - 1) / nseg;
-    if (nseg > 1 && per > kBoundChunks) per = (per + kBoundChunks - 1) / kBoundChunks * kBoundChunks;
-    LinPlan p;
-    p.seg_chunks = (int32_t)per;
-    p.nseg = (int32_t)((chunks + per - 1) / per);
-    p.bound_chunks = p.nseg > 1 && per < kBoundChunks ? (int32_t)per : kBoundChunks;
-    p.nb = (int32_t)((chunks + p.bound_chunks - 1) / p.bound_chunks);
-    return p;
-}
-
-int64_t walk_bound_floats(int32_t x_rows, int32_t z_rows) {
-    return (int64_t)(x_rows <= 64 ? 64 : 128) * (z_rows <= 64 ? 64 : 128);
-}
-
 hipError_t launch_walk(const WalkArgs& a, WalkMode mode, bool exact, hipStream_t s) {
     switch (a.dtype) {
         case 1: return walk_t<bf16_t, bf16_t>(a, mode, exact, s);

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "launch.hpp"
+
 namespace pm {
 
 constexpr int64_t kLinChunk = 64;       // tokens of a chunk
@@ -50,15 +52,40 @@ enum WalkMode : int { kWalkPlain = 0, kWalkDq = 1, kWalkDk = 2 };
 // operands are split so that the state keeps 32-bit accuracy (else 16 bits of the weighted values).
 hipError_t launch_walk(const WalkArgs& a, WalkMode mode, bool exact, hipStream_t s);
 hipError_t launch_walk_segments(const WalkArgs& a, hipStream_t s);
-// threads' floats of one stored state
-int64_t walk_bound_floats(int32_t x_rows, int32_t z_rows);
+// floats of one stored state, in the threads' order
+inline int64_t walk_bound_floats(int32_t x_rows, int32_t z_rows) {
+    return (int64_t)(x_rows <= 64 ? 64 : 128) * (z_rows <= 64 ? 64 : 128);
+}
 
-// Split of the rows into segments of whole chunks, each walked by its own block.
+// Split of the rows into segments of whole chunks, each walked by its own block, with the states that enter them
+// from two launches more (aggregate and chain): where rows and heads give the CUs less than a block each, and
+// rows are long enough.  Two blocks a CU are aimed at.  Us of a walk of 4096 tokens, dk 128 and dv 64, bf16:
+// 512 (row, head) pairs 330, 128 pairs unsplit 217, so that a chunk takes 8100 cycles alone and 12300 with another
+// block on its CU; 128 pairs in four segments 105 with the two launches.  256 pairs gain nothing by it.
+constexpr int64_t kWalkBlocks = 512;
+// Rows of fewer chunks are walked whole: the launches take as long as the chunks (256 tokens, 2 heads, fp32, the
+// whole backward: 65 us split, 126 unsplit).
+constexpr int64_t kSplitChunks = 4;
+// Chunks between the boundaries at which the backward takes the product of the two states.
+constexpr int32_t kBoundChunks = 8;
+
 struct LinPlan {
     int32_t nseg, seg_chunks;
     int32_t bound_chunks, nb;
 };
-LinPlan linear_plan(int64_t batch, int64_t heads, int64_t seqlen);
+inline LinPlan linear_plan(int64_t batch, int64_t heads, int64_t seqlen) {
+    const int64_t chunks = (seqlen + kLinChunk - 1) / kLinChunk, blocks = batch * heads;
+    int64_t nseg = blocks >= kWalkBlocks / 2 || chunks < kSplitChunks ? 1 : (kWalkBlocks + blocks - 1) / blocks;
+    if (nseg > chunks) nseg = chunks;
+    int64_t per = (chunks + nseg - 1) / nseg;
+    if (nseg > 1 && per > kBoundChunks) per = (per + kBoundChunks - 1) / kBoundChunks * kBoundChunks;
+    LinPlan p;
+    p.seg_chunks = (int32_t)per;
+    p.nseg = (int32_t)((chunks + per - 1) / per);
+    p.bound_chunks = p.nseg > 1 && per < kBoundChunks ? (int32_t)per : kBoundChunks;
+    p.nb = (int32_t)((chunks + p.bound_chunks - 1) / p.bound_chunks);
+    return p;
+}
 
 struct LinDecayArgs {
     const float* rq;        // (batch, heads, seqlen)
@@ -105,7 +132,10 @@ struct GatedArgs {
     int64_t batch, dim, seqlen;
     int32_t groups, gate_first, dtype;
 };
-int64_t gated_bwd_partial_rows(int64_t batch, int64_t seqlen);
+// rows of dweight's partial sums: one for each kRmsTile tokens of a batch row
+inline int64_t gated_bwd_partial_rows(int64_t batch, int64_t seqlen) {
+    return batch * ((seqlen + kRmsTile - 1) / kRmsTile);
+}
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s);
 hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s);
 

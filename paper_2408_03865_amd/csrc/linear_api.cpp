@@ -10,7 +10,8 @@
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int64_t kMaxRows = (int64_t)1 << 23;      // (batch, head) pairs: one block each
+constexpr int64_t kMaxRows = (int64_t)1 << 21;      // (batch, head) pairs: a block of up to 1024 threads each, 2^32 in all
+constexpr int64_t kMaxNormTiles = ((int64_t)1 << 22) - 1;   // tiles of 32 tokens, a block each
 constexpr int64_t kMaxSeqlen = (int64_t)1 << 22;    // 64 rows of it in fp32 are an offset of 32 bits in the walks
 constexpr int64_t kMaxElems = (int64_t)1 << 33;     // of a tensor, heads' copies of q and k included
 
@@ -70,6 +71,7 @@ int check_norm(int64_t batch, int64_t dim, int64_t seqlen, int64_t groups) {
     if (groups > (1 << 20) || batch > (1 << 20) / groups) return PACKMAMBA_ERR_SHAPE;
     if (dim > INT32_MAX || seqlen > INT32_MAX / 2) return PACKMAMBA_ERR_SHAPE;
     if (batch * dim > kMaxElems / seqlen) return PACKMAMBA_ERR_SHAPE;
+    if (batch * groups > kMaxNormTiles / ((seqlen + 31) / 32)) return PACKMAMBA_ERR_SHAPE;
     return PACKMAMBA_OK;
 }
 

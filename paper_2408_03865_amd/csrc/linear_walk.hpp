@@ -405,10 +405,10 @@ __device__ __forceinline__ float uniform(float v) {
 }
 
 // S <- A S + sum_j up_j y_j z_j^T
-template <typename T, bool REV, int NS, bool HIDE, int KF>
+template <typename T, bool REV, int NS, int KF>
 __device__ __forceinline__ void update(State<KF>& S, const T* ys, const T* zs, const ChunkDecay& c, bool cut, bool bad) {
     using M = Mat<T>;
-    const int l = fresh<HIDE>(lane_id()), four = (l >> 4) * 4;
+    const int l = here(lane_id()), four = (l >> 4) * 4;
     ys += S.xf * kC;
     zs += S.zf * kC;
     S.decay(cut, uniform(c.a));
@@ -498,7 +498,6 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
     using Frag = typename M::Frag;
     constexpr int KT = KC / 16, VT = VP / 16, kParts = walk_parts<T, KC, VP>(), KF = KT / kParts, XT = 4 / kParts;
     constexpr int kWaves = VT * kParts, kThreads = kWaves * 64, kYParts = kWaves / 4, kYTiles = 4 / kYParts;
-    constexpr bool kAhead = sizeof(T) == 2;             // the next chunk's tiles are loaded during a chunk
     constexpr bool kTight = MODE != kWalkPlain || VP > KC;
     __shared__ WalkSmem<T, KC, VP, MODE> sm;
     const int l = lane_id(), w = wave_id();
@@ -590,7 +589,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
     const int begin = REV ? last : first, n = last - first + 1;
     if (threadIdx.x == 0) sm.c[0].bad[0] = sm.c[1].bad[0] = 0;
     load_td(begin);
-    if (kAhead) load(begin);
+    load(begin);
     if (w == coef_wave) chunk_decay<REV>(td, sm.c[0], a.iscale, a.uscale);
     if (n > 1) load_td(begin + step);
     for (int it = 0; it < n; ++it) {
@@ -598,7 +597,6 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
         ChunkDecay& c = sm.c[it & 1];
         __syncthreads();                                // the tiles of the chunk before are read
         if (it > 0) flush_r(chunk - step);
-        if (!kAhead) load(chunk);
         const int64_t ct = (int64_t)chunk * kC;
         xr.settle(tid, xp, a.x.rows, ct, L);
         yr.settle(tid, yp, a.y.rows, ct, L);
@@ -618,7 +616,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
                 bound_dot((next + a.bound_chunks - 1) / a.bound_chunks);
         }
         __syncthreads();
-        if (kAhead && it + 1 < n) load(chunk + step);
+        if (it + 1 < n) load(chunk + step);     // the next chunk's tiles, during this one
 
         const bool cut = __builtin_amdgcn_readfirstlane(__float_as_int(c.a)) < 0;      // a sequence starts in the chunk
         // products of x and y, weighted: 16 x's by all y's, or a part of them
@@ -637,7 +635,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
             const int xt = strip * 16 + col;
             const float xhi = c.hi[xt], xlo = c.lo[xt];
             float rs = 0.0f;
-#pragma unroll (kYTiles == 2 ? 2 : 1)
+#pragma unroll 1
             for (int i = 0; i < kYTiles; ++i) {
                 const int yt = ypart * kYTiles + i;
                 f32x4 d = {0, 0, 0, 0};
@@ -725,7 +723,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP,
                 os[1] = part ? all[2] : all[3];
             }
         }
-        update<T, REV, NS, kTight>(S, sm.y, sm.z, c, cut, bad);
+        update<T, REV, NS>(S, sm.y, sm.z, c, cut, bad);
         __syncthreads();
 
         // out, from those sums and the chunk's own products
@@ -864,7 +862,7 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>())) void walk_aggregate(Wa
             }
         }
         const bool cut = __builtin_amdgcn_readfirstlane(__float_as_int(c.a)) < 0;
-        update<T, REV, NS, false>(S, sm.y, sm.z, c, cut, __builtin_amdgcn_readfirstlane(c.bad[0]) != 0);
+        update<T, REV, NS>(S, sm.y, sm.z, c, cut, __builtin_amdgcn_readfirstlane(c.bad[0]) != 0);
         all = cut || all < 0.0f ? -1.0f : all * c.a;
     }
     const int64_t sz = (int64_t)a.x.rows * a.z.rows;

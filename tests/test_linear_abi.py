@@ -31,15 +31,15 @@ def test_sizes():
     lib = _lib()
     fwd, bwd = lib.packmamba_linear_attention_fwd_workspace_size, lib.packmamba_linear_attention_bwd_workspace_size
     assert fwd(8, 64, 8, 128, 64, 4096) == 0                    # rows and heads enough
-    assert fwd(1, 8, 8, 64, 64, 7 * 64) == 0                    # few chunks
-    assert fwd(1, 8, 8, 64, 64, 7 * 64 + 1) >= 8 * 2 * 64 * 64 * 4      # segments
+    assert fwd(1, 8, 8, 64, 64, 3 * 64) == 0                    # few chunks
+    assert fwd(1, 8, 8, 64, 64, 4 * 64) >= 8 * 2 * 64 * 64 * 4      # segments
     assert bwd(2, 6, 2, 128, 64, 300) >= 2 * 6 * 300 * 4 * (128 + 2)
     for bad in [(0, 8, 8, 64, 64, 64), (1, 8, 3, 64, 64, 64), (1, 8, 8, 129, 64, 64), (1, 8, 8, 64, 0, 64), (1, 8, 8, 64, 64, -1),
-                (1 << 20, 64, 64, 64, 64, 64), (1, 1, 1, 64, 64, (1 << 22) + 1), (1, 8, 8, 64, 64, 1 << 40), (64, 64, 64, 128, 128, 1 << 17), (1 << 62, 4, 4, 8, 8, 8)]:
+                (1 << 21, 2, 2, 64, 64, 64), (1, 1, 1, 64, 64, (1 << 22) + 1), (1, 8, 8, 64, 64, 1 << 40), (64, 64, 64, 128, 128, 1 << 17), (1 << 62, 4, 4, 8, 8, 8)]:
         assert fwd(*bad) == 0 and bwd(*bad) == 0, bad
     norm = lib.packmamba_gated_rmsnorm_bwd_workspace_size
     assert norm(2, 48, 130, 3) == 2 * 3 * 48 * 4 // 256 * 256 + (256 if 2 * 3 * 48 * 4 % 256 else 0)
-    assert norm(2, 48, 130, 5) == 0 and norm(0, 48, 130, 3) == 0 and norm(1 << 20, 48, 1, 3) == 0
+    assert norm(2, 48, 130, 5) == 0 and norm(0, 48, 130, 3) == 0 and norm(1 << 20, 48, 1, 3) == 0 and norm(1 << 10, 8, 1 << 14, 8) == 0
 
 
 @pytest.mark.skipif(_gpu_visible(), reason="fake pointers are only passed where no GPU exists")
