@@ -58,14 +58,17 @@ inline int64_t walk_bound_floats(int32_t x_rows, int32_t z_rows) {
 }
 
 // Split of the rows into segments of whole chunks, each walked by its own block, with the states that enter them
-// from two launches more (aggregate and chain): where rows and heads give the CUs less than a block each, and
-// rows are long enough.  Two blocks a CU are aimed at.  Us of a walk of 4096 tokens, dk 128 and dv 64, bf16:
-// 512 (row, head) pairs 330, 128 pairs unsplit 217, so that a chunk takes 8100 cycles alone and 12300 with another
-// block on its CU; 128 pairs in four segments 105 with the two launches.  256 pairs gain nothing by it.
-constexpr int64_t kWalkBlocks = 512;
-// Rows of fewer chunks are walked whole: the launches take as long as the chunks (256 tokens, 2 heads, fp32, the
-// whole backward: 65 us split, 126 unsplit).
-constexpr int64_t kSplitChunks = 4;
+// from two launches more (aggregate and chain).  The plan is the cheapest in units of a chunk walked alone on a CU:
+//   - a CU holds two blocks (one where dk and dv are both above 64), and a chunk in company takes 1.5 (8100 and
+//     12300 cycles, dk 128, dv 64, bf16); blocks beyond a round follow as others end, with half a block's wait;
+//   - an aggregate takes 0.45 of a walk; the backward has two for its three walks;
+//   - a block costs three chunks besides its own, the two launches two (forward calls of 4 and 5 chunks: bf16 25 us
+//     for 16 and 18 unsplit, fp32 25 for 32 and 38).
+// Us of a bf16 call, dk and dv 64, planned and unsplit (batch x heads x tokens, forward then the whole backward):
+//   4 x 24 x 2048 56, 83; 188, 376   2 x 64 x 4096 (dk 128) 132, 206; 576, 1000   1 x 300 x 4096 222, 220; 1046, 1225
+//   1 x 32 x 16384 103, 623; 398, 2670   1 x 8 x 320 24, 18; 58, 79   1 x 150 x 2048 (dk 128) 105, 108; 471, 565
+// and 1 x 100 x 4096 with dk and dv 128 227, 259; 892, 1213.
+constexpr int64_t kSplitChunks = 4;     // rows of fewer are walked whole
 // Chunks between the boundaries at which the backward takes the product of the two states.
 constexpr int32_t kBoundChunks = 8;
 
@@ -73,16 +76,31 @@ struct LinPlan {
     int32_t nseg, seg_chunks;
     int32_t bound_chunks, nb;
 };
-inline LinPlan linear_plan(int64_t batch, int64_t heads, int64_t seqlen) {
+inline LinPlan linear_plan(int64_t batch, int64_t heads, int64_t dk, int64_t dv, int64_t seqlen, bool backward) {
     const int64_t chunks = (seqlen + kLinChunk - 1) / kLinChunk, blocks = batch * heads;
-    int64_t nseg = blocks >= kWalkBlocks / 2 || chunks < kSplitChunks ? 1 : (kWalkBlocks + blocks - 1) / blocks;
-    if (nseg > chunks) nseg = chunks;
-    int64_t per = (chunks + nseg - 1) / nseg;
-    if (nseg > 1 && per > kBoundChunks) per = (per + kBoundChunks - 1) / kBoundChunks * kBoundChunks;
+    const int64_t cus = 256, slots = dk > 64 && dv > 64 ? cus : 2 * cus;
+    const double company = slots > cus ? 1.5 : 1.0, walk = backward ? 1.3 : 1.45;
+    const auto load = [&](int64_t n) { return n <= cus ? 1.0 : n <= slots ? company : company * (double)n / (double)slots + 0.5; };
+    int64_t best = chunks;
+    if (blocks < slots && chunks >= kSplitChunks) {
+        double least = load(blocks) * (double)chunks + 3.0;
+        for (int64_t per = 1; per < chunks; ++per) {
+            if (per > kBoundChunks) per = (per + kBoundChunks - 1) / kBoundChunks * kBoundChunks;
+            if (per >= chunks) break;
+            const int64_t n = blocks * ((chunks + per - 1) / per);
+            if (n > 4 * slots) continue;
+            const double rounds = n <= slots ? 1.0 : (double)n / (double)slots;
+            const double cost = walk * load(n) * (double)per + 3.0 * rounds + 2.0;
+            if (cost < least) {
+                least = cost;
+                best = per;
+            }
+        }
+    }
     LinPlan p;
-    p.seg_chunks = (int32_t)per;
-    p.nseg = (int32_t)((chunks + per - 1) / per);
-    p.bound_chunks = p.nseg > 1 && per < kBoundChunks ? (int32_t)per : kBoundChunks;
+    p.seg_chunks = (int32_t)best;
+    p.nseg = (int32_t)((chunks + best - 1) / best);
+    p.bound_chunks = p.nseg > 1 && best < kBoundChunks ? (int32_t)best : kBoundChunks;
     p.nb = (int32_t)((chunks + p.bound_chunks - 1) / p.bound_chunks);
     return p;
 }

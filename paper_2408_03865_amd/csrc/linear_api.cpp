@@ -82,7 +82,7 @@ extern "C" {
 size_t packmamba_linear_attention_fwd_workspace_size(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
                                                      int64_t seqlen) {
     if (check_heads(batch, heads, groups, dk, dv, seqlen)) return 0;
-    return seg_ws(pm::linear_plan(batch, heads, seqlen), batch * heads, dk, dv).total;
+    return seg_ws(pm::linear_plan(batch, heads, dk, dv, seqlen, false), batch * heads, dk, dv).total;
 }
 
 int packmamba_linear_attention_fwd(const void* q, const void* k, const void* v, const float* decay,
@@ -94,7 +94,7 @@ int packmamba_linear_attention_fwd(const void* q, const void* k, const void* v, 
     if (int e = check_heads(batch, heads, groups, dk, dv, seqlen)) return e;
     if (int e = check_dtype(dtype)) return e;
     if (!aligned16(q, k, v, decay, position_indices, initial_state, out, final_state, workspace)) return PACKMAMBA_ERR_ALIGN;
-    const pm::LinPlan p = pm::linear_plan(batch, heads, seqlen);
+    const pm::LinPlan p = pm::linear_plan(batch, heads, dk, dv, seqlen, false);
     const SegWs w = seg_ws(p, batch * heads, dk, dv);
     if (w.total && (!workspace || workspace_bytes < w.total)) return PACKMAMBA_ERR_WORKSPACE;
     pm::WalkArgs a{};
@@ -120,7 +120,7 @@ int packmamba_linear_attention_fwd(const void* q, const void* k, const void* v, 
 size_t packmamba_linear_attention_bwd_workspace_size(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
                                                      int64_t seqlen) {
     if (check_heads(batch, heads, groups, dk, dv, seqlen)) return 0;
-    return bwd_ws(pm::linear_plan(batch, heads, seqlen), batch, heads, groups, dk, dv, seqlen).total;
+    return bwd_ws(pm::linear_plan(batch, heads, dk, dv, seqlen, true), batch, heads, groups, dk, dv, seqlen).total;
 }
 
 int packmamba_linear_attention_bwd(const void* q, const void* k, const void* v, const float* decay,
@@ -137,7 +137,7 @@ int packmamba_linear_attention_bwd(const void* q, const void* k, const void* v, 
     if (!aligned16(q, k, v, decay, position_indices, initial_state, dout, dfinal_state) ||
         !aligned16(dq, dk, dv, ddecay, dinitial_state, workspace))
         return PACKMAMBA_ERR_ALIGN;
-    const pm::LinPlan p = pm::linear_plan(batch, heads, seqlen);
+    const pm::LinPlan p = pm::linear_plan(batch, heads, dk_size, dv_size, seqlen, true);
     const BwdWs w = bwd_ws(p, batch, heads, groups, dk_size, dv_size, seqlen);
     if (!workspace || workspace_bytes < w.total) return PACKMAMBA_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
