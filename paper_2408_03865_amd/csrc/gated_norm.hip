@@ -31,11 +31,12 @@ bool far(const GatedArgs& a) { return a.dim / a.groups * a.seqlen >= (int64_t)1 
 // The block's tile.  Blocks go to the 8 XCDs in turn; where rows end inside a line, neighbouring tiles share lines
 // and are given to one XCD, an eighth of all tiles each, whose L2 then holds them (us, in turn and in eighths,
 // forward and backward: 2 x 3001 x 1536 fp32 35, 56 against 24, 48; 8 x 4096 x 4096 bf16, whole lines, 169, 339
-// against 180, 343).
-template <typename T>
+// against 180, 343), and so where a tile's piece of a row is less than a line (2 x 1024 x 4096 in tiles of 16 tokens 48,
+// 82 against 29, 54).
+template <typename T, int TILE>
 __device__ __forceinline__ uint32_t tile_block(int64_t L) {
     const uint32_t id = blockIdx.x, per = gridDim.x / 8;
-    return L * (int64_t)sizeof(T) % 128 && id < per * 8 ? (id % 8) * per + id / 8 : id;
+    return (TILE * sizeof(T) < 128 || L * (int64_t)sizeof(T) % 128) && id < per * 8 ? (id % 8) * per + id / 8 : id;
 }
 
 // The same raw values, unknown to the compiler: what it computed from them for the sum is computed again after it
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
     __shared__ float red[THREADS / 64][GROUPS * TOK];
     const int grp = threadIdx.x % GROUPS, sl = threadIdx.x / GROUPS;
     const int64_t L = a.seqlen, tiles = (L + GROUPS * TOK - 1) / (GROUPS * TOK);
-    const uint32_t id = tile_block<T>(L);
+    const uint32_t id = tile_block<T, GROUPS * TOK>(L);
     const int64_t bg = id / (uint32_t)tiles, t0 = (id - bg * tiles) * (GROUPS * TOK);
     const int per = (int)(a.dim / a.groups);
     const bool whole = t0 + GROUPS * TOK <= L || L % TOK == 0;     // no vector crosses the row end
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_token(GatedArgs a) {
 
 // With up the gradient of a rstd (dout weight, or dout weight gate) and m the mean of up a over the group,
 //   da = rstd (up - a rstd^2 m), and from it dx and dz; partial[b, tile, f] = the tile's sum for dweight.
-// A tile is kRmsTile tokens, or fewer that hold the whole row: partial has one row for kRmsTile tokens.
+// A tile has gated_tile() tokens, and partial a row for each.
 template <typename T, typename TO, int GROUPS, int THREADS, int KEPT, bool FIRST, bool FAR>
 __global__ __launch_bounds__(THREADS, (THREADS >= 512 ? 4 : THREADS / 128)) void gated_bwd_kernel(GatedArgs a) {
     constexpr int TOK = Storage<T>::kPerVec, SL = THREADS / GROUPS;
@@ -252,7 +253,7 @@ __global__ __launch_bounds__(THREADS, (THREADS >= 512 ? 4 : THREADS / 128)) void
     const int grp = threadIdx.x % GROUPS, sl = threadIdx.x / GROUPS;
     constexpr int kTile = GROUPS * TOK;
     const int64_t L = a.seqlen, tiles = (L + kTile - 1) / kTile;
-    const uint32_t id = tile_block<T>(L);
+    const uint32_t id = tile_block<T, kTile>(L);
     const int64_t bg = id / (uint32_t)tiles, tile = id - bg * tiles, t0 = tile * kTile;
     const int64_t b = bg / a.groups;
     const int per = (int)(a.dim / a.groups), first = (int)(bg - b * a.groups) * per;
@@ -383,15 +384,22 @@ hipError_t token_one(const GatedArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-constexpr int64_t kFewTokens = 8;       // rows no longer take a narrow tile: more slices of the features
-
+// Threads of a block: slices that leave a thread about as many features as it keeps.  Us of the bf16 forward and
+// backward of 2 x 4096 tokens with 256, 512 and 1024 threads (features of a group):
+//   2048 in groups of 128 24, 38, 91; 35, 40, 61   of 256 19, 24, 51; 37, 36, 47   4096 in groups of 512 41, 34, 58; 76, 72, 74
+//   4096 in one 130, 72, 62; 219, 126, 97          fp32 backward, 2048 in groups of 256 75, 66, 60
+// Single tokens with 64 and 512: 64 x 4096 in groups of 512 3.8, 5.2, of 768 4.0, 4.1, in one 8.4, 4.2.  Tiles of 8 tokens
+// with 256 and 1024: 64 rows of 4 x 4096 in groups of 512 10.1, 14.2, of 1024 12.5, 10.2; tiles of 16: 256 tokens in groups of
+// 512 8.0, 11.4, of 4096 30, 19.
 template <typename T, typename TO, bool FIRST>
 hipError_t fwd_t(const GatedArgs& a, hipStream_t s) {
-    constexpr int kNarrow = (int)kFewTokens / Storage<T>::kPerVec;
-    const int64_t per = a.dim / a.groups;
+    constexpr int kFew = (int)kGatedFewTokens / Storage<T>::kPerVec, kNarrow = (int)kGatedNarrow / Storage<T>::kPerVec;
+    const int64_t per = a.dim / a.groups, tile = gated_tile(a.batch, a.seqlen, a.groups);
     if (a.seqlen == 1) return per <= 512 ? token_one<T, TO, 64, 2, FIRST>(a, s) : token_one<T, TO, 512, 2, FIRST>(a, s);
-    if (a.seqlen <= kFewTokens)
-        return per <= 512 ? fwd_one<T, TO, kNarrow, 256, 2, FIRST>(a, s) : fwd_one<T, TO, kNarrow, 1024, 4, FIRST>(a, s);
+    if (tile == kGatedFewTokens)
+        return per <= 512 ? fwd_one<T, TO, kFew, 256, 2, FIRST>(a, s) : fwd_one<T, TO, kFew, 1024, 4, FIRST>(a, s);
+    if (tile == kGatedNarrow)
+        return per <= 512 ? fwd_one<T, TO, kNarrow, 256, 4, FIRST>(a, s) : fwd_one<T, TO, kNarrow, 1024, 4, FIRST>(a, s);
     if (per <= 256) return fwd_one<T, TO, 8, 256, 8, FIRST>(a, s);
     if (per <= 512) return fwd_one<T, TO, 8, 512, 8, FIRST>(a, s);
     return fwd_one<T, TO, 8, 1024, 8, FIRST>(a, s);
@@ -410,10 +418,13 @@ hipError_t bwd_one(const GatedArgs& a, hipStream_t s) {
 
 template <typename T, typename TO, bool FIRST>
 hipError_t bwd_t(const GatedArgs& a, hipStream_t s) {
-    constexpr int TOK = Storage<T>::kPerVec, kWide = (int)kRmsTile / TOK, kNarrow = (int)kFewTokens / TOK;
-    const int64_t per = a.dim / a.groups;
-    if (a.seqlen <= kFewTokens)
-        return per <= 512 ? bwd_one<T, TO, kNarrow, 256, 2, FIRST>(a, s) : bwd_one<T, TO, kNarrow, 1024, 4, FIRST>(a, s);
+    constexpr int TOK = Storage<T>::kPerVec, kWide = (int)kRmsTile / TOK;
+    constexpr int kFew = (int)kGatedFewTokens / TOK, kNarrow = (int)kGatedNarrow / TOK;
+    const int64_t per = a.dim / a.groups, tile = gated_tile(a.batch, a.seqlen, a.groups);
+    if (tile == kGatedFewTokens)
+        return per <= 512 ? bwd_one<T, TO, kFew, 256, 2, FIRST>(a, s) : bwd_one<T, TO, kFew, 1024, 4, FIRST>(a, s);
+    if (tile == kGatedNarrow)
+        return per <= 512 ? bwd_one<T, TO, kNarrow, 256, 4, FIRST>(a, s) : bwd_one<T, TO, kNarrow, 1024, 4, FIRST>(a, s);
     if (per <= 128) return bwd_one<T, TO, kWide, 256, 4, FIRST>(a, s);
     if (per <= 256) return bwd_one<T, TO, kWide, 512, 4, FIRST>(a, s);
     return bwd_one<T, TO, kWide, 1024, 4, FIRST>(a, s);

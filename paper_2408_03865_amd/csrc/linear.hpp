@@ -150,9 +150,23 @@ struct GatedArgs {
     int64_t batch, dim, seqlen;
     int32_t groups, gate_first, dtype;
 };
-// rows of dweight's partial sums: one for each kRmsTile tokens of a batch row
-inline int64_t gated_bwd_partial_rows(int64_t batch, int64_t seqlen) {
-    return batch * ((seqlen + kRmsTile - 1) / kRmsTile);
+// Tokens of a block's tile: 64 (the fp32 forward 32) where that makes more than 64 tiles of them, 16 where fewer
+// leave CUs idle, 8 for rows of no more.  Fewer tokens are more slices of the features, and shorter pieces of lines.
+// Us of the bf16 forward and backward, tiles of 16 against 64 (batch x tokens x features, groups):
+//   1 x 64 x 4096, 1 (1 tile of 64) 19, 48; 26, 73     1 x 512 x 4096, 1 (8) 19, 49; 27, 73    2 x 1024 x 4096, 1 (32) 29, 51; 54, 86
+//   1 x 256 x 4096, 8 (32) 7.9, 10.3; 10.7, 16.6       1 x 512 x 4096, 8 (64) 9.0, 10.3; 13, 17    4 x 1024 x 4096, 1 (64) 49, 58; 94, 87
+//   2 x 1024 x 4096, 4 (128) 24, 18; 39, 31            8 x 1024 x 4096, 1 (128) 91, 64; 166, 99
+// and in fp32 4 x 1024 x 4096, 1 57, 56; 94, 131, 2 x 1024 x 4096, 4 24, 19; 46, 47.
+// Rows of 4 and 8 tokens (4 x 4096, 1 group, bf16): tiles of 8 18 and 10 us, of 64 78 and 54.
+constexpr int64_t kGatedFewTokens = 8, kGatedFewTiles = 64, kGatedNarrow = 16;
+inline int64_t gated_tile(int64_t batch, int64_t seqlen, int64_t groups) {
+    if (seqlen <= kGatedFewTokens) return kGatedFewTokens;
+    return batch * groups * ((seqlen + kRmsTile - 1) / kRmsTile) <= kGatedFewTiles ? kGatedNarrow : kRmsTile;
+}
+// rows of dweight's partial sums: one for each tile of a batch row
+inline int64_t gated_bwd_partial_rows(int64_t batch, int64_t seqlen, int64_t groups) {
+    const int64_t tile = gated_tile(batch, seqlen, groups);
+    return batch * ((seqlen + tile - 1) / tile);
 }
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s);
 hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s);

@@ -246,7 +246,7 @@ int packmamba_gated_rmsnorm_fwd(const void* x, const void* z, const float* weigh
 
 size_t packmamba_gated_rmsnorm_bwd_workspace_size(int64_t batch, int64_t dim, int64_t seqlen, int64_t groups) {
     if (check_norm(batch, dim, seqlen, groups)) return 0;
-    return floats(pm::gated_bwd_partial_rows(batch, seqlen) * dim);
+    return floats(pm::gated_bwd_partial_rows(batch, seqlen, groups) * dim);
 }
 
 int packmamba_gated_rmsnorm_bwd(const void* x, const void* z, const float* weight, const float* rstd, const void* dout,

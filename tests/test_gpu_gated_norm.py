@@ -52,7 +52,10 @@ def held(name, got, ref, n, rounded):
 
 # one token, tiles of whole and of partial vectors, odd lengths, groups of one feature, of few and of more than is kept
 SHAPES = [(1, 1, 1, 1), (5, 96, 1, 1), (3, 4096, 1, 1), (2, 70, 33, 1), (2, 48, 64, 6), (3, 24, 130, 24), (1, 640, 100, 5),
-          (2, 1100, 72, 1), (1, 2600, 129, 2), (1, 5000, 40, 1), (70, 64, 7, 2)]
+          (2, 1100, 72, 1), (1, 2600, 129, 2), (1, 5000, 40, 1), (70, 64, 7, 2),
+          # tiles of 64 tokens: more than 64 of them, groups for each number of threads; then 64, of 16 tokens each
+          (3, 36, 130, 12), (33, 200, 70, 1), (70, 300, 9, 1), (33, 1100, 72, 1), (34, 1040, 64, 2), (66, 4200, 33, 1),
+          (1, 40, 4160, 1), (1, 40, 4096, 1), (4, 1040, 1016, 1), (1, 128, 16, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -38,7 +38,10 @@ def test_sizes():
                 (1 << 21, 2, 2, 64, 64, 64), (1, 1, 1, 64, 64, (1 << 22) + 1), (1, 8, 8, 64, 64, 1 << 40), (64, 64, 64, 128, 128, 1 << 17), (1 << 62, 4, 4, 8, 8, 8)]:
         assert fwd(*bad) == 0 and bwd(*bad) == 0, bad
     norm = lib.packmamba_gated_rmsnorm_bwd_workspace_size
-    assert norm(2, 48, 130, 3) == 2 * 3 * 48 * 4 // 256 * 256 + (256 if 2 * 3 * 48 * 4 % 256 else 0)
+    up = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    assert norm(4, 48, 130, 6) == up(4 * 3 * 48 * 4)           # 72 tiles of 64 tokens
+    assert norm(2, 48, 130, 3) == up(2 * 9 * 48 * 4)           # 18 of them: tiles of 16
+    assert norm(2, 48, 8, 3) == up(2 * 48 * 4)                 # one of 8
     assert norm(2, 48, 130, 5) == 0 and norm(0, 48, 130, 3) == 0 and norm(1 << 20, 48, 1, 3) == 0 and norm(1 << 10, 8, 1 << 14, 8) == 0
 
 
