@@ -30,9 +30,9 @@ bool far(const GatedArgs& a) { return a.dim / a.groups * a.seqlen >= (int64_t)1 
 
 // The block's tile.  Blocks go to the 8 XCDs in turn; where rows end inside a line, neighbouring tiles share lines
 // and are given to one XCD, an eighth of all tiles each, whose L2 then holds them (us, in turn and in eighths,
-// forward and backward: 2 x 3001 x 1536 fp32 35, 56 against 24, 48; 8 x 4096 x 4096 bf16, whole lines, 169, 339
-// against 180, 343), and so where a tile's piece of a row is less than a line (2 x 1024 x 4096 in tiles of 16 tokens 48,
-// 82 against 29, 54).
+// forward and backward: 2 x 3001 x 1536 fp32 37, 55 against 28, 45; 8 x 4096 x 4096 bf16, whole lines, 169, 339
+// against 180, 343), and so where a tile's piece of a row is less than a line (2 x 1024 x 4096 in tiles of 16 tokens 49,
+// 87 against 30, 56).
 template <typename T, int TILE>
 __device__ __forceinline__ uint32_t tile_block(int64_t L) {
     const uint32_t id = blockIdx.x, per = gridDim.x / 8;
@@ -52,6 +52,33 @@ __device__ __forceinline__ void forget(RawRun<T, K>& r) {
             r.w[i][k] = v;
         }
 }
+
+// The TOK tokens that a lane takes, from l0 on.  In rows of a vector and more (FULL) all loads are whole vectors: the one
+// that would cross the row's end is read from further ahead, and lanes beyond the end read it too; a lane's own
+// tokens are those from the own-th on.  Reading that vector's elements one by one, and its tile's features twice, made
+// the row's last tile the last to end: 2 x 1001 x 4096 bf16, one group, 64 and 115 us, now 45 and 82.
+template <int TOK>
+struct Lane {
+    int64_t l0;
+    int own;
+    __device__ Lane(int64_t L, int64_t t0, int grp) {
+        const int64_t lt = t0 + grp * TOK;
+        l0 = L >= TOK ? min(lt, L - TOK) : lt;
+        own = L < TOK ? 0 : lt < L ? (int)(lt - l0) : TOK;
+    }
+    template <bool FULL, typename TO>
+    __device__ __forceinline__ void store(TO* p, int64_t left, const float (&v)[TOK]) const {
+        if constexpr (!FULL) {
+            store_run<TO, TOK, false>(p, 0, left, v);
+        } else if (own == 0) {
+            store_run<TO, TOK, true>(p, 0, left, v);
+        } else {
+#pragma unroll
+            for (int k = 1; k < TOK; ++k)
+                if (k >= own) Storage<TO>::store1(p + k, v[k]);
+        }
+    }
+};
 
 // Sum over the slices of each token's value, in a fixed order; every thread gets its own tokens' sums.
 template <int GROUPS, int THREADS, int TOK>
@@ -81,9 +108,8 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
     const uint32_t id = tile_block<T, GROUPS * TOK>(L);
     const int64_t bg = id / (uint32_t)tiles, t0 = (id - bg * tiles) * (GROUPS * TOK);
     const int per = (int)(a.dim / a.groups);
-    const bool whole = t0 + GROUPS * TOK <= L || L % TOK == 0;     // no vector crosses the row end
-    const bool live = t0 + grp * TOK < L;
-    const int64_t l0 = whole && !live ? t0 : t0 + grp * TOK;
+    const Lane<TOK> lane(L, t0, grp);
+    const int64_t l0 = lane.l0;
     const int64_t base = bg * per * L;
     const T* x = static_cast<const T*>(a.x) + base;
     const T* z = static_cast<const T*>(a.z) + base;
@@ -137,7 +163,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
         if (sl == 0) {
 #pragma unroll
             for (int k = 0; k < TOK; ++k)
-                if (FULL ? live : l0 + k < L) a.rstd_out[bg * L + l0 + k] = r[k];
+                if (FULL ? k >= lane.own : l0 + k < L) a.rstd_out[bg * L + l0 + k] = r[k];
         }
         const auto put = [&](float (&v)[TOK], const float (&zv)[TOK], int f) {
             const float wv = w[f];
@@ -146,7 +172,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
                 v[k] = v[k] * r[k] * wv;
                 if constexpr (!FIRST) v[k] *= zv[k] * sigmoid_f(zv[k]);
             }
-            if (!FULL || live) store_run<TO, TOK, FULL>(at(out, off(f)), 0, left, v);
+            lane.template store<FULL>(at(out, off(f)), left, v);
         };
 #pragma unroll
         for (int i = 0; i < C; ++i) {
@@ -173,7 +199,7 @@ __global__ __launch_bounds__(THREADS) void gated_fwd_kernel(GatedArgs a) {
             put(v, zv, f);
         }
     };
-    if (whole) body(std::true_type{});
+    if (L >= TOK) body(std::true_type{});
     else body(std::false_type{});
 }
 
@@ -257,9 +283,8 @@ __global__ __launch_bounds__(THREADS, (THREADS >= 512 ? 4 : THREADS / 128)) void
     const int64_t bg = id / (uint32_t)tiles, tile = id - bg * tiles, t0 = tile * kTile;
     const int64_t b = bg / a.groups;
     const int per = (int)(a.dim / a.groups), first = (int)(bg - b * a.groups) * per;
-    const bool whole = t0 + kTile <= L || L % TOK == 0;
-    const bool live = t0 + grp * TOK < L;
-    const int64_t l0 = whole && !live ? t0 : t0 + grp * TOK;
+    const Lane<TOK> lane(L, t0, grp);
+    const int64_t l0 = lane.l0;
     const int64_t base = bg * per * L;
     const T* x = static_cast<const T*>(a.x) + base;
     const T* z = static_cast<const T*>(a.z) + base;
@@ -322,19 +347,16 @@ __global__ __launch_bounds__(THREADS, (THREADS >= 512 ? 4 : THREADS / 128)) void
                     const float av = xv[k] * gate, da = r[k] * (gv[k] * wv - av * c[k]);
                     ox[k] = da * gate;
                     oz[k] = da * xv[k] * dgate;
-                    pw = fmaf(gv[k] * av, r[k], pw);
+                    pw = k >= lane.own ? fmaf(gv[k] * av, r[k], pw) : pw;
                 } else {
                     ox[k] = r[k] * (gv[k] * wv * gate - xv[k] * c[k]);
                     const float n = gv[k] * xv[k] * r[k];
                     oz[k] = n * wv * dgate;
-                    pw = fmaf(n, gate, pw);
+                    pw = k >= lane.own ? fmaf(n, gate, pw) : pw;
                 }
             }
-            if (FULL && !live) pw = 0.0f;
-            if (!FULL || live) {
-                store_run<TO, TOK, FULL>(at(dx, off(f)), 0, left, ox);
-                store_run<TO, TOK, FULL>(at(dz, off(f)), 0, left, oz);
-            }
+            lane.template store<FULL>(at(dx, off(f)), left, ox);
+            lane.template store<FULL>(at(dz, off(f)), left, oz);
 #pragma unroll
             for (int m = 1; m < GROUPS; m *= 2) pw += __shfl_xor(pw, m, GROUPS);
             if (grp == 0) part[f] = pw;
@@ -363,7 +385,7 @@ __global__ __launch_bounds__(THREADS, (THREADS >= 512 ? 4 : THREADS / 128)) void
             grad(xv, zv, gv, f);
         }
     };
-    if (whole) body(std::true_type{});
+    if (L >= TOK) body(std::true_type{});
     else body(std::false_type{});
 }
 

@@ -1,7 +1,7 @@
 // linear_step.hip -- linear attention of one token a sequence: S <- a S + k v^T, out = scale S^T q, the
 // state (dk, dv) of every batch row and head read and written in place, in 32 bits.
 // Bound by the state's bytes, 8 dk dv a head.  A block takes one head of one batch row, or some of its
-// columns where heads are few: LPR lanes of VEC consecutive columns side by side, 256 / LPR rows at once, all of a
+// columns where heads are few: LPR lanes of four consecutive columns side by side, 256 / LPR rows at once, all of a
 // thread's rows loaded before the first is used.
 #include "common.hpp"
 #include "linear.hpp"
@@ -9,12 +9,26 @@
 namespace pm {
 namespace {
 
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 constexpr int kThreads = 256;
 constexpr float kStepCut = -104.0f;      // as a chunk's decays: exp of it is 0 in 32 bits
 
-template <typename T, typename TO, int VEC, int LPR>
+template <bool ALIGNED>
+__device__ __forceinline__ f32x4 load4(const float* p) {
+    if constexpr (ALIGNED) return *reinterpret_cast<const f32x4*>(p);
+    else return *reinterpret_cast<const f32x4_a4*>(p);
+}
+template <bool ALIGNED>
+__device__ __forceinline__ void store4(float* p, const f32x4& v) {
+    if constexpr (ALIGNED) *reinterpret_cast<f32x4*>(p) = v;
+    else *reinterpret_cast<f32x4_a4*>(p) = v;
+}
+
+// WHOLE: a row of the state is whole vectors, 16-byte aligned; else vectors have an element's alignment and a row's
+// last columns go one by one.
+template <typename T, typename TO, bool WHOLE, int LPR>
 __global__ __launch_bounds__(kThreads) void step_kernel(LinStepArgs a) {
-    constexpr int R = kThreads / LPR, kCols = LPR * VEC, kAhead = R >= 16 ? 8 : 16;
+    constexpr int VEC = 4, R = kThreads / LPR, kCols = LPR * VEC, kAhead = R >= 16 ? 8 : 16;
     __shared__ float qk[2][kLinMaxHead];
     __shared__ float red[kThreads / 64][kCols];
     const int parts = (a.dv + kCols - 1) / kCols;
@@ -23,13 +37,14 @@ __global__ __launch_bounds__(kThreads) void step_kernel(LinStepArgs a) {
     const int64_t b = bh / a.heads, h = bh - b * a.heads;
     const int lane = threadIdx.x % LPR, row = threadIdx.x / LPR;
     const int c = part * kCols + lane * VEC;
-    const bool live = c < a.dv;
+    const bool live = c < a.dv, vector = WHOLE ? live : c + VEC <= a.dv;
     const int p = a.pos ? a.pos[b] : 1;
     TO* out = static_cast<TO*>(a.out) + bh * a.dv;
     if (p < 0) {                                          // an idle row
         if (row == 0 && live) {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) Storage<TO>::store1(out + c + i, 0.0f);
+            for (int i = 0; i < VEC; ++i)
+                if (WHOLE || c + i < a.dv) Storage<TO>::store1(out + c + i, 0.0f);
         }
         return;
     }
@@ -42,7 +57,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(LinStepArgs a) {
     const T* k = static_cast<const T*>(a.k) + gq;
     float v[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = live ? Storage<T>::load1(static_cast<const T*>(a.v) + bh * a.dv + c + i) : 0.0f;
+    for (int i = 0; i < VEC; ++i) v[i] = c + i < a.dv ? Storage<T>::load1(static_cast<const T*>(a.v) + bh * a.dv + c + i) : 0.0f;
     float acc[VEC] = {};
     bool staged = false;
     for (int f0 = 0; f0 < a.dk; f0 += R * kAhead) {
@@ -52,14 +67,15 @@ __global__ __launch_bounds__(kThreads) void step_kernel(LinStepArgs a) {
             const int f = f0 + n * R + row;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s[n][i] = 0.0f;
-            if (f < a.dk && live && !cut) {
-                if constexpr (VEC == 4) {
-                    const f32x4 w = *reinterpret_cast<const f32x4*>(st + f * a.dv);
+            if (f < a.dk && vector && !cut) {
+                const f32x4 w = load4<WHOLE>(st + f * a.dv);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[n][i] = w[i];
-                } else {
-                    s[n][0] = st[f * a.dv];
-                }
+                for (int i = 0; i < VEC; ++i) s[n][i] = w[i];
+            }
+            if (!WHOLE && f < a.dk && live && !vector && !cut) {
+#pragma unroll
+                for (int i = 0; i < VEC - 1; ++i)
+                    if (c + i < a.dv) s[n][i] = st[f * a.dv + i];
             }
         }
         if (!staged) {                                    // block-uniform
@@ -80,8 +96,13 @@ __global__ __launch_bounds__(kThreads) void step_kernel(LinStepArgs a) {
                     s[n][i] = cut ? kf * v[i] : fmaf(decay, s[n][i], kf * v[i]);
                     acc[i] = fmaf(qf, s[n][i], acc[i]);
                 }
-                if constexpr (VEC == 4) *reinterpret_cast<f32x4*>(st + f * a.dv) = f32x4{s[n][0], s[n][1], s[n][2], s[n][3]};
-                else st[f * a.dv] = s[n][0];
+                if (vector) {
+                    store4<WHOLE>(st + f * a.dv, f32x4{s[n][0], s[n][1], s[n][2], s[n][3]});
+                } else if (!WHOLE) {
+#pragma unroll
+                    for (int i = 0; i < VEC - 1; ++i)
+                        if (c + i < a.dv) st[f * a.dv + i] = s[n][i];
+                }
             }
         }
     }
@@ -102,22 +123,25 @@ __global__ __launch_bounds__(kThreads) void step_kernel(LinStepArgs a) {
     }
 }
 
-template <typename T, typename TO, int VEC, int LPR>
+template <typename T, typename TO, bool WHOLE, int LPR>
 hipError_t step_one(const LinStepArgs& a, hipStream_t s) {
-    const int64_t parts = (a.dv + LPR * VEC - 1) / (LPR * VEC);
-    hipLaunchKernelGGL((step_kernel<T, TO, VEC, LPR>), dim3((unsigned)((int64_t)a.batch * a.heads * parts)), dim3(kThreads),
+    const int64_t parts = (a.dv + LPR * 4 - 1) / (LPR * 4);
+    hipLaunchKernelGGL((step_kernel<T, TO, WHOLE, LPR>), dim3((unsigned)((int64_t)a.batch * a.heads * parts)), dim3(kThreads),
                        0, s, a);
     return hipGetLastError();
 }
 
-// 64 columns of the state in 16-byte vectors, or 16 where the heads alone leave most CUs idle; single columns where a
-// row is no whole number of vectors.  Us with 16, 64 and single columns (heads, dk x dv): 24, 64 x 64 4.2, 4.5, 7.8; 24,
-// 128 x 64 4.5, 5.3, 11; 96, 64 x 64 5.1, 4.7, 7.9; 160, 128 x 64 7.7, 5.9, 11; 1024, 128 x 128 38, 24, 55 (all 128
-// columns 25).  4096 heads of 128 x 64 take 57 us, 4.7 TB/s of states read and written, a large copy's rate.
+// 64 columns of the state in 16-byte vectors, or 16 where the heads alone leave most CUs idle.  Us with 16 and 64 (heads,
+// dk x dv): 24, 64 x 64 4.2, 4.5; 24, 128 x 64 4.5, 5.3; 96, 64 x 64 5.1, 4.7; 160, 128 x 64 7.7, 5.9; 1024, 128 x 128
+// 38, 24 (all 128 columns 25).  4096 heads of 128 x 64 take 57 us, 4.7 TB/s of states read and written, a large
+// copy's rate.
+template <typename T, typename TO, bool WHOLE>
+hipError_t step_w(const LinStepArgs& a, hipStream_t s) {
+    return (int64_t)a.batch * a.heads <= 64 ? step_one<T, TO, WHOLE, 4>(a, s) : step_one<T, TO, WHOLE, 16>(a, s);
+}
 template <typename T, typename TO>
 hipError_t step_t(const LinStepArgs& a, hipStream_t s) {
-    if (a.dv % 4) return step_one<T, TO, 1, 64>(a, s);
-    return (int64_t)a.batch * a.heads <= 64 ? step_one<T, TO, 4, 4>(a, s) : step_one<T, TO, 4, 16>(a, s);
+    return a.dv % 4 ? step_w<T, TO, false>(a, s) : step_w<T, TO, true>(a, s);
 }
 
 }  // namespace
