@@ -50,7 +50,7 @@ __global__ void walk_chain(float* __restrict__ seg, const float* __restrict__ se
 template <typename T, int KC, int VP>
 hipError_t aggregate_vp(const WalkArgs& a, hipStream_t s) {
     constexpr int NS = Mat<T>::kSplit ? 3 : 1;
-    const dim3 grid((unsigned)((int64_t)a.batch * a.heads * (a.nseg - 1))), block(walk_threads<T, KC, VP>());
+    const dim3 grid((unsigned)((int64_t)a.batch * a.heads * (a.nseg - 1))), block(walk_threads(VP, walk_parts<T, KC, VP>()));
     if (a.rev) hipLaunchKernelGGL((walk_aggregate<T, KC, VP, true, NS>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((walk_aggregate<T, KC, VP, false, NS>), grid, block, 0, s, a);
     return hipGetLastError();

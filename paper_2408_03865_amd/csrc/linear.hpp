@@ -67,8 +67,11 @@ inline int64_t walk_bound_floats(int32_t x_rows, int32_t z_rows) {
 // Us of a bf16 call, dk and dv 64, planned and unsplit (batch x heads x tokens, forward then the whole backward):
 //   4 x 24 x 2048 56, 83; 188, 376   2 x 64 x 4096 (dk 128) 132, 206; 576, 1000   1 x 300 x 4096 222, 220; 1046, 1225
 //   1 x 32 x 16384 103, 623; 398, 2670   1 x 8 x 320 24, 18; 58, 79   1 x 150 x 2048 (dk 128) 105, 108; 471, 565
-// and 1 x 100 x 4096 with dk and dv 128 227, 259; 892, 1213.
+// and 1 x 100 x 4096 with dk and dv 128 227, 259; 892, 1213.  More segments to use the four blocks a CU of one part
+// (below) gain nothing: 1 x 32 x 65536 forward in 16 a row 455, in 32 492.
 constexpr int64_t kSplitChunks = 4;     // rows of fewer are walked whole
+// Blocks from which plain bf16 walks of heads of up to 64 features take one part (linear_walk.hpp).
+constexpr int64_t kManyWalks = 768;
 // Chunks between the boundaries at which the backward takes the product of the two states.
 constexpr int32_t kBoundChunks = 8;
 

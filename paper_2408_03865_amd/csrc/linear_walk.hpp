@@ -457,15 +457,19 @@ __device__ __forceinline__ void store_sum16(int l, float* four, const f32x2& s) 
     }
 }
 
-// bf16: the x features are split over two waves, so that twice the waves share a chunk's latencies; each
-// multiplies x with its half of the state for all tokens, and the sums meet in LDS.
+// Parts: in bf16 the x features can be split over two waves, so that twice the waves share a chunk's latencies; each
+// multiplies x with its half of the state for all tokens, and the sums meet in LDS.  One part has fewer waves,
+// but more blocks to a CU, and does less in all: plain walks of heads of up to 64 features take it from 768 blocks
+// on.  Us with one part and two (batch x heads x 4096 tokens, forward): dk and dv 64, 4 x 64 231, 185; 8 x 64 281, 283;
+// 12 x 64 338, 408; 16 x 64 413, 511; dk 128, dv 64, 8 x 64 402, 382; 16 x 64 718, 679; the whole backward of 8 x 32 heads,
+// dk and dv 128, 2068, 1477.
 template <typename T, int KC, int VP>
 constexpr int walk_parts() {
     return sizeof(T) == 2 && KC >= VP ? 2 : 1;
 }
-template <typename T, int KC, int VP, int MODE>
+template <typename T, int KC, int VP, int MODE, int kParts>
 struct WalkSmem {
-    static constexpr int kParts = walk_parts<T, KC, VP>(), kWaves = VP / 16 * kParts;
+    static constexpr int kWaves = VP / 16 * kParts;
     __attribute__((aligned(16))) T x[KC * kC];
     __attribute__((aligned(16))) T y[KC * kC];
     __attribute__((aligned(16))) T z[VP * kC];
@@ -485,21 +489,19 @@ constexpr int walk_waves() {
     if (sizeof(T) == 4) return VP == 64 ? 1 : 2;
     return 4;
 }
-template <typename T, int KC, int VP>
-constexpr int walk_threads() {
-    return VP * 4 * walk_parts<T, KC, VP>();
-}
+constexpr int walk_threads(int VP, int parts) { return VP * 4 * parts; }
 
 // Wave (z tile, part): 16 of z's features, and of the x features and the out's tokens all or, of two waves,
 // half.  All waves share the products of x and y by strips of 16 x's and parts of the y's.
-template <typename T, typename TO, int KC, int VP, int MODE, bool REV, int NS, int NO>
-__global__ __launch_bounds__((walk_threads<T, KC, VP>()), (walk_waves<T, KC, VP, MODE>())) void walk_kernel(WalkArgs a) {
+template <typename T, typename TO, int KC, int VP, int MODE, bool REV, int NS, int NO, int kParts>
+__global__ __launch_bounds__((walk_threads(VP, kParts)), (walk_waves<T, KC, VP, MODE>())) void walk_kernel(WalkArgs a) {
     using M = Mat<T>;
     using Frag = typename M::Frag;
-    constexpr int KT = KC / 16, VT = VP / 16, kParts = walk_parts<T, KC, VP>(), KF = KT / kParts, XT = 4 / kParts;
+    constexpr int KT = KC / 16, VT = VP / 16, KF = KT / kParts, XT = 4 / kParts;
     constexpr int kWaves = VT * kParts, kThreads = kWaves * 64, kYParts = kWaves / 4, kYTiles = 4 / kYParts;
-    constexpr bool kTight = MODE != kWalkPlain || VP > KC;
-    __shared__ WalkSmem<T, KC, VP, MODE> sm;
+    // short of registers
+    constexpr bool kTight = MODE != kWalkPlain || VP > KC || (REV && kParts < walk_parts<T, KC, VP>());
+    __shared__ WalkSmem<T, KC, VP, MODE, kParts> sm;
     const int l = lane_id(), w = wave_id();
     const int64_t L = a.seqlen;
     const uint32_t id = walk_block((uint32_t)a.batch * a.heads * a.nseg);       // at most 2^23 of them
@@ -806,8 +808,8 @@ struct AggSmem {
 };
 
 template <typename T, int KC, int VP, bool REV, int NS>
-__global__ __launch_bounds__((walk_threads<T, KC, VP>())) void walk_aggregate(WalkArgs a) {
-    constexpr int VT = VP / 16, KF = KC / 16 / walk_parts<T, KC, VP>(), kThreads = walk_threads<T, KC, VP>();
+__global__ __launch_bounds__((walk_threads(VP, walk_parts<T, KC, VP>()))) void walk_aggregate(WalkArgs a) {
+    constexpr int VT = VP / 16, KF = KC / 16 / walk_parts<T, KC, VP>(), kThreads = walk_threads(VP, walk_parts<T, KC, VP>());
     __shared__ AggSmem<T, KC, VP> sm;
     const int l = lane_id(), w = wave_id();
     const int64_t L = a.seqlen;
@@ -873,27 +875,32 @@ __global__ __launch_bounds__((walk_threads<T, KC, VP>())) void walk_aggregate(Wa
 // --------------------------------------------------------------------------------------------
 // launches: one T, TO and KC in each translation unit
 // --------------------------------------------------------------------------------------------
-template <typename T, typename TO, int KC, int VP, int MODE, bool REV, int NS, int NO>
+template <typename T, typename TO, int KC, int VP, int MODE, bool REV, int NS, int NO, int PARTS = walk_parts<T, KC, VP>()>
 hipError_t launch_walk_one(const WalkArgs& a, hipStream_t s) {
     const int64_t blocks = (int64_t)a.batch * a.heads * a.nseg;
-    hipLaunchKernelGGL((walk_kernel<T, TO, KC, VP, MODE, REV, NS, NO>), dim3((unsigned)blocks), dim3(walk_threads<T, KC, VP>()),
-                       0, s, a);
+    hipLaunchKernelGGL((walk_kernel<T, TO, KC, VP, MODE, REV, NS, NO, PARTS>), dim3((unsigned)blocks),
+                       dim3(walk_threads(VP, PARTS)), 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T, typename TO, int KC, int VP, bool REV, int PARTS = walk_parts<T, KC, VP>()>
+hipError_t launch_walk_plain(const WalkArgs& a, bool exact, hipStream_t s) {
+    constexpr int kAll = Mat<T>::kSplit ? 3 : 1, kSome = Mat<T>::kSplit ? 2 : 1;
+    return exact ? launch_walk_one<T, TO, KC, VP, kWalkPlain, REV, kAll, 1, PARTS>(a, s)
+                 : launch_walk_one<T, TO, KC, VP, kWalkPlain, REV, kSome, 1, PARTS>(a, s);
 }
 
 template <typename T, typename TO, int KC, int VP>
 hipError_t launch_walk_vp(const WalkArgs& a, WalkMode mode, bool exact, hipStream_t s) {
-    constexpr int kAll = Mat<T>::kSplit ? 3 : 1, kSome = Mat<T>::kSplit ? 2 : 1;
-    switch (mode) {
-        case kWalkDq: return launch_walk_one<T, TO, KC, VP, kWalkDq, false, kAll, kAll>(a, s);
-        case kWalkDk: return launch_walk_one<T, TO, KC, VP, kWalkDk, true, kAll, kAll>(a, s);
-        default:
-            if (a.rev)
-                return exact ? launch_walk_one<T, TO, KC, VP, kWalkPlain, true, kAll, 1>(a, s)
-                             : launch_walk_one<T, TO, KC, VP, kWalkPlain, true, kSome, 1>(a, s);
-            return exact ? launch_walk_one<T, TO, KC, VP, kWalkPlain, false, kAll, 1>(a, s)
-                         : launch_walk_one<T, TO, KC, VP, kWalkPlain, false, kSome, 1>(a, s);
+    constexpr int kAll = Mat<T>::kSplit ? 3 : 1;
+    if (mode == kWalkDq) return launch_walk_one<T, TO, KC, VP, kWalkDq, false, kAll, kAll>(a, s);
+    if (mode == kWalkDk) return launch_walk_one<T, TO, KC, VP, kWalkDk, true, kAll, kAll>(a, s);
+    if constexpr (sizeof(T) == 2 && KC == 64 && VP == 64) {
+        if ((int64_t)a.batch * a.heads * a.nseg >= kManyWalks)
+            return a.rev ? launch_walk_plain<T, TO, KC, VP, true, 1>(a, exact, s)
+                         : launch_walk_plain<T, TO, KC, VP, false, 1>(a, exact, s);
     }
+    return a.rev ? launch_walk_plain<T, TO, KC, VP, true>(a, exact, s) : launch_walk_plain<T, TO, KC, VP, false>(a, exact, s);
 }
 
 template <typename T, typename TO, int KC>
