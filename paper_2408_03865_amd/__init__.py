@@ -20,6 +20,12 @@ the first part's final states (the future work of §5):
     y2 = selective_scan_fwd(..., pos2, initial_state=hf)
 and in the backward the second part's initial-state gradients are the first part's
 final-state gradients (dfinal_x, dfinal_state).
+
+Linear attention with a decay for each head over the same packed rows, its single-token form and the gated
+RMSNorm (``include/packmamba_linear.h``) are in ``linear.py``:
+    out, state = linear_attention_fwd(q, k, v, decay, position_indices, return_final=True)
+    out = linear_attention_step(q, k, v, decay, state)
+    y, rstd = gated_rmsnorm_fwd(out, z, weight, groups=heads)
 """
 from __future__ import annotations
 

@@ -5,7 +5,9 @@
 // A block owns the features of one group at a tile of consecutive tokens: GROUPS lanes side by side, each with a
 // 16-byte vector of tokens, and THREADS / GROUPS slices of the features.  A thread keeps what it
 // read of its first KEPT features in registers from the sum over the features to the second sweep; features
-// beyond those are read again.  Bound by HBM: three tensors in the forward, five in the backward.
+// beyond those are read again.  Bound by HBM: three tensors in the forward, five in the backward.  8 x 4096
+// tokens x 4096 features in 8 groups, bf16: forward 170 us (4.7 TB/s), backward 334 (4.0 TB/s, a copy 4.9; one block of
+// 1024 threads a CU, whose loads, sum and stores follow each other, the VALU issuing 58% of the cycles).
 #include "common.hpp"
 #include "launch.hpp"
 #include "linear.hpp"
