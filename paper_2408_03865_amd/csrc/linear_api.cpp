@@ -57,7 +57,7 @@ BwdWs bwd_ws(const pm::LinPlan& p, int64_t batch, int64_t heads, int64_t groups,
     const int64_t rows = batch * heads;
     BwdWs w;
     w.seg = seg_ws(p, rows, dk, dv);
-    w.bound = floats(rows * (p.nb + 1) * pm::walk_bound_floats((int32_t)dv, (int32_t)dk));
+    w.bound = floats(rows * p.nb * pm::walk_bound_floats((int32_t)dv, (int32_t)dk));
     w.dot = floats(rows * (p.nb + 1));
     w.r = floats(rows * seqlen);
     w.pieces = floats(rows * p.nb);

@@ -527,9 +527,9 @@ __global__ __launch_bounds__((walk_threads(VP, kParts)), (walk_waves<T, KC, VP, 
     const int64_t sz = (int64_t)a.x.rows * a.z.rows;
     S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a);
 
-    // boundary n of the row: the state there, stored (dq) or multiplied with the one that dq stored (dk)
+    // boundary n of the row, 1 to nb: the state there, stored (dq) or multiplied with the one that dq stored (dk)
     const auto bound_at = [&](int64_t n) {
-        return a.bound + ((bh * (a.nb + 1) + n) * KF * kThreads + here(threadIdx.x)) * 4;
+        return a.bound + ((bh * a.nb + n - 1) * KF * kThreads + here(threadIdx.x)) * 4;
     };
     const auto bound_store = [&](int64_t n) {
         float* p = bound_at(n);

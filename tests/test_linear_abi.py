@@ -37,6 +37,7 @@ def test_sizes():
     for bad in [(0, 8, 8, 64, 64, 64), (1, 8, 3, 64, 64, 64), (1, 8, 8, 129, 64, 64), (1, 8, 8, 64, 0, 64), (1, 8, 8, 64, 64, -1),
                 (1 << 21, 2, 2, 64, 64, 64), (1, 1, 1, 64, 64, (1 << 22) + 1), (1, 8, 8, 64, 64, 1 << 40), (64, 64, 64, 128, 128, 1 << 17), (1 << 62, 4, 4, 8, 8, 8)]:
         assert fwd(*bad) == 0 and bwd(*bad) == 0, bad
+    assert bwd(1024, 64, 64, 64, 64, 64) <= 4 * 65536 * (64 * 64 + 2 + 2 * 64 + 1) + 8 * 256       # one state a row
     norm = lib.packmamba_gated_rmsnorm_bwd_workspace_size
     up = lambda n: (n + 255) // 256 * 256  # noqa: E731
     assert norm(4, 48, 130, 6) == up(4 * 3 * 48 * 4)           # 72 tiles of 64 tokens
