@@ -25,7 +25,7 @@
 // LDS.  Each wave owns 16 of z's features, and of x's all or half: its part of S stays in registers, in
 // the layout that an MFMA result has and, four rows of it a lane, an MFMA operand takes.
 // What bounds it: the waves' own work between three barriers a chunk, none of the units alone.  8 x 64 heads x
-// 4096 tokens, dk 128 and dv 64, bf16, forward: 326 us; the VALU issues 57% of the cycles (weights, the splits of S and of
+// 4096 tokens, dk 128 and dv 64, bf16, forward: 311 to 345 us on different cards; the VALU issues 57% of the cycles (weights, the splits of S and of
 // weighted z), LDS is read and written in 53% (every wave reads all of x and y for its part of z), the matrix units are
 // busy 19%; 682 MB move at 2.1 TB/s.  8 x 32 heads, 128 and 128: dq 528 us (VALU 68%, LDS 37%, matrix 22%), dk 517, dv 308.
 // Longer chunks would do more products inside a chunk, shorter ones split S more often.
