@@ -27,8 +27,10 @@
  * multiplied with are rounded to bf16 once, also where PACKMAMBA_BF16_F32OUT returns 32 bits: out
  * has bf16's accuracy in both.  Final states, the initial state's gradient and the decays' gradient
  * have 32-bit accuracy for all types.  Results are bitwise reproducible.
- * An infinity or NaN does not reach other sequences of the row or earlier tokens (in the backward:
- * later ones).
+ * An infinity or NaN at token t reaches no other sequence, and in its own only what the sums hold it in:
+ *   q: out at t; dk, dv up to t          k: out, dq from t on; dv at t     v: out, dq from t on; dk at t
+ *   dout: dq at t; dk, dv up to t        decay of t: out, dq from t on; dk, dv before t
+ * and ddecay of the sequence's tokens (of the head, where it has one decay).
  */
 #ifndef PACKMAMBA_LINEAR_H
 #define PACKMAMBA_LINEAR_H

@@ -34,9 +34,9 @@
 // split into two or three bf16 terms that hold 16 or all 24 bits of it, and in the walks that feed
 // the decay's gradient so is the copy of S.
 //
-// Infinities and NaN stay in their sequence and do not pass to earlier tokens: masks select, and a
-// chunk whose y or z holds one takes plain loops over the unmasked pairs in place of the matrix
-// products over tokens, where 0 times it would spread.
+// Infinities and NaN reach the outs whose sums hold them and no other: masks select, a chunk whose y or z
+// holds one takes plain loops over the unmasked pairs in place of the matrix products over tokens, where 0
+// times it would spread, and the decays are summed in the walk's direction (chunk_decay).
 #pragma once
 
 #include "common.hpp"
@@ -179,7 +179,7 @@ __device__ __forceinline__ float tile_value(const T* tile, int r, int t) {
 // a chunk's decays
 // --------------------------------------------------------------------------------------------
 struct __attribute__((aligned(16))) ChunkDecay {
-    float hi[kC], lo[kC];       // G in log2 units, as a sum of two floats
+    float hi[kC], lo[kC];       // G in log2 units, as a sum of two floats (its differences are what is used)
     float in[kC], up[kC];       // scaled; 0 where the term is left out
     int32_t start[kC];          // the last start up to the token, -1: none in the chunk
     float a;                    // -1: a start in the chunk
@@ -236,31 +236,66 @@ __device__ __forceinline__ void scan_step(double& v, int& start) {
     }
 }
 
-// One wave, lane = token.  The sum is kept in 64 bits and starts anew at each start, so that no
-// sequence's decays reach another's.
-template <bool REV>
-__device__ __forceinline__ void chunk_decay(const TokenDecay& d, ChunkDecay& c, float iscale, float uscale) {
-    const int l = lane_id();
-    bool cut = d.pos == 0 || d.g <= kDecayCut;
-    double v = cut ? 0.0 : (double)d.g * 1.4426950408889634;
-    int start = cut ? l : -1;
+__device__ __forceinline__ void scan_lanes(double& v, int& start) {
     scan_step<row_shr(1), 0xf>(v, start);
     scan_step<row_shr(2), 0xf>(v, start);
     scan_step<row_shr(4), 0xf>(v, start);
     scan_step<row_shr(8), 0xf>(v, start);
     scan_step<0x142, 0xa>(v, start);     // lane 15 of rows 0 and 2 to the rows after them
     scan_step<0x143, 0xc>(v, start);     // lane 31 to rows 2 and 3
-    const float hi = (float)v, lo = (float)(v - (double)hi);
-    const float ehi = __shfl(hi, 63), elo = __shfl(lo, 63);
-    const int estart = __shfl(start, 63);
-    const float first = start < 0 ? fast_exp2(hi + lo) : 0.0f;
-    const float last = l >= estart ? pair_decay(ehi, elo, hi, lo) : 0.0f;
-    c.hi[l] = hi;
-    c.lo[l] = lo;
-    c.start[l] = start;
-    c.in[l] = (REV ? last : first) * iscale;
-    c.up[l] = (REV ? first : last) * uscale;
-    if (l == 63) c.a = start < 0 ? first : -1.0f;
+}
+
+// The chunk's token whose decay a lane loads: the sums run over the lanes.
+template <bool REV>
+__device__ __forceinline__ int decay_token(int l) {
+    return REV ? kC - 1 - l : l;
+}
+
+// The value of the lane before, 0 in lane 0.
+__device__ __forceinline__ int lane_before(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x138, 0xf, 0xf, false); }
+
+// One wave, lane l = token decay_token(l).  The sum is kept in 64 bits and starts anew at each start, so that no
+// sequence's decays reach another's.  In a reverse walk G is less the sum of the decays after the token, up to the
+// chunk's or the sequence's end: whichever way the walk goes, a sum that holds an infinite decay or a NaN belongs
+// to a token whose out holds it too, by a pair or by the state, and pairs on its other side do not meet it.
+template <bool REV>
+__device__ __forceinline__ void chunk_decay(const TokenDecay& d, ChunkDecay& c, float iscale, float uscale) {
+    const int l = lane_id(), tok = decay_token<REV>(l);
+    const bool cut = d.pos == 0 || d.g <= kDecayCut;
+    double v = cut ? 0.0 : (double)d.g * 1.4426950408889634;
+    if constexpr (!REV) {
+        int start = cut ? l : -1;
+        scan_lanes(v, start);
+        const float hi = (float)v, lo = (float)(v - (double)hi);
+        const float ehi = __shfl(hi, 63), elo = __shfl(lo, 63);
+        const int estart = __shfl(start, 63);
+        const float first = start < 0 ? fast_exp2(hi + lo) : 0.0f;
+        const float last = l >= estart ? pair_decay(ehi, elo, hi, lo) : 0.0f;
+        c.hi[tok] = hi;
+        c.lo[tok] = lo;
+        c.start[tok] = start;
+        c.in[tok] = first * iscale;
+        c.up[tok] = last * uscale;
+        if (l == 63) c.a = start < 0 ? first : -1.0f;
+    } else {
+        const uint64_t starts = __builtin_bitreverse64(__ballot(cut));      // bit: token
+        const double own = v;
+        const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+        v = __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_before((int)(uint32_t)(bits >> 32)) << 32 |
+                                           (uint32_t)lane_before((int)(uint32_t)bits));
+        int after = lane_before(cut ? 1 : 0) - 1;       // 0: a start among the tokens after it, -1: none
+        scan_lanes(v, after);
+        const float hi = (float)v, lo = (float)(v - (double)hi);
+        const double all = __shfl(v + own, 63);         // of the tokens before the first start
+        const uint64_t upto = starts & (~0ull >> l);    // starts up to the token
+        const float first = upto == 0 ? fast_exp2((float)(all - v)) : 0.0f;
+        c.hi[tok] = -hi;
+        c.lo[tok] = -lo;
+        c.start[tok] = upto ? 63 - __builtin_clzll(upto) : -1;
+        c.in[tok] = after < 0 ? fast_exp2(hi + lo) * iscale : 0.0f;
+        c.up[tok] = first * uscale;
+        if (l == 0) c.a = starts ? -1.0f : first;
+    }
 }
 
 // --------------------------------------------------------------------------------------------
@@ -571,7 +606,7 @@ __global__ __launch_bounds__((walk_threads(VP, kParts)), (walk_waves<T, KC, VP, 
         if constexpr (MODE != kWalkPlain) er.load(tid, at, ep, a.e.rows, (int)L);
     };
     const auto load_td = [&](int chunk) {
-        if (w == coef_wave) td = load_decay(a, b, h, (int64_t)chunk * kC + l);
+        if (w == coef_wave) td = load_decay(a, b, h, (int64_t)chunk * kC + decay_token<REV>(l));
     };
     // the decay's part of a finished chunk, from the waves' sums
     const auto flush_r = [&](int chunk) {
@@ -839,9 +874,9 @@ __global__ __launch_bounds__((walk_threads(VP, walk_parts<T, KC, VP>()))) void w
     if (threadIdx.x == 0) sm.c[0].bad[0] = sm.c[1].bad[0] = 0;
     TokenDecay td{0.0f, 1};
     if (w == 0) {
-        td = load_decay(a, b, h, (int64_t)begin * kC + l);
+        td = load_decay(a, b, h, (int64_t)begin * kC + decay_token<REV>(l));
         chunk_decay<REV>(td, sm.c[0], a.iscale, a.uscale);
-        if (n > 1) td = load_decay(a, b, h, (int64_t)(begin + step) * kC + l);
+        if (n > 1) td = load_decay(a, b, h, (int64_t)(begin + step) * kC + decay_token<REV>(l));
     }
     const int tid = threadIdx.x;
     const auto load = [&](int chunk) {
@@ -866,7 +901,7 @@ __global__ __launch_bounds__((walk_threads(VP, walk_parts<T, KC, VP>()))) void w
                 ChunkDecay& cn = sm.c[(it + 1) & 1];
                 chunk_decay<REV>(td, cn, a.iscale, a.uscale);
                 if (l == 0) cn.bad[0] = 0;
-                if (it + 2 < n) td = load_decay(a, b, h, (int64_t)(chunk + 2 * step) * kC + l);
+                if (it + 2 < n) td = load_decay(a, b, h, (int64_t)(chunk + 2 * step) * kC + decay_token<REV>(l));
             }
         }
         const bool cut = __builtin_amdgcn_readfirstlane(__float_as_int(c.a)) < 0;
