@@ -97,8 +97,8 @@ int packmamba_linear_attention_step(const void* q, const void* k, const void* v,
  *   gate_first:  a = x gate,  out = a rstd weight          rstd = 1 / sqrt(mean over the group of a^2 + eps)
  *   otherwise:   a = x,       out = a rstd weight gate
  *   x, z, out in dtype; weight (dim) float; rstd (batch, groups, seqlen) float, written for the backward.
- *   dim a multiple of groups; eps >= 0; batch * groups at most 2^20, batch * groups * ceil(seqlen / 32) below 2^22
- *   and batch * dim * seqlen at most 2^33.
+ *   dim a multiple of groups, at most 2^27 - 32; eps >= 0; batch * groups at most 2^20, batch * groups *
+ *   ceil(seqlen / 32) below 2^22 and batch * dim * seqlen at most 2^33.
  */
 int packmamba_gated_rmsnorm_fwd(const void* x, const void* z, const float* weight, float eps, void* out, float* rstd,
                                 int64_t batch, int64_t dim, int64_t seqlen, int64_t groups, int32_t gate_first,

@@ -12,6 +12,8 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxRows = (int64_t)1 << 21;      // (batch, head) pairs: a block of up to 1024 threads each, 2^32 in all
 constexpr int64_t kMaxNormTiles = ((int64_t)1 << 22) - 1;   // tiles of 32 tokens, a block each
+// features: counted in 32 bits with strides of some thousands; dweight's sum takes 32 threads each, 2^32 in all
+constexpr int64_t kMaxNormDim = ((int64_t)1 << 27) - 32;
 constexpr int64_t kMaxSeqlen = (int64_t)1 << 22;    // 64 rows of it in fp32 are an offset of 32 bits in the walks
 constexpr int64_t kMaxElems = (int64_t)1 << 33;     // of a tensor, heads' copies of q and k included
 
@@ -69,7 +71,7 @@ BwdWs bwd_ws(const pm::LinPlan& p, int64_t batch, int64_t heads, int64_t groups,
 int check_norm(int64_t batch, int64_t dim, int64_t seqlen, int64_t groups) {
     if (batch <= 0 || dim <= 0 || seqlen <= 0 || groups <= 0 || dim % groups) return PACKMAMBA_ERR_SHAPE;
     if (groups > (1 << 20) || batch > (1 << 20) / groups) return PACKMAMBA_ERR_SHAPE;
-    if (dim > INT32_MAX || seqlen > INT32_MAX / 2) return PACKMAMBA_ERR_SHAPE;
+    if (dim > kMaxNormDim || seqlen > INT32_MAX / 2) return PACKMAMBA_ERR_SHAPE;
     if (batch * dim > kMaxElems / seqlen) return PACKMAMBA_ERR_SHAPE;
     if (batch * groups > kMaxNormTiles / ((seqlen + 31) / 32)) return PACKMAMBA_ERR_SHAPE;
     return PACKMAMBA_OK;
