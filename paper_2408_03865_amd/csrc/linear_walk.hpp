@@ -248,7 +248,14 @@ __device__ __forceinline__ void scan_lanes(double& v, int& start) {
 // The chunk's token whose decay a lane loads: the sums run over the lanes.
 template <bool REV>
 __device__ __forceinline__ int decay_token(int l) {
-    return REV ? kC - 1 - l : l;
+    return REV ? kC - 1 - here(l) : l;      // computed anew: kept over the loop it is a register too many
+}
+
+// The value of one lane, in all.
+__device__ __forceinline__ double uniform(double v, int lane) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(bits >> 32), lane) << 32 |
+                                          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)bits, lane));
 }
 
 // The value of the lane before, 0 in lane 0.
@@ -279,19 +286,19 @@ __device__ __forceinline__ void chunk_decay(const TokenDecay& d, ChunkDecay& c, 
         if (l == 63) c.a = start < 0 ? first : -1.0f;
     } else {
         const uint64_t starts = __builtin_bitreverse64(__ballot(cut));      // bit: token
-        const double own = v;
         const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+        const double own = uniform(v, 63);
         v = __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_before((int)(uint32_t)(bits >> 32)) << 32 |
                                            (uint32_t)lane_before((int)(uint32_t)bits));
         int after = lane_before(cut ? 1 : 0) - 1;       // 0: a start among the tokens after it, -1: none
         scan_lanes(v, after);
         const float hi = (float)v, lo = (float)(v - (double)hi);
-        const double all = __shfl(v + own, 63);         // of the tokens before the first start
-        const uint64_t upto = starts & (~0ull >> l);    // starts up to the token
+        const double all = own + uniform(v, 63);        // of the tokens before the first start
+        const uint64_t upto = starts << here(l);        // bit 63: the token
         const float first = upto == 0 ? fast_exp2((float)(all - v)) : 0.0f;
         c.hi[tok] = -hi;
         c.lo[tok] = -lo;
-        c.start[tok] = upto ? 63 - __builtin_clzll(upto) : -1;
+        c.start[tok] = upto ? tok - __builtin_clzll(upto) : -1;
         c.in[tok] = after < 0 ? fast_exp2(hi + lo) * iscale : 0.0f;
         c.up[tok] = first * uscale;
         if (l == 0) c.a = starts ? -1.0f : first;
