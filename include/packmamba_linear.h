@@ -26,7 +26,9 @@
  * products inside a chunk of 64 tokens (q . k, weighted) and the copy of the state that q is
  * multiplied with are rounded to bf16 once, also where PACKMAMBA_BF16_F32OUT returns 32 bits: out
  * has bf16's accuracy in both.  Final states, the initial state's gradient and the decays' gradient
- * have 32-bit accuracy for all types.  Results are bitwise reproducible.
+ * have 32-bit accuracy for all types.  The same call gives the same bits; with another choice of the
+ * optional outputs (final states, ddecay) other kernels may run, and bf16 results may differ within
+ * their accuracy.
  * An infinity or NaN at token t reaches no other sequence, and in its own only what the sums hold it in:
  *   q: out at t; dk, dv up to t          k: out, dq from t on; dv at t     v: out, dq from t on; dk at t
  *   dout: dq at t; dk, dv up to t        decay of t: out, dq from t on; dk, dv before t

@@ -64,6 +64,9 @@ inline int64_t walk_bound_floats(int32_t x_rows, int32_t z_rows) {
 //   - an aggregate takes 0.45 of a walk; the backward has two for its three walks;
 //   - a block costs three chunks besides its own, the two launches two (forward calls of 4 and 5 chunks: bf16 25 us
 //     for 16 and 18 unsplit, fp32 25 for 32 and 38).
+// These are bf16's numbers, and fp32 rows are split alike: the plan does not look at the type.  fp32 walks hold one
+// block a CU in every form but the plain one of 64 x 64 (85 to 154 KB of LDS), so that 257 to 511 blocks of them are
+// two rounds where it counts one.
 // Us of a bf16 call, dk and dv 64, planned and unsplit (batch x heads x tokens, forward then the whole backward):
 //   4 x 24 x 2048 56, 83; 188, 376   2 x 64 x 4096 (dk 128) 132, 206; 576, 1000   1 x 300 x 4096 222, 220; 1046, 1225
 //   1 x 32 x 16384 103, 623; 398, 2670   1 x 8 x 320 24, 18; 58, 79   1 x 150 x 2048 (dk 128) 105, 108; 471, 565

@@ -27,12 +27,15 @@
 // What bounds it: the waves' own work between three barriers a chunk, none of the units alone.  8 x 64 heads x
 // 4096 tokens, dk 128 and dv 64, bf16, forward: 311 to 345 us on different cards; the VALU issues 57% of the cycles (weights, the splits of S and of
 // weighted z), LDS is read and written in 53% (every wave reads all of x and y for its part of z), the matrix units are
-// busy 19%; 682 MB move at 2.1 TB/s.  8 x 32 heads, 128 and 128: dq 528 us (VALU 68%, LDS 37%, matrix 22%), dk 517, dv 308.
+// busy 19%; 682 MB move at 2.1 TB/s.  8 x 32 heads, 128 and 128, backward 1409 us; of it, in a trace whose kernels are 14%
+// slower, dq 552 (VALU 68%, LDS 36%, matrix 22%), dk 540, dv 325.  In fp32 the matrix units bound them: forward 930 us, busy
+// 65% (VALU 15%, LDS 18%), backward 3392.
 // Longer chunks would do more products inside a chunk, shorter ones split S more often.
 // Rounding in bf16: the weighted products x . y and, in plain walks, the copy of S that is
-// multiplied with x are rounded to bf16 once (each enters bf16 outputs only); what S itself adds is
-// split into two or three bf16 terms that hold 16 or all 24 bits of it, and in the walks that feed
-// the decay's gradient so is the copy of S.
+// multiplied with x are rounded to bf16 once (each enters the out alone, which a bf16 output rounds as
+// much once more; a 32-bit output of bf16 inputs has their accuracy); what S itself adds is split into
+// two or three bf16 terms that hold 16 or all 24 bits of it, and in the walks that feed the decay's
+// gradient so is the copy of S.
 //
 // Infinities and NaN reach the outs whose sums hold them and no other: masks select, a chunk whose y or z
 // holds one takes plain loops over the unmasked pairs in place of the matrix products over tokens, where 0

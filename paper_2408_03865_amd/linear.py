@@ -9,8 +9,9 @@ chunks, and token by token) and the gated RMSNorm after it.
 
 S_t = exp(decay_t) S_{t-1} + k_t v_t^T (nothing of S_{t-1} where position_indices is 0) and
 out_t = scale S_t^T q_t, per batch row and head; q and k are shared by heads / groups heads.
-Tensors are contiguous, on one GPU; what does not fit raises TypeError or ValueError before
-anything is launched.
+Tensors are contiguous, on one GPU; what does not fit raises TypeError, ValueError or, from the
+library's own checks (alignment, limits, the workspace's size), PackMambaError before anything is
+launched.
 """
 from __future__ import annotations
 
