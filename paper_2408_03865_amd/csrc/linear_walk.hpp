@@ -182,7 +182,7 @@ __device__ __forceinline__ float tile_value(const T* tile, int r, int t) {
 // a chunk's decays
 // --------------------------------------------------------------------------------------------
 struct __attribute__((aligned(16))) ChunkDecay {
-    float hi[kC], lo[kC];       // G in log2 units, as a sum of two floats (its differences are what is used)
+    float hi[kC], lo[kC];       // G in log2 units, as a sum of two floats
     float in[kC], up[kC];       // scaled; 0 where the term is left out
     int32_t start[kC];          // the last start up to the token, -1: none in the chunk
     float a;                    // -1: a start in the chunk
@@ -265,9 +265,10 @@ __device__ __forceinline__ double uniform(double v, int lane) {
 __device__ __forceinline__ int lane_before(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x138, 0xf, 0xf, false); }
 
 // One wave, lane l = token decay_token(l).  The sum is kept in 64 bits and starts anew at each start, so that no
-// sequence's decays reach another's.  In a reverse walk G is less the sum of the decays after the token, up to the
-// chunk's or the sequence's end: whichever way the walk goes, a sum that holds an infinite decay or a NaN belongs
-// to a token whose out holds it too, by a pair or by the state, and pairs on its other side do not meet it.
+// sequence's decays reach another's.  In a reverse walk G is minus the sum of the decays after the token, up to the
+// chunk's or the sequence's end (differences of G are the same): whichever way the walk goes, a sum that holds an
+// infinite decay or a NaN belongs to a token whose out holds it too, by a pair or by the state, and pairs on its
+// other side do not meet it.
 template <bool REV>
 __device__ __forceinline__ void chunk_decay(const TokenDecay& d, ChunkDecay& c, float iscale, float uscale) {
     const int l = lane_id(), tok = decay_token<REV>(l);
