@@ -26,6 +26,10 @@ RMSNorm (``include/packmamba_linear.h``) are in ``linear.py``:
     out, state = linear_attention_fwd(q, k, v, decay, position_indices, return_final=True)
     out = linear_attention_step(q, k, v, decay, state)
     y, rstd = gated_rmsnorm_fwd(out, z, weight, groups=heads)
+
+The gated delta rule over packed rows and its single-token form (``include/packmamba_delta.h``) are in ``delta.py``:
+    out, state = delta_rule_fwd(q, k, v, beta, decay, position_indices, return_final=True)
+    out = delta_rule_step(q, k, v, beta, decay, state)
 """
 from __future__ import annotations
 
@@ -41,6 +45,7 @@ __all__ = [
     "pack_positions",
     "rmsnorm_fwd", "rmsnorm_bwd",
     "linear_attention_fwd", "linear_attention_bwd", "linear_attention_step", "gated_rmsnorm_fwd", "gated_rmsnorm_bwd",
+    "delta_rule_fwd", "delta_rule_bwd", "delta_rule_step",
     "padding_rate", "PackMambaError", "load", "F32", "BF16",
     "STATE_STRIDE", "BF16_F32OUT",
 ]
@@ -316,3 +321,4 @@ def padding_rate(pieces, n_rows: int, seqlen: int) -> float:
 
 from .linear import (gated_rmsnorm_bwd, gated_rmsnorm_fwd, linear_attention_bwd, linear_attention_fwd,  # noqa: E402
                      linear_attention_step)
+from .delta import delta_rule_bwd, delta_rule_fwd, delta_rule_step  # noqa: E402

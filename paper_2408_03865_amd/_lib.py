@@ -48,6 +48,15 @@ LINEAR_EXPORTS = {
     "packmamba_gated_rmsnorm_bwd": ("pppppppp" + "ps" + "llll" + "iip", False),
 }
 
+# The same of include/packmamba_delta.h.
+DELTA_EXPORTS = {
+    "packmamba_delta_rule_fwd_workspace_size": ("llllll", True),
+    "packmamba_delta_rule_fwd": ("pppppppfppps" + "llllll" + "iip", False),
+    "packmamba_delta_rule_bwd_workspace_size": ("lllllli", True),
+    "packmamba_delta_rule_bwd": ("pppppppf" + "pppppppp" + "ps" + "llllll" + "iip", False),
+    "packmamba_delta_rule_step": ("pppppppfp" + "lllll" + "iip", False),
+}
+
 PACK_SEQUENTIAL, PACK_GREEDY, PACK_CUT = 0, 1, 2
 
 
@@ -116,7 +125,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
                  "packmamba_check_position_indices", "packmamba_rmsnorm_fwd", "packmamba_rmsnorm_bwd"):
         getattr(lib, name).restype = ctypes.c_int
     kinds = {"p": vp, "s": sz, "l": i64, "i": i32, "f": ctypes.c_float}
-    for name, (args, size) in LINEAR_EXPORTS.items():
+    for name, (args, size) in {**LINEAR_EXPORTS, **DELTA_EXPORTS}.items():
         fn = getattr(lib, name, None)        # a build of the other header's host layer alone lacks them
         if fn is not None:
             fn.argtypes = [kinds[c] for c in args]

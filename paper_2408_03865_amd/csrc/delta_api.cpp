@@ -1,0 +1,264 @@
+// delta_api.cpp -- the C ABI of packmamba_delta.h: argument validation (before anything is
+// enqueued), workspace layout and the order of the launches.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "delta.hpp"
+#include "packmamba_delta.h"
+
+namespace {
+
+constexpr size_t kAlign = 256;
+constexpr int64_t kMaxSeqlen = (int64_t)1 << 22;    // 64 rows of it in fp32 are an offset of 32 bits in the walks
+constexpr int64_t kMaxUnits = (int64_t)1 << 20;     // chunks of all rows and heads: up to 180 KB of workspace each
+
+inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+inline size_t floats(int64_t n) { return align_up(sizeof(float) * (size_t)n); }
+inline int launch_status(hipError_t e) { return e == hipSuccess ? PACKMAMBA_OK : PACKMAMBA_ERR_LAUNCH; }
+
+template <typename... P>
+bool aligned16(P... p) {
+    return ((((uintptr_t)p & 15u) == 0) && ...);
+}
+
+int check_dtype(int32_t dtype) {
+    return (dtype == PACKMAMBA_F32 || dtype == PACKMAMBA_BF16 || dtype == PACKMAMBA_BF16_F32OUT) ? PACKMAMBA_OK
+                                                                                                 : PACKMAMBA_ERR_UNSUPPORTED;
+}
+
+int check_heads(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv, int64_t seqlen) {
+    if (batch <= 0 || heads <= 0 || groups <= 0 || dk <= 0 || dv <= 0 || seqlen <= 0) return PACKMAMBA_ERR_SHAPE;
+    if (heads > kMaxUnits || batch > kMaxUnits / heads || heads % groups) return PACKMAMBA_ERR_SHAPE;
+    if (dk > PACKMAMBA_DELTA_MAX_HEAD || dv > PACKMAMBA_DELTA_MAX_HEAD) return PACKMAMBA_ERR_UNSUPPORTED;
+    if (seqlen > kMaxSeqlen || (seqlen + pm::kLinChunk - 1) / pm::kLinChunk > kMaxUnits / (batch * heads)) return PACKMAMBA_ERR_SHAPE;
+    return PACKMAMBA_OK;
+}
+
+// Split of the rows into segments of whole chunks, each walked by its own block.
+struct Plan {
+    int64_t chunks, units;
+    int32_t nseg, seg_chunks, nb, heads_per, grad_per, grad_parts;
+};
+constexpr int32_t kBoundChunks = 8;     // chunks between the boundaries at which the backward multiplies the two states
+constexpr int64_t kSplitChunks = 16;    // rows of fewer are walked whole
+
+// heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks
+int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
+    int64_t per = rep;
+    while (per > 1 && blocks * ((rep + per - 1) / per) < target) per = (per + 1) / 2;
+    return (int32_t)per;
+}
+
+Plan make_plan(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv, int64_t seqlen) {
+    Plan p;
+    p.chunks = (seqlen + pm::kLinChunk - 1) / pm::kLinChunk;
+    const int64_t rows = batch * heads, slots = dv <= 64 ? 512 : 256;
+    p.units = rows * p.chunks;
+    int64_t per = p.chunks;
+    if (p.chunks >= kSplitChunks && rows * 4 <= slots) {
+        const int64_t n = slots / rows, least = kSplitChunks / 2;
+        per = (p.chunks + n - 1) / n;
+        if (per < least) per = least;
+    }
+    p.seg_chunks = (int32_t)per;
+    p.nseg = (int32_t)((p.chunks + per - 1) / per);
+    p.nb = (int32_t)((p.chunks + kBoundChunks - 1) / kBoundChunks);
+    const int64_t rep = heads / groups, blocks = batch * p.chunks * groups;
+    p.heads_per = heads_for(blocks, rep, 1024);
+    p.grad_per = heads_for(blocks * (dk <= 64 ? 1 : 2), rep, 256);
+    p.grad_parts = (int32_t)((rep + p.grad_per - 1) / p.grad_per);
+    return p;
+}
+
+// Hands out pieces of the workspace, or with none sums them up.
+struct Taker {
+    char* base;
+    size_t at = 0;
+    void* take(size_t bytes) {
+        void* got = base ? base + at : nullptr;
+        at += align_up(bytes);
+        return got;
+    }
+    float* floats(int64_t n) { return static_cast<float*>(take(sizeof(float) * (size_t)n)); }
+};
+
+void take_common(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t rows, int64_t dk, int64_t dv, bool backward) {
+    for (int i = 0; i < (backward ? 2 : 1); ++i) {
+        a.h[i] = t.floats(p.units * pm::kDeltaProduct);
+        a.p[i] = t.floats(p.units * pm::kDeltaProduct);
+    }
+    a.coef = t.floats(p.units * pm::kDeltaCoef);
+    if (p.nseg > 1) {
+        const int64_t pad = pm::delta_pad((int32_t)dk);
+        a.seg = t.floats(rows * p.nseg * dk * dv);
+        a.seg_m = t.floats(rows * p.nseg * pad * pad);
+        a.seg_cut = static_cast<int32_t*>(t.take(sizeof(int32_t) * (size_t)(rows * p.nseg)));
+    }
+}
+
+struct BwdExtra {
+    float *pieces, *dq, *dk;
+};
+BwdExtra take_bwd(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
+                  int64_t seqlen, int32_t dtype) {
+    const int64_t rows = batch * heads, state = (int64_t)pm::delta_pad((int32_t)dk) * pm::delta_pad((int32_t)dv);
+    const size_t size = dtype == PACKMAMBA_F32 ? 4 : 2;
+    take_common(t, a, p, rows, dk, dv, true);
+    a.states = t.take(size * (size_t)(p.units * state));
+    a.grads = t.take(size * (size_t)(p.units * state));
+    a.bound = t.floats(rows * p.nb * state);
+    a.dot = t.floats(rows * (p.nb + 1));
+    a.u = t.take(size * (size_t)(rows * dv * seqlen));
+    a.w = dtype == PACKMAMBA_BF16_F32OUT ? t.take(size * (size_t)(rows * dv * seqlen)) : nullptr;
+    a.e = t.floats(p.units * pm::kLinChunk * pm::delta_pad((int32_t)dv));
+    a.rq = t.floats(rows * seqlen);
+    a.rk = t.floats(rows * seqlen);
+    BwdExtra x{};
+    x.pieces = t.floats(rows * p.nb);
+    if (p.grad_parts > 1) {
+        x.dq = t.floats(batch * groups * p.grad_parts * dk * seqlen);
+        x.dk = t.floats(batch * groups * p.grad_parts * dk * seqlen);
+    }
+    return x;
+}
+
+void set_plan(pm::DeltaArgs& a, const Plan& p) {
+    a.chunks = (int32_t)p.chunks;
+    a.nseg = p.nseg;
+    a.seg_chunks = p.seg_chunks;
+    a.bound_chunks = kBoundChunks;
+    a.nb = p.nb;
+    a.heads_per = p.heads_per;
+    a.grad_per = p.grad_per;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t packmamba_delta_rule_fwd_workspace_size(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
+                                               int64_t seqlen) {
+    if (check_heads(batch, heads, groups, dk, dv, seqlen)) return 0;
+    Taker t{nullptr};
+    pm::DeltaArgs a{};
+    take_common(t, a, make_plan(batch, heads, groups, dk, dv, seqlen), batch * heads, dk, dv, false);
+    return t.at;
+}
+
+int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const float* beta, const float* decay,
+                             const int32_t* position_indices, const float* initial_state, float scale, void* out,
+                             float* final_state, void* workspace, size_t workspace_bytes, int64_t batch, int64_t heads,
+                             int64_t groups, int64_t dk, int64_t dv, int64_t seqlen, int32_t decay_per_token,
+                             int32_t dtype, void* stream) {
+    if (!q || !k || !v || !beta || !position_indices || !out) return PACKMAMBA_ERR_NULL;
+    if (int e = check_heads(batch, heads, groups, dk, dv, seqlen)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!aligned16(q, k, v, beta, decay, position_indices, initial_state, out, final_state, workspace)) return PACKMAMBA_ERR_ALIGN;
+    const Plan p = make_plan(batch, heads, groups, dk, dv, seqlen);
+    Taker t{static_cast<char*>(workspace)};
+    pm::DeltaArgs a{};
+    take_common(t, a, p, batch * heads, dk, dv, false);
+    if (!workspace || workspace_bytes < t.at) return PACKMAMBA_ERR_WORKSPACE;
+    a.q = q; a.k = k; a.v = v; a.beta = beta; a.decay = decay; a.pos = position_indices;
+    a.entry = initial_state; a.leave = final_state; a.out = out; a.scale = scale;
+    a.seqlen = seqlen; a.batch = (int32_t)batch; a.heads = (int32_t)heads; a.groups = (int32_t)groups;
+    a.dk = (int32_t)dk; a.dv = (int32_t)dv; a.dtype = dtype;
+    a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
+    set_plan(a, p);
+    a.sum_segs = p.nseg - 1;
+    const hipStream_t s = (hipStream_t)stream;
+    if (int e = launch_status(pm::launch_delta_prep(a, false, s))) return e;
+    if (p.nseg > 1)
+        if (int e = launch_status(pm::launch_delta_segments(a, false, s))) return e;
+    return launch_status(pm::launch_delta_fwd(a, final_state != nullptr, s));
+}
+
+size_t packmamba_delta_rule_bwd_workspace_size(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
+                                               int64_t seqlen, int32_t dtype) {
+    if (check_heads(batch, heads, groups, dk, dv, seqlen) || check_dtype(dtype)) return 0;
+    Taker t{nullptr};
+    pm::DeltaArgs a{};
+    take_bwd(t, a, make_plan(batch, heads, groups, dk, dv, seqlen), batch, heads, groups, dk, dv, seqlen, dtype);
+    return t.at;
+}
+
+int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const float* beta, const float* decay,
+                             const int32_t* position_indices, const float* initial_state, float scale, const void* dout,
+                             const float* dfinal_state, void* dq, void* dk, void* dv, float* dbeta, float* ddecay,
+                             float* dinitial_state, void* workspace, size_t workspace_bytes, int64_t batch,
+                             int64_t heads, int64_t groups, int64_t dk_size, int64_t dv_size, int64_t seqlen,
+                             int32_t decay_per_token, int32_t dtype, void* stream) {
+    if (!q || !k || !v || !beta || !position_indices || !dout || !dq || !dk || !dv || !dbeta) return PACKMAMBA_ERR_NULL;
+    if (ddecay && !decay) return PACKMAMBA_ERR_NULL;
+    if ((initial_state == nullptr) != (dinitial_state == nullptr)) return PACKMAMBA_ERR_NULL;
+    if (int e = check_heads(batch, heads, groups, dk_size, dv_size, seqlen)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!aligned16(q, k, v, beta, decay, position_indices, initial_state, dout, dfinal_state) ||
+        !aligned16(dq, dk, dv, dbeta, ddecay, dinitial_state, workspace))
+        return PACKMAMBA_ERR_ALIGN;
+    const Plan p = make_plan(batch, heads, groups, dk_size, dv_size, seqlen);
+    Taker t{static_cast<char*>(workspace)};
+    pm::DeltaArgs a{};
+    const BwdExtra x = take_bwd(t, a, p, batch, heads, groups, dk_size, dv_size, seqlen, dtype);
+    if (!workspace || workspace_bytes < t.at) return PACKMAMBA_ERR_WORKSPACE;
+    a.q = q; a.k = k; a.v = v; a.dout = dout; a.beta = beta; a.decay = decay; a.pos = position_indices;
+    a.scale = scale; a.dbeta = dbeta;
+    a.seqlen = seqlen; a.batch = (int32_t)batch; a.heads = (int32_t)heads; a.groups = (int32_t)groups;
+    a.dk = (int32_t)dk_size; a.dv = (int32_t)dv_size; a.dtype = dtype;
+    a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
+    a.bound_end = dfinal_state != nullptr;
+    set_plan(a, p);
+    a.sum_segs = p.nseg;                // the reverse walk takes the last segment's multiplier too
+    const hipStream_t s = (hipStream_t)stream;
+    if (int e = launch_status(pm::launch_delta_prep(a, true, s))) return e;
+    a.entry = initial_state;
+    if (p.nseg > 1)
+        if (int e = launch_status(pm::launch_delta_segments(a, false, s))) return e;
+    if (int e = launch_status(pm::launch_delta_states(a, s))) return e;
+
+    a.entry = dfinal_state;
+    a.leave = dinitial_state;
+    a.out = dv;
+    if (p.nseg > 1)
+        if (int e = launch_status(pm::launch_delta_segments(a, true, s))) return e;
+    if (int e = launch_status(pm::launch_delta_rev(a, s))) return e;
+
+    if (!a.w) a.w = dv;
+    const bool pieces = p.grad_parts > 1;
+    a.dq = pieces ? x.dq : dq;
+    a.dk_out = pieces ? x.dk : dk;
+    if (int e = launch_status(pm::launch_delta_grads(a, pieces || dtype != PACKMAMBA_BF16, s))) return e;
+    if (pieces) {
+        const int32_t of = (int32_t)groups * p.grad_parts;
+        for (int i = 0; i < 2; ++i)
+            if (int e = launch_status(pm::launch_linear_group_sum(i ? x.dk : x.dq, i ? dk : dq, batch, of, (int32_t)groups,
+                                                                  dk_size * seqlen, dtype != PACKMAMBA_BF16, s)))
+                return e;
+    }
+    if (!ddecay) return PACKMAMBA_OK;
+    pm::LinDecayArgs d{};
+    d.rq = a.rq; d.rk = a.rk; d.dot = a.dot; d.decay = decay; d.pos = position_indices; d.ddecay = ddecay; d.partial = x.pieces;
+    d.seqlen = seqlen; d.batch = a.batch; d.heads = a.heads; d.decay_mode = a.decay_mode;
+    d.bound_tokens = kBoundChunks * (int32_t)pm::kLinChunk; d.nb = p.nb; d.bound_end = a.bound_end;
+    return launch_status(pm::launch_linear_ddecay(d, s));
+}
+
+int packmamba_delta_rule_step(const void* q, const void* k, const void* v, const float* beta, const float* decay,
+                              const int32_t* position_indices, float* state, float scale, void* out, int64_t batch,
+                              int64_t heads, int64_t groups, int64_t dk, int64_t dv, int32_t decay_per_token,
+                              int32_t dtype, void* stream) {
+    if (!q || !k || !v || !beta || !state || !out) return PACKMAMBA_ERR_NULL;
+    if (int e = check_heads(batch, heads, groups, dk, dv, 1)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!aligned16(q, k, v, beta, decay, position_indices, state, out)) return PACKMAMBA_ERR_ALIGN;
+    pm::DeltaStepArgs a{};
+    a.q = q; a.k = k; a.v = v; a.beta = beta; a.decay = decay; a.pos = position_indices; a.state = state; a.out = out; a.scale = scale;
+    a.batch = (int32_t)batch; a.heads = (int32_t)heads; a.groups = (int32_t)groups;
+    a.dk = (int32_t)dk; a.dv = (int32_t)dv;
+    a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
+    a.dtype = dtype;
+    return launch_status(pm::launch_delta_step(a, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,741 @@
+// delta_walk.hpp -- the walks of the gated delta rule over the chunks of a row.
+//
+// For every head, with S' = a_t S_{t-1} (a_t = exp(g_t), 0 at a sequence start):
+//   e_t = v_t - S'^T k_t,  u_t = beta_t e_t,  S_t = S' + k_t u_t^T,  out_t = scale S_t^T q_t.
+// In chunks of 64 tokens, with what delta_prep.hip made of the keys and queries (H, P) and the weights in, up
+// and A of linear_walk.hpp:
+//   x = v - in (K^T S),  e = x - H (beta x),  u = beta e
+//   out = scale in (Q^T S) + P u,      S <- A S + K (up u)
+// and backwards in time, D the gradient of the state that leaves the chunk, dx_t that of u_t:
+//   x = up (K^T D) + P^T dout,  du = x - H^T (beta x),  dv = beta du
+//   D <- A D + scale Q (in dout) - K (in dv)
+// The gradients of beta are du . e, those of the log decays sums of out . dout - v . dv over the tokens that
+// follow in the sequence, up to a boundary, plus the product of S and D there: with F the gradient of S',
+// dg_t = <F_t, S'_t> = <D_t, S_t> - v_t . dv_t (S_t - beta_t k_t v_t^T is linear in a_t), and the <D, S> of
+// the token before is dg_t + out . dout there.
+//
+// Mapping.  The columns of S (v's features) need nothing of each other: each wave owns 16 of them and all of
+// k's features, in registers, in the layout that an MFMA result has and, four rows of it a lane, an MFMA operand
+// takes.  So do x, e, u and the outs: four consecutive tokens of a feature a lane.  A block's waves share the chunk's
+// K, Q, H and P in LDS, which the next chunk's loads pass through registers.
+// Rounding in bf16: operands that the state holds are split into two or three bf16 terms (16 or all 24 bits), H
+// and P too where they meet them; a plain forward rounds P, its u and the S that q meets to bf16 once.
+//
+// Infinities and NaN: masks select.  A chunk whose k or q holds one, or whose u a wave finds it in, is walked by that
+// wave token by token from the definition, so that 0 times it reaches no other token or sequence.
+#pragma once
+
+#include "linear_walk.hpp"
+#include "delta.hpp"
+
+namespace pm {
+
+enum DeltaMode : int { kDeltaOut = 0, kDeltaSum = 1, kDeltaStates = 2 };
+
+template <typename T, int KC, int VP, int NH, int NP, bool Q, int DOTS>
+struct DeltaSmem {
+    using Frag = typename Mat<T>::Frag;
+    __attribute__((aligned(16))) T k[KC * kC];
+    __attribute__((aligned(16))) T q[Q ? KC * kC : 8];
+    Frag h[NH][kDeltaTiles][64];
+    Frag p[NP ? NP : 1][NP ? kDeltaTiles : 1][64];
+    __attribute__((aligned(16))) float coef[3][kC];
+    __attribute__((aligned(16))) float misc[4];
+    __attribute__((aligned(16))) float dot[DOTS ? DOTS : 1][VP / 16][kC];
+    float xdot[VP / 16];
+};
+
+__host__ __device__ constexpr int delta_tile(int i, int j) { return i * (i + 1) / 2 + j; }
+
+// A prepared product on its way into LDS.
+template <typename T, int N, int THREADS>
+struct ProductRegs {
+    using M = Mat<T>;
+    static constexpr int kVecs = kDeltaTiles * 64, kPasses = (kVecs + THREADS - 1) / THREADS;
+    f32x4 w[kPasses];
+    __device__ void load(int tid, const float* p) {
+        const f32x4* v = reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) w[i] = v[min(i * THREADS + tid, kVecs - 1)];
+    }
+    __device__ void store(int tid, typename M::Frag (*to)[kDeltaTiles][64]) const {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int at = i * THREADS + tid;
+            if (at >= kVecs) continue;
+            typename M::Frag f[N];
+            M::template split<N>(w[i], f);
+#pragma unroll
+            for (int n = 0; n < N; ++n) to[n][0][at] = f[n];
+        }
+    }
+};
+
+// Four consecutive tokens of one feature's row at a time, for the four tiles of a chunk: what a lane's result
+// registers hold of it.
+template <typename T>
+struct TokenRegs {
+    using Raw = std::conditional_t<sizeof(T) == 2, u32x2, u32x4>;
+    Raw w[4];
+    // p: the feature's row, t0: the chunk's first token, g4: the lane's first in a tile
+    __device__ void load(const T* p, int64_t t0, int g4, int64_t L) {
+        if (t0 + kC <= L) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = load_vec<T, 4>(p + t0 + i * 16 + g4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t t = t0 + i * 16 + g4 + r;
+                    v[r] = t < L ? Storage<T>::load1(p + t) : 0.0f;
+                }
+                w[i] = pack(v);
+            }
+        }
+    }
+    __device__ static Raw pack(const float* v) {
+        if constexpr (sizeof(T) == 2) return Raw{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else return Raw{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+    __device__ f32x4 get(int i) const { return Mat<T>::widen(__builtin_bit_cast(typename Mat<T>::Frag, w[i])); }
+};
+
+// v at four consecutive tokens t.. of a row
+template <typename TO>
+__device__ __forceinline__ void store_tokens(TO* row, int64_t t, int64_t L, const f32x4& v) {
+    if (t + 4 <= L) {
+        if constexpr (sizeof(TO) == 2) *reinterpret_cast<u32x2_a2*>(row + t) = Mat<bf16_t>::round(v);
+        else *reinterpret_cast<u32x4_a4*>(row + t) = __builtin_bit_cast(u32x4, v);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (t + r < L) Storage<TO>::store1(row + t + r, v[r]);
+    }
+}
+
+// The state: rows 16 k + 4 (lane / 16) .. + 3, column lane % 16 of the wave's 16.
+template <int KF>
+struct DeltaState {
+    f32x4 s[KF];
+    template <typename F>
+    __device__ void each(F f) {
+        const int l = here(lane_id());
+#pragma unroll
+        for (int k = 0; k < KF; ++k) f(k * 16 + (l >> 4) * 4, l & 15, s[k]);
+    }
+    // rows x cols, row-major with `stride`; zf: the wave's first column
+    __device__ void load(const float* p, int rows, int cols, int zf, int stride) {
+        each([&](int x, int z, f32x4& v) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = p && x + r < rows && zf + z < cols ? p[(int64_t)(x + r) * stride + zf + z] : 0.0f;
+        });
+    }
+    __device__ void store(float* p, int rows, int cols, int zf, int stride) {
+        each([&](int x, int z, f32x4& v) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (x + r < rows && zf + z < cols) p[(int64_t)(x + r) * stride + zf + z] = v[r];
+        });
+    }
+    // columns of the identity from zf on
+    __device__ void identity(int zf) {
+        each([&](int x, int z, f32x4& v) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = x + r == zf + z ? 1.0f : 0.0f;
+        });
+    }
+    __device__ void decay(bool cut, float a) {
+#pragma unroll
+        for (int k = 0; k < KF; ++k) s[k] = cut ? f32x4{0, 0, 0, 0} : s[k] * a;
+    }
+    // transposed, rounded to T: column z is a row of KF * 16
+    template <typename T>
+    __device__ void keep(T* p, int zf) {
+        each([&](int x, int z, f32x4& v) {
+            T* to = p + (int64_t)(zf + z) * (KF * 16) + x;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = Mat<T>::round(v);
+            else *reinterpret_cast<f32x4*>(to) = v;
+        });
+    }
+    // one token, of which column f of a tile is the key's or query's: sum over the rows of it times the column
+    template <typename T>
+    __device__ float against(const T* tile, int j) {
+        const int l = here(lane_id());
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v = fmaf(tile_value(tile + k * 16 * kC, (l >> 4) * 4 + r, j), s[k][r], v);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+        return v;
+    }
+    template <typename T>
+    __device__ void add(const T* tile, int j, float f) {
+        const int l = here(lane_id());
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[k][r] = fmaf(tile_value(tile + k * 16 * kC, (l >> 4) * 4 + r, j), f, s[k][r]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+// c + the terms' products, of operands split into NA and NB terms; those below the last term's size are left out.
+template <typename T, int NA, int NB>
+__device__ __forceinline__ f32x4 mma_terms(const typename Mat<T>::Frag (&a0)[NA], const typename Mat<T>::Frag (&a1)[NA],
+                                           const typename Mat<T>::Frag (&b0)[NB], const typename Mat<T>::Frag (&b1)[NB], f32x4 c) {
+    constexpr int kMost = NA > NB ? NA : NB;
+#pragma unroll
+    for (int n = kMost - 1; n >= 0; --n)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = n - i;
+            if (j >= 0 && j < NB) c = Mat<T>::mma(a0[i], a1[i], b0[j], b1[j], c);
+        }
+    return c;
+}
+
+// acc[i] (token tile i) += product tiles (i, j) times y[j], over j <= i, or with REV over j >= i of the turned tiles
+template <typename T, bool REV, int NA, int NB>
+__device__ __forceinline__ void multiply_product(int l, const typename Mat<T>::Frag (*tiles)[kDeltaTiles][64],
+                                                 const typename Mat<T>::Frag (&y)[4][NB], f32x4 (&acc)[4]) {
+    using Frag = typename Mat<T>::Frag;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int jp = 0; jp < 2; ++jp) {
+            const auto in = [&](int j) { return REV ? j >= i : j <= i; };
+            const auto at = [&](int j) { return REV ? delta_tile(j, i) : delta_tile(i, j); };
+            if (!in(2 * jp) && !in(2 * jp + 1)) continue;
+            Frag a0[NA], a1[NA];
+#pragma unroll
+            for (int n = 0; n < NA; ++n) {
+                a0[n] = in(2 * jp) ? tiles[n][at(2 * jp)][l] : Frag{};
+                a1[n] = in(2 * jp + 1) ? tiles[n][at(2 * jp + 1)][l] : Frag{};
+            }
+            acc[i] = mma_terms<T, NA, NB>(a0, a1, y[2 * jp], y[2 * jp + 1], acc[i]);
+        }
+}
+
+// S += rows of a tile times w, over the chunk's tokens
+template <typename T, int KF, int NS>
+__device__ __forceinline__ void add_tokens(int l, DeltaState<KF>& S, const T* tile, const typename Mat<T>::Frag (&w)[4][NS]) {
+    using M = Mat<T>;
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+            const typename M::Frag y0 = M::direct(l, tile + k * 16 * kC, 2 * p), y1 = M::direct(l, tile + k * 16 * kC, 2 * p + 1);
+#pragma unroll
+            for (int n = NS - 1; n >= 0; --n) S.s[k] = M::mma(y0, y1, w[2 * p][n], w[2 * p + 1][n], S.s[k]);
+        }
+}
+
+__device__ __forceinline__ bool any_nonfinite(const f32x4 (&v)[4]) {
+    float z = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z = fmaf(v[i][r], 0.0f, z);
+    return __ballot(!(z == 0.0f)) != 0;
+}
+
+// v where the weight is not 0, which a masked infinity or NaN must not pass
+__device__ __forceinline__ f32x4 weighted(const f32x4& v, const f32x4& weight) {
+    f32x4 o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = weight[r] == 0.0f ? 0.0f : v[r] * weight[r];
+    return o;
+}
+
+// the multiplier of the state at one token
+__device__ __forceinline__ float token_decay(const DeltaArgs& a, int64_t b, int64_t h, int64_t t, bool& cut) {
+    float g = 0.0f;
+    int pos = 1;
+    if (t < a.seqlen) {
+        pos = a.pos[b * a.seqlen + t];
+        if (a.decay_mode == 2) g = a.decay[(b * a.heads + h) * a.seqlen + t];
+        else if (a.decay_mode == 1) g = a.decay[h];
+    }
+    cut = pos == 0 || g <= kDecayCut;
+    return cut ? 0.0f : expf(g);
+}
+
+__device__ __forceinline__ float lanes16(float v) {      // the sum over the 16 lanes of a row, in all of them
+    v += __shfl_xor(v, 1);
+    v += __shfl_xor(v, 2);
+    v += __shfl_xor(v, 4);
+    v += __shfl_xor(v, 8);
+    return v;
+}
+
+// --------------------------------------------------------------------------------------------
+// forward in time.  MODE kDeltaOut: the outs; kDeltaSum: a segment's end state from zeros, in further blocks from the
+// identity's columns; kDeltaStates: what the backward needs.
+// --------------------------------------------------------------------------------------------
+template <typename T, typename TO, int KC, int VP, int MODE, int NS>
+__global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
+    using M = Mat<T>;
+    using Frag = typename M::Frag;
+    constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
+    constexpr bool kQ = MODE != kDeltaSum;
+    constexpr int NQ = MODE == kDeltaStates ? NS : 1;       // terms of what the outs are made of
+    __shared__ DeltaSmem<T, KC, VP, NS, kQ ? NQ : 0, kQ, MODE == kDeltaStates ? 1 : 0> sm;
+    const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
+    const int64_t L = a.seqlen;
+    const int mblocks = MODE == kDeltaSum ? (KC + VP - 1) / VP : 0, nseg = MODE == kDeltaSum ? a.sum_segs : a.nseg;
+    const uint32_t id = walk_block((uint32_t)a.batch * a.heads * nseg * (1 + mblocks));
+    const uint32_t rs = id / (uint32_t)(1 + mblocks), mb = id - rs * (1 + mblocks);     // mb: 0 the columns of v, else of the identity
+    const uint32_t row = rs / (uint32_t)nseg, bat = row / (uint32_t)a.heads;
+    const int64_t bh = row, b = bat, h = row - bat * a.heads, seg = rs - row * nseg;
+    const int first = (int)seg * a.seg_chunks, last = min(a.chunks, first + a.seg_chunks) - 1;
+    const T* kp = static_cast<const T*>(a.k) + (b * a.groups + h / (a.heads / a.groups)) * a.dk * L;
+    const T* qp = static_cast<const T*>(a.q) + (b * a.groups + h / (a.heads / a.groups)) * a.dk * L;
+    const int zf = w * 16, z = zf + col;
+    const bool live = mb == 0 && z < a.dv;
+    const int64_t zrow = bh * a.dv + min(z, a.dv - 1);
+    const T* vp = static_cast<const T*>(a.v) + zrow * L;
+    const T* dop = MODE == kDeltaStates ? static_cast<const T*>(a.dout) + zrow * L : nullptr;
+    TO* op = MODE == kDeltaOut ? static_cast<TO*>(a.out) + zrow * L : nullptr;
+    T* up = MODE == kDeltaStates ? static_cast<T*>(a.u) + zrow * L : nullptr;
+    const float* betap = a.beta + bh * L;
+
+    DeltaState<KF> S;
+    const int64_t sz = (int64_t)a.dk * a.dv;
+    if (MODE == kDeltaSum && mb == 0) S.load(nullptr, 0, 0, 0, 0);
+    else if (MODE == kDeltaSum) S.identity((int)(mb - 1) * VP + zf);
+    else S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
+
+    TileRegs<T, KC, kThreads> kr, qr;
+    ProductRegs<T, NS, kThreads> hr;
+    ProductRegs<T, NQ, kThreads> pr;
+    TokenRegs<T> vr, dr;
+    f32x4 cr;
+    const auto load = [&](int chunk) {
+        const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
+        const int64_t unit = bh * a.chunks + chunk;
+        kr.load(tid, at, kp, a.dk, (int)L);
+        if constexpr (kQ) qr.load(tid, at, qp, a.dk, (int)L);
+        hr.load(tid, a.h[0] + unit * kDeltaProduct);
+        if constexpr (kQ) pr.load(tid, a.p[0] + unit * kDeltaProduct);
+        const float* cf = a.coef + unit * kDeltaCoef;
+        cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
+        vr.load(vp, (int64_t)chunk * kC, g4, L);
+        if constexpr (MODE == kDeltaStates) dr.load(dop, (int64_t)chunk * kC, g4, L);
+    };
+    const auto flush = [&](int chunk) {
+        if constexpr (MODE == kDeltaStates) {
+            const int64_t t = (int64_t)chunk * kC + tid;
+            if (tid < kC && t < L) {
+                float v = sm.dot[0][0][tid];
+#pragma unroll
+                for (int n = 1; n < kWaves; ++n) v += sm.dot[0][n][tid];
+                a.rq[bh * L + t] = v;
+            }
+        }
+    };
+    bool all_cut = false;
+    load(first);
+    for (int chunk = first; chunk <= last; ++chunk) {
+        const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
+        __syncthreads();
+        if (MODE == kDeltaStates && chunk > first) flush(chunk - 1);
+        kr.settle(tid, kp, a.dk, ct, L);
+        kr.store(tid, sm.k);
+        if constexpr (kQ) {
+            qr.settle(tid, qp, a.dk, ct, L);
+            qr.store(tid, sm.q);
+            pr.store(tid, sm.p);
+        }
+        hr.store(tid, sm.h);
+        if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
+        f32x4 x[4], dov[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = live ? vr.get(i) : f32x4{0, 0, 0, 0};
+            if constexpr (MODE == kDeltaStates) dov[i] = live ? dr.get(i) : f32x4{0, 0, 0, 0};
+        }
+        __syncthreads();
+        if (chunk < last) load(chunk + 1);
+        const float A = uniform(sm.misc[0]);
+        const bool cut = A < 0.0f;
+        all_cut = all_cut || cut;
+        const bool bad = __builtin_amdgcn_readfirstlane(__float_as_int(sm.misc[1])) != 0;
+        if constexpr (MODE == kDeltaStates) {
+            S.keep(static_cast<T*>(a.states) + unit * KC * VP, zf);
+            if (chunk > 0 && chunk % a.bound_chunks == 0) {
+                float* p = a.bound + ((bh * a.nb + chunk / a.bound_chunks - 1) * KF * kThreads + tid) * 4;
+#pragma unroll
+                for (int k = 0; k < KF; ++k) *reinterpret_cast<f32x4*>(p + k * 4 * kThreads) = S.s[k];
+            }
+        }
+        // K^T S and Q^T S
+        f32x4 ak[4], aq[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ak[i] = aq[i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KF; k += 2) {
+            Frag s0[NS], s1[NS];
+            M::template split<NS>(S.s[k], s0);
+            M::template split<NS>(S.s[k + 1], s1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Frag k0 = M::transposed(l, sm.k + k * 16 * kC, i), k1 = M::transposed(l, sm.k + (k + 1) * 16 * kC, i);
+#pragma unroll
+                for (int n = NS - 1; n >= 0; --n) ak[i] = M::mma(k0, k1, s0[n], s1[n], ak[i]);
+                if constexpr (kQ) {
+                    const Frag q0 = M::transposed(l, sm.q + k * 16 * kC, i), q1 = M::transposed(l, sm.q + (k + 1) * 16 * kC, i);
+                    if constexpr (NQ == 1 && NS > 1) {
+                        aq[i] = M::mma(q0, q1, M::round(S.s[k]), M::round(S.s[k + 1]), aq[i]);
+                    } else {
+#pragma unroll
+                        for (int n = NQ - 1; n >= 0; --n) aq[i] = M::mma(q0, q1, s0[n], s1[n], aq[i]);
+                    }
+                }
+            }
+        }
+        const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4]); };
+        Frag y[4][NS];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] -= weighted(ak[i], four(0, i));
+            M::template split<NS>(x[i] * four(2, i), y[i]);
+        }
+        f32x4 hx[4], u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
+        multiply_product<T, false, NS, NS>(l, sm.h, y, hx);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] -= hx[i];                               // the errors
+            u[i] = x[i] * four(2, i);
+        }
+        if (!bad && !any_nonfinite(u)) {
+            if constexpr (kQ) {
+                Frag uf[4][NQ];
+                f32x4 o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    M::template split<NQ>(u[i], uf[i]);
+                    o[i] = weighted(aq[i], four(0, i)) * a.scale;
+                }
+                multiply_product<T, false, NQ, NQ>(l, sm.p, uf, o);
+                if constexpr (MODE == kDeltaOut) {
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) store_tokens(op, ct + i * 16 + g4, L, o[i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16(o[i] * dov[i]));
+                        if (live) store_tokens(up, ct + i * 16 + g4, L, u[i]);
+                        *reinterpret_cast<f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4) = x[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) M::template split<NS>(u[i] * four(1, i), y[i]);
+            S.decay(cut, A);
+            add_tokens<T, KF, NS>(l, S, sm.k, y);
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < kC; ++j) {
+                const int64_t t = ct + j;
+                bool start;
+                const float mult = token_decay(a, b, h, t, start);
+                S.decay(start, mult);
+                const float beta = t < L ? betap[t] : 0.0f;
+                const float e = (live && t < L ? Storage<T>::load1(vp + t) : 0.0f) - S.against(sm.k, j);
+                const float ut = t < L ? beta * e : 0.0f;
+                S.add(sm.k, j, ut);
+                if constexpr (kQ) {
+                    const float o = S.against(sm.q, j) * a.scale;
+                    const bool mine = g4 == 0 && live && t < L;
+                    if constexpr (MODE == kDeltaOut) {
+                        if (mine) Storage<TO>::store1(op + t, o);
+                    } else {
+                        const float d = lanes16(live && t < L ? o * Storage<T>::load1(dop + t) : 0.0f);
+                        if (l == 0) sm.dot[0][w][j] = d;
+                        if (g4 == 0) {
+                            if (mine) Storage<T>::store1(up + t, ut);
+                            a.e[(((unit * kWaves + w) * 4 + j / 16) * 64 + (j % 16) / 4 * 16 + col) * 4 + j % 4] = t < L ? e : 0.0f;
+                        }
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (MODE == kDeltaStates) {
+        __syncthreads();
+        flush(last);
+        if (last == a.chunks - 1 && a.bound_end) {
+            float* p = a.bound + ((bh * a.nb + a.nb - 1) * KF * kThreads + tid) * 4;
+#pragma unroll
+            for (int k = 0; k < KF; ++k) *reinterpret_cast<f32x4*>(p + k * 4 * kThreads) = S.s[k];
+        }
+    }
+    if constexpr (MODE == kDeltaSum) {
+        if (mb == 0) {
+            S.store(a.seg + (bh * a.nseg + seg) * sz, a.dk, a.dv, zf, a.dv);
+            if (tid == 0) a.seg_cut[bh * a.nseg + seg] = all_cut;
+        } else {
+            S.store(a.seg_m + (bh * a.nseg + seg) * KC * KC, KC, KC, (int)(mb - 1) * VP + zf, KC);
+        }
+    } else if (MODE == kDeltaOut && a.leave && last == a.chunks - 1) {
+        S.store(a.leave + bh * sz, a.dk, a.dv, zf, a.dv);
+    }
+}
+
+// --------------------------------------------------------------------------------------------
+// backwards in time: dv, the gradients that the states after the chunks get, and dbeta's and ddecay's parts; SUM: only
+// the gradient that a segment adds
+// --------------------------------------------------------------------------------------------
+template <typename T, typename TO, int KC, int VP, bool SUM, int NS>
+__global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
+    using M = Mat<T>;
+    using Frag = typename M::Frag;
+    constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
+    __shared__ DeltaSmem<T, KC, VP, NS, NS, true, SUM ? 0 : 2> sm;
+    const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
+    const int64_t L = a.seqlen;
+    const int nseg = SUM ? a.nseg - 1 : a.nseg;             // the first segment adds to nothing
+    const uint32_t id = walk_block((uint32_t)a.batch * a.heads * nseg);
+    const uint32_t row = id / (uint32_t)nseg, bat = row / (uint32_t)a.heads;
+    const int64_t bh = row, b = bat, h = row - bat * a.heads, seg = id - row * nseg + (SUM ? 1 : 0);
+    const int first = (int)seg * a.seg_chunks, last = min(a.chunks, first + a.seg_chunks) - 1;
+    const T* kp = static_cast<const T*>(a.k) + (b * a.groups + h / (a.heads / a.groups)) * a.dk * L;
+    const T* qp = static_cast<const T*>(a.q) + (b * a.groups + h / (a.heads / a.groups)) * a.dk * L;
+    const int zf = w * 16, z = zf + col;
+    const bool live = z < a.dv;
+    const int64_t zrow = bh * a.dv + min(z, a.dv - 1);
+    const T* vp = static_cast<const T*>(a.v) + zrow * L;
+    const T* dop = static_cast<const T*>(a.dout) + zrow * L;
+    TO* op = SUM ? nullptr : static_cast<TO*>(a.out) + zrow * L;
+    T* wp = SUM || !a.w ? nullptr : static_cast<T*>(a.w) + zrow * L;      // a copy in T, where the out has another type
+    const float* betap = a.beta + bh * L;
+
+    DeltaState<KF> D;
+    const int64_t sz = (int64_t)a.dk * a.dv;
+    D.load(SUM ? nullptr : a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
+
+    TileRegs<T, KC, kThreads> kr, qr;
+    ProductRegs<T, NS, kThreads> hr, pr;
+    TokenRegs<T> vr, dr;
+    f32x4 cr, er[4];
+    const auto load = [&](int chunk) {
+        const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
+        const int64_t unit = bh * a.chunks + chunk;
+        kr.load(tid, at, kp, a.dk, (int)L);
+        qr.load(tid, at, qp, a.dk, (int)L);
+        hr.load(tid, a.h[1] + unit * kDeltaProduct);
+        pr.load(tid, a.p[1] + unit * kDeltaProduct);
+        const float* cf = a.coef + unit * kDeltaCoef;
+        cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
+        dr.load(dop, (int64_t)chunk * kC, g4, L);
+        if constexpr (!SUM) {
+            vr.load(vp, (int64_t)chunk * kC, g4, L);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) er[i] = *reinterpret_cast<const f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4);
+        }
+    };
+    const auto flush = [&](int chunk) {
+        if constexpr (!SUM) {
+            const int64_t t = (int64_t)chunk * kC + tid;
+            if (tid < kC && t < L) {
+                float v = sm.dot[0][0][tid], d = sm.dot[1][0][tid];
+#pragma unroll
+                for (int n = 1; n < kWaves; ++n) {
+                    v += sm.dot[0][n][tid];
+                    d += sm.dot[1][n][tid];
+                }
+                a.rk[bh * L + t] = -v;
+                a.dbeta[bh * L + t] = d;
+            }
+        }
+    };
+    load(last);
+    for (int chunk = last; chunk >= first; --chunk) {
+        const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
+        __syncthreads();
+        if (!SUM && chunk < last) flush(chunk + 1);
+        kr.settle(tid, kp, a.dk, ct, L);
+        kr.store(tid, sm.k);
+        qr.settle(tid, qp, a.dk, ct, L);
+        qr.store(tid, sm.q);
+        pr.store(tid, sm.p);
+        hr.store(tid, sm.h);
+        if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
+        f32x4 dov[4], vv[4], ev[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            dov[i] = live ? dr.get(i) : f32x4{0, 0, 0, 0};
+            if constexpr (!SUM) {
+                vv[i] = live ? vr.get(i) : f32x4{0, 0, 0, 0};
+                ev[i] = er[i];
+            }
+        }
+        if constexpr (!SUM) {
+            // a boundary at the chunk's end: the product of the state and its gradient there
+            const int next = chunk + 1;
+            if (next < a.chunks ? next % a.bound_chunks == 0 : a.bound_end != 0) {          // block-uniform
+                const int64_t n = (next + a.bound_chunks - 1) / a.bound_chunks;
+                const float* p = a.bound + ((bh * a.nb + n - 1) * KF * kThreads + tid) * 4;
+                float v = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KF; ++k) {
+                    const f32x4 o = *reinterpret_cast<const f32x4*>(p + k * 4 * kThreads);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v = fmaf(o[r], D.s[k][r], v);
+                }
+#pragma unroll
+                for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
+                if (l == 0) sm.xdot[w] = v;
+                __syncthreads();
+                if (tid == 0) {
+                    v = sm.xdot[0];
+#pragma unroll
+                    for (int i = 1; i < kWaves; ++i) v += sm.xdot[i];
+                    a.dot[bh * (a.nb + 1) + n] = v;
+                }
+            }
+            D.keep(static_cast<T*>(a.grads) + unit * KC * VP, zf);
+        }
+        __syncthreads();
+        if (chunk > first) load(chunk - 1);
+        const float A = uniform(sm.misc[0]);
+        const bool cut = A < 0.0f;
+        const bool bad = __builtin_amdgcn_readfirstlane(__float_as_int(sm.misc[1])) != 0;
+        f32x4 ak[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ak[i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KF; k += 2) {
+            Frag s0[NS], s1[NS];
+            M::template split<NS>(D.s[k], s0);
+            M::template split<NS>(D.s[k + 1], s1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Frag k0 = M::transposed(l, sm.k + k * 16 * kC, i), k1 = M::transposed(l, sm.k + (k + 1) * 16 * kC, i);
+#pragma unroll
+                for (int n = NS - 1; n >= 0; --n) ak[i] = M::mma(k0, k1, s0[n], s1[n], ak[i]);
+            }
+        }
+        const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4]); };
+        f32x4 x[4];
+        {
+            Frag df[4][1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                df[i][0] = M::round(dov[i]);             // exact: dout is of this type
+                x[i] = weighted(ak[i], four(1, i));
+            }
+            multiply_product<T, true, NS, 1>(l, sm.p, df, x);
+        }
+        Frag y[4][NS];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) M::template split<NS>(x[i] * four(2, i), y[i]);
+        f32x4 hx[4], dv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
+        multiply_product<T, true, NS, NS>(l, sm.h, y, hx);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] -= hx[i];                               // du
+            dv[i] = x[i] * four(2, i);
+        }
+        if (!bad && !any_nonfinite(x)) {
+            if constexpr (!SUM) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16(vv[i] * dv[i]));
+                    store_sum16(l, &sm.dot[1][w][i * 16 + g4], sum16(x[i] * ev[i]));
+                    if (live) {
+                        store_tokens(op, ct + i * 16 + g4, L, dv[i]);
+                        if (wp) store_tokens(wp, ct + i * 16 + g4, L, dv[i]);
+                    }
+                }
+            }
+            D.decay(cut, A);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) M::template split<NS>(weighted(dov[i], four(0, i)) * a.scale, y[i]);
+            add_tokens<T, KF, NS>(l, D, sm.q, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) M::template split<NS>(-weighted(dv[i], four(0, i)), y[i]);
+            add_tokens<T, KF, NS>(l, D, sm.k, y);
+        } else {
+#pragma unroll 1
+            for (int j = kC - 1; j >= 0; --j) {
+                const int64_t t = ct + j;
+                const bool in = t < L;
+                bool start;
+                const float mult = token_decay(a, b, h, t, start);
+                const float d = in && live ? Storage<T>::load1(dop + t) : 0.0f;
+                D.add(sm.q, j, d * a.scale);
+                const float du = D.against(sm.k, j), dvt = in ? betap[t] * du : 0.0f;
+                if constexpr (!SUM) {
+                    const float et = a.e[(((unit * kWaves + w) * 4 + j / 16) * 64 + (j % 16) / 4 * 16 + col) * 4 + j % 4];
+                    const float vd = lanes16(in && live ? Storage<T>::load1(vp + t) * dvt : 0.0f), db = lanes16(in && live ? du * et : 0.0f);
+                    if (l == 0) {
+                        sm.dot[0][w][j] = vd;
+                        sm.dot[1][w][j] = db;
+                    }
+                    if (g4 == 0 && live && in) {
+                        Storage<TO>::store1(op + t, dvt);
+                        if (wp) Storage<T>::store1(wp + t, dvt);
+                    }
+                }
+                D.add(sm.k, j, -dvt);
+                D.decay(start, mult);
+            }
+        }
+    }
+    if constexpr (!SUM) {
+        __syncthreads();
+        flush(first);
+        if (a.leave && first == 0) D.store(a.leave + bh * sz, a.dk, a.dv, zf, a.dv);
+    } else {
+        D.store(a.seg + (bh * a.nseg + seg) * sz, a.dk, a.dv, zf, a.dv);
+    }
+}
+
+// --------------------------------------------------------------------------------------------
+// launches: one T, TO and KC in each translation unit
+// --------------------------------------------------------------------------------------------
+enum DeltaWalk : int {
+    kWalkOut = 0, kWalkOutExact = 1, kWalkStates = 2, kWalkRev = 3, kWalkSum = 4, kWalkSumRev = 5
+};
+
+template <typename T, typename TO, int KC, int VP>
+hipError_t launch_delta_vp(const DeltaArgs& a, DeltaWalk which, hipStream_t s) {
+    constexpr int kAll = Mat<T>::kSplit ? 3 : 1, kSome = Mat<T>::kSplit ? 2 : 1;
+    const int64_t rows = (int64_t)a.batch * a.heads, mblocks = (KC + VP - 1) / VP;
+    const dim3 block(VP * 4), grid((unsigned)(rows * a.nseg));
+    switch (which) {
+        case kWalkOut: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaOut, kSome>), grid, block, 0, s, a); break;
+        case kWalkOutExact: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaOut, kAll>), grid, block, 0, s, a); break;
+        case kWalkStates: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaStates, kAll>), grid, block, 0, s, a); break;
+        case kWalkRev: hipLaunchKernelGGL((delta_rev_kernel<T, TO, KC, VP, false, kAll>), grid, block, 0, s, a); break;
+        case kWalkSum:
+            hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaSum, kAll>), dim3((unsigned)(rows * a.sum_segs * (1 + mblocks))),
+                               block, 0, s, a);
+            break;
+        case kWalkSumRev:
+            hipLaunchKernelGGL((delta_rev_kernel<T, TO, KC, VP, true, kAll>), dim3((unsigned)(rows * (a.nseg - 1))), block, 0, s, a);
+            break;
+    }
+    return hipGetLastError();
+}
+
+template <typename T, typename TO, int KC>
+hipError_t launch_delta_kc(const DeltaArgs& a, DeltaWalk which, hipStream_t s) {
+    return a.dv <= 64 ? launch_delta_vp<T, TO, KC, 64>(a, which, s) : launch_delta_vp<T, TO, KC, 128>(a, which, s);
+}
+
+}  // namespace pm
