@@ -96,6 +96,42 @@ int packmamba_delta_rule_step(const void* q, const void* k, const void* v, const
                               int64_t heads, int64_t groups, int64_t dk, int64_t dv, int32_t decay_per_token,
                               int32_t dtype, void* stream);
 
+/*
+ * Each head's features divided by their length: the features of (batch, dim, seqlen) form `groups` groups of dim /
+ * groups consecutive ones, and at every token out = x rnorm, rnorm = 1 / sqrt(sum over the group of x^2 + eps).
+ *   x, out in dtype; rnorm (batch, groups, seqlen) float, written for the backward.
+ *   dim a multiple of groups, at most 2^26 - 32; eps >= 0; batch * groups at most 2^20, batch * groups *
+ *   ceil(seqlen / 16) below 2^22 and batch * dim * seqlen at most 2^33.
+ */
+int packmamba_head_l2norm_fwd(const void* x, float eps, void* out, float* rnorm, int64_t batch, int64_t dim,
+                              int64_t seqlen, int64_t groups, int32_t dtype, void* stream);
+
+/* Its backward: dx (the dtype's output type) from x, dout (dtype) and the forward's rnorm. */
+int packmamba_head_l2norm_bwd(const void* x, const float* rnorm, const void* dout, void* dx, int64_t batch, int64_t dim,
+                              int64_t seqlen, int64_t groups, int32_t dtype, void* stream);
+
+/*
+ * Layer norm over the features of (batch, dim, seqlen) activations, at every token:
+ *   out = (x - mean) rstd weight + bias,   rstd = 1 / sqrt(mean of (x - mean)^2 + eps)
+ *   x, out in dtype; weight, bias (dim) float, bias NULL for none; mean, rstd (batch, seqlen) float,
+ *   written for the backward.  Limits as of packmamba_head_l2norm_fwd with one group.
+ */
+int packmamba_layernorm_fwd(const void* x, const float* weight, const float* bias, float eps, void* out, float* mean,
+                            float* rstd, int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype, void* stream);
+
+/* Bytes of workspace packmamba_layernorm_bwd needs with inputs of the dtype. */
+size_t packmamba_layernorm_bwd_workspace_size(int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype);
+
+/*
+ * Its backward: dx (the dtype's output type), dweight (dim) and dbias (dim, or NULL), float, from x, dout (dtype)
+ * and the forward's mean and rstd.  dresidual, if not NULL (dtype), is added to dx.  The sums over tokens are in a fixed
+ * order.
+ */
+int packmamba_layernorm_bwd(const void* x, const float* weight, const float* mean, const float* rstd, const void* dout,
+                            const void* dresidual, void* dx, float* dweight, float* dbias, void* workspace,
+                            size_t workspace_bytes, int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

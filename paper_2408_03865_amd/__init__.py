@@ -27,9 +27,12 @@ RMSNorm (``include/packmamba_linear.h``) are in ``linear.py``:
     out = linear_attention_step(q, k, v, decay, state)
     y, rstd = gated_rmsnorm_fwd(out, z, weight, groups=heads)
 
-The gated delta rule over packed rows and its single-token form (``include/packmamba_delta.h``) are in ``delta.py``:
+The gated delta rule over packed rows, its single-token form (``delta.py``), the norm of its keys and queries and the layer
+norm (``norms.py``; all in ``include/packmamba_delta.h``):
+    k, rnorm = head_l2norm_fwd(k, groups=heads)
     out, state = delta_rule_fwd(q, k, v, beta, decay, position_indices, return_final=True)
     out = delta_rule_step(q, k, v, beta, decay, state)
+    y, mean, rstd = layernorm_fwd(x, weight, bias)
 """
 from __future__ import annotations
 
@@ -45,7 +48,7 @@ __all__ = [
     "pack_positions",
     "rmsnorm_fwd", "rmsnorm_bwd",
     "linear_attention_fwd", "linear_attention_bwd", "linear_attention_step", "gated_rmsnorm_fwd", "gated_rmsnorm_bwd",
-    "delta_rule_fwd", "delta_rule_bwd", "delta_rule_step",
+    "delta_rule_fwd", "delta_rule_bwd", "delta_rule_step", "head_l2norm_fwd", "head_l2norm_bwd", "layernorm_fwd", "layernorm_bwd",
     "padding_rate", "PackMambaError", "load", "F32", "BF16",
     "STATE_STRIDE", "BF16_F32OUT",
 ]
@@ -322,3 +325,4 @@ def padding_rate(pieces, n_rows: int, seqlen: int) -> float:
 from .linear import (gated_rmsnorm_bwd, gated_rmsnorm_fwd, linear_attention_bwd, linear_attention_fwd,  # noqa: E402
                      linear_attention_step)
 from .delta import delta_rule_bwd, delta_rule_fwd, delta_rule_step  # noqa: E402
+from .norms import head_l2norm_bwd, head_l2norm_fwd, layernorm_bwd, layernorm_fwd  # noqa: E402

@@ -55,6 +55,11 @@ DELTA_EXPORTS = {
     "packmamba_delta_rule_bwd_workspace_size": ("lllllli", True),
     "packmamba_delta_rule_bwd": ("pppppppf" + "pppppppp" + "ps" + "llllll" + "iip", False),
     "packmamba_delta_rule_step": ("pppppppfp" + "lllll" + "iip", False),
+    "packmamba_head_l2norm_fwd": ("pfpp" + "llll" + "ip", False),
+    "packmamba_head_l2norm_bwd": ("pppp" + "llll" + "ip", False),
+    "packmamba_layernorm_fwd": ("pppfppp" + "lll" + "ip", False),
+    "packmamba_layernorm_bwd_workspace_size": ("llli", True),
+    "packmamba_layernorm_bwd": ("ppppppppp" + "ps" + "lll" + "ip", False),
 }
 
 PACK_SEQUENTIAL, PACK_GREEDY, PACK_CUT = 0, 1, 2

@@ -17,7 +17,7 @@ OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpackmamba.so")
 SOURCES = ["api.cpp", "pack.cpp", "conv1d.hip", "scan_fwd.hip", "scan_bwd.hip", "check_pos.hip", "rmsnorm.hip",
            "noalloc.hip", "linear_api.cpp", "linear.hip", "linear_step.hip", "gated_norm.hip",
-           "delta_api.cpp", "delta.hip", "delta_prep.hip", "delta_step.hip",
+           "delta_api.cpp", "delta.hip", "delta_prep.hip", "delta_step.hip", "norms.hip",
            *(f"{k}_walk_{t}_{kc}.hip" for k in ("linear", "delta") for t in ("f32", "bf16", "bf16_f32out") for kc in (64, 128))]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

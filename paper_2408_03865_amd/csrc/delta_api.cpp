@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "delta.hpp"
+#include "norms.hpp"
 #include "packmamba_delta.h"
 
 namespace {
@@ -33,6 +34,26 @@ int check_heads(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_
     if (dk > PACKMAMBA_DELTA_MAX_HEAD || dv > PACKMAMBA_DELTA_MAX_HEAD) return PACKMAMBA_ERR_UNSUPPORTED;
     if (seqlen > kMaxSeqlen || (seqlen + pm::kLinChunk - 1) / pm::kLinChunk > kMaxUnits / (batch * heads)) return PACKMAMBA_ERR_SHAPE;
     return PACKMAMBA_OK;
+}
+
+constexpr int64_t kMaxNormRows = (int64_t)1 << 20;
+constexpr int64_t kMaxNormTiles = ((int64_t)1 << 22) - 1;   // tiles of 16 tokens, a block of up to 1024 threads each
+constexpr int64_t kMaxNormDim = ((int64_t)1 << 26) - 32;    // the sums over tokens take 64 threads a feature, 2^32 in all
+constexpr int64_t kMaxElems = (int64_t)1 << 33;
+
+int check_norm(int64_t batch, int64_t dim, int64_t seqlen, int64_t groups) {
+    if (batch <= 0 || dim <= 0 || seqlen <= 0 || groups <= 0 || dim % groups) return PACKMAMBA_ERR_SHAPE;
+    if (groups > kMaxNormRows || batch > kMaxNormRows / groups) return PACKMAMBA_ERR_SHAPE;
+    if (dim > kMaxNormDim || seqlen > INT32_MAX / 2) return PACKMAMBA_ERR_SHAPE;
+    if (batch * dim > kMaxElems / seqlen) return PACKMAMBA_ERR_SHAPE;
+    if (batch * groups > kMaxNormTiles / ((seqlen + 15) / 16)) return PACKMAMBA_ERR_SHAPE;
+    return PACKMAMBA_OK;
+}
+
+pm::NormArgs norm_args(const void* x, int64_t rows, int64_t dim, int64_t seqlen, int32_t dtype) {
+    pm::NormArgs a{};
+    a.x = x; a.rows = rows; a.dim = dim; a.seqlen = seqlen; a.dtype = dtype;
+    return a;
 }
 
 // Split of the rows into segments of whole chunks, each walked by its own block.
@@ -259,6 +280,61 @@ int packmamba_delta_rule_step(const void* q, const void* k, const void* v, const
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     a.dtype = dtype;
     return launch_status(pm::launch_delta_step(a, (hipStream_t)stream));
+}
+
+int packmamba_head_l2norm_fwd(const void* x, float eps, void* out, float* rnorm, int64_t batch, int64_t dim,
+                              int64_t seqlen, int64_t groups, int32_t dtype, void* stream) {
+    if (!x || !out || !rnorm) return PACKMAMBA_ERR_NULL;
+    if (int e = check_norm(batch, dim, seqlen, groups)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!(eps >= 0.0f)) return PACKMAMBA_ERR_SHAPE;
+    if (!aligned16(x, out, rnorm)) return PACKMAMBA_ERR_ALIGN;
+    pm::NormArgs a = norm_args(x, batch * groups, dim / groups, seqlen, dtype);
+    a.eps = eps; a.out = out; a.rstd_out = rnorm;
+    return launch_status(pm::launch_l2norm_fwd(a, (hipStream_t)stream));
+}
+
+int packmamba_head_l2norm_bwd(const void* x, const float* rnorm, const void* dout, void* dx, int64_t batch, int64_t dim,
+                              int64_t seqlen, int64_t groups, int32_t dtype, void* stream) {
+    if (!x || !rnorm || !dout || !dx) return PACKMAMBA_ERR_NULL;
+    if (int e = check_norm(batch, dim, seqlen, groups)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!aligned16(x, rnorm, dout, dx)) return PACKMAMBA_ERR_ALIGN;
+    pm::NormArgs a = norm_args(x, batch * groups, dim / groups, seqlen, dtype);
+    a.rstd = rnorm; a.dout = dout; a.out = dx;
+    return launch_status(pm::launch_l2norm_bwd(a, (hipStream_t)stream));
+}
+
+int packmamba_layernorm_fwd(const void* x, const float* weight, const float* bias, float eps, void* out, float* mean,
+                            float* rstd, int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype, void* stream) {
+    if (!x || !weight || !out || !mean || !rstd) return PACKMAMBA_ERR_NULL;
+    if (int e = check_norm(batch, dim, seqlen, 1)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!(eps >= 0.0f)) return PACKMAMBA_ERR_SHAPE;
+    if (!aligned16(x, weight, bias, out, mean, rstd)) return PACKMAMBA_ERR_ALIGN;
+    pm::NormArgs a = norm_args(x, batch, dim, seqlen, dtype);
+    a.w = weight; a.b = bias; a.eps = eps; a.out = out; a.mean_out = mean; a.rstd_out = rstd;
+    return launch_status(pm::launch_layernorm_fwd(a, (hipStream_t)stream));
+}
+
+size_t packmamba_layernorm_bwd_workspace_size(int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype) {
+    if (check_norm(batch, dim, seqlen, 1) || check_dtype(dtype)) return 0;
+    return floats(pm::norm_tiles(batch, dim, seqlen, dtype == PACKMAMBA_F32) * 2 * dim);
+}
+
+int packmamba_layernorm_bwd(const void* x, const float* weight, const float* mean, const float* rstd, const void* dout,
+                            const void* dresidual, void* dx, float* dweight, float* dbias, void* workspace,
+                            size_t workspace_bytes, int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype,
+                            void* stream) {
+    if (!x || !weight || !mean || !rstd || !dout || !dx || !dweight) return PACKMAMBA_ERR_NULL;
+    if (int e = check_norm(batch, dim, seqlen, 1)) return e;
+    if (int e = check_dtype(dtype)) return e;
+    if (!aligned16(x, weight, mean, rstd, dout, dresidual, dx, dweight, dbias, workspace)) return PACKMAMBA_ERR_ALIGN;
+    if (!workspace || workspace_bytes < packmamba_layernorm_bwd_workspace_size(batch, dim, seqlen, dtype)) return PACKMAMBA_ERR_WORKSPACE;
+    pm::NormArgs a = norm_args(x, batch, dim, seqlen, dtype);
+    a.w = weight; a.mean = mean; a.rstd = rstd; a.dout = dout; a.dres = dresidual; a.out = dx; a.dw = dweight; a.db = dbias;
+    a.partial = static_cast<float*>(workspace);
+    return launch_status(pm::launch_layernorm_bwd(a, (hipStream_t)stream));
 }
 
 }  // extern "C"
