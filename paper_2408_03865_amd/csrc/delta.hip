@@ -111,7 +111,7 @@ struct GradSmem {
 };
 
 template <typename T, typename TO, int KC>
-__global__ __launch_bounds__(256, 2) void delta_grads_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_kernel(DeltaArgs a) {
     using M = Mat<T>;
     using Frag = typename M::Frag;
     using Regs = TileRegs<T, 64, 256>;
@@ -165,7 +165,9 @@ __global__ __launch_bounds__(256, 2) void delta_grads_kernel(DeltaArgs a) {
         cr[1] = a.coef[unit * kDeltaCoef + min(tid + 256, kDeltaCoef - 1)];
     };
     load(0);
-    f32x4 o1[4], o2[4], v1[4], v2[4], sq[4], sk[4], gk[4];
+    // Mo's tiles of the wave's 16 tokens: with the earlier ones (and its own) as rows of dq, with the later ones of dk; the
+    // diagonal tile a second time for dk.  Mv's the same way.
+    f32x4 mo[4], mv[4], mo_d, mv_d;
     for (int step = 0; step < steps; ++step) {
         const bool first = step % vhalves == 0, done = step % vhalves == vhalves - 1;
         const int v0 = step % vhalves * 64, rows = min(64, a.dv - v0);
@@ -182,77 +184,94 @@ __global__ __launch_bounds__(256, 2) void delta_grads_kernel(DeltaArgs a) {
         if (tid + 256 < kDeltaCoef) sm.coef[tid + 256] = cr[1];
         __syncthreads();
         if (step + 1 < steps) load(step + 1);
+        const auto c4 = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which + i * 16 + g4]); };
+        const auto tok = [&](const T* tile, int k, int i) { return M::transposed(l, tile + k * 16 * kC, i); };
         if (first) {
+            mo_d = mv_d = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o1[i] = o2[i] = v1[i] = v2[i] = sq[i] = sk[i] = gk[i] = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < 4; ++i) mo[i] = mv[i] = f32x4{0, 0, 0, 0};
+        }
+        Frag dw[4], uw[4], ww[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            dw[n] = tok(sm.dout, n, w);
+            uw[n] = tok(sm.u, n, w);
+            ww[n] = tok(sm.w, n, w);
         }
 #pragma unroll
-        for (int n = 0; n < 4; n += 2) {                        // 32 features of v
-            const auto tok = [&](const T* tile, int k, int i) { return M::transposed(l, tile + k * 16 * kC, i); };
-            const Frag d0 = tok(sm.dout, n, w), d1 = tok(sm.dout, n + 1, w), u0 = tok(sm.u, n, w), u1 = tok(sm.u, n + 1, w);
-            const Frag w0 = tok(sm.w, n, w), w1 = tok(sm.w, n + 1, w);
+        for (int i = 0; i < 4; ++i) {
+            if (i <= w) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (i <= w) {
+                for (int n = 0; n < 4; n += 2) {
                     const Frag x0 = tok(sm.u, n, i), x1 = tok(sm.u, n + 1, i);
-                    o1[i] = M::mma(x0, x1, d0, d1, o1[i]);
-                    v1[i] = M::mma(x0, x1, w0, w1, v1[i]);
+                    mo[i] = M::mma(x0, x1, dw[n], dw[n + 1], mo[i]);
+                    mv[i] = M::mma(x0, x1, ww[n], ww[n + 1], mv[i]);
                 }
-                if (i >= w) {
-                    o2[i] = M::mma(tok(sm.dout, n, i), tok(sm.dout, n + 1, i), u0, u1, o2[i]);
-                    v2[i] = M::mma(tok(sm.w, n, i), tok(sm.w, n + 1, i), u0, u1, v2[i]);
+            } else {
+#pragma unroll
+                for (int n = 0; n < 4; n += 2) {
+                    mo[i] = M::mma(tok(sm.dout, n, i), tok(sm.dout, n + 1, i), uw[n], uw[n + 1], mo[i]);
+                    mv[i] = M::mma(tok(sm.w, n, i), tok(sm.w, n + 1, i), uw[n], uw[n + 1], mv[i]);
                 }
-                const Frag s0 = tok(sm.s, n, i), s1 = tok(sm.s, n + 1, i);
-                sq[i] = M::mma(d0, d1, s0, s1, sq[i]);
-                sk[i] = M::mma(w0, w1, s0, s1, sk[i]);
-                gk[i] = M::mma(u0, u1, tok(sm.d, n, i), tok(sm.d, n + 1, i), gk[i]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; n += 2) {
+            mo_d = M::mma(dw[n], dw[n + 1], uw[n], uw[n + 1], mo_d);
+            mv_d = M::mma(ww[n], ww[n + 1], uw[n], uw[n + 1], mv_d);
+        }
+        {
+            const f32x4 in = c4(kCoefIn, w), up = c4(kCoefUp, w);
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                f32x4 q = {0, 0, 0, 0}, g = q, x = q;
+#pragma unroll
+                for (int n = 0; n < 4; n += 2) {
+                    const Frag s0 = tok(sm.s, n, f), s1 = tok(sm.s, n + 1, f);
+                    q = M::mma(dw[n], dw[n + 1], s0, s1, q);
+                    x = M::mma(ww[n], ww[n + 1], s0, s1, x);
+                    g = M::mma(uw[n], uw[n + 1], tok(sm.d, n, f), tok(sm.d, n + 1, f), g);
+                }
+                dq[f] += weighted(q, in) * a.scale;
+                dk[f] += weighted(g, up) - weighted(x, in);
             }
         }
         if (!done) continue;
         // weights between the tokens
-        const auto c4 = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which + i * 16 + g4]); };
         {
             const int t = w * 16 + col;
             const float hi = sm.coef[kCoefHi + t], lo = sm.coef[kCoefLo + t];
             const int start = __float_as_int(sm.coef[kCoefStart + t]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            const auto weigh = [&](int i, bool later, f32x4& o, f32x4& v) {       // later: tile i has the later tokens
                 const f32x4 hi4 = c4(kCoefHi, i), lo4 = c4(kCoefLo, i), st4 = c4(kCoefStart, i);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int s = i * 16 + g4 + r;
-                    if (i <= w) {                                // t is the later one
-                        const float d = pair_decay(hi, lo, hi4[r], lo4[r]);
-                        const bool on = s <= t && start <= s;
-                        o1[i][r] = on ? o1[i][r] * (d * a.scale) : 0.0f;
-                        v1[i][r] = on && s < t ? -v1[i][r] * d : 0.0f;
-                    }
-                    if (i >= w) {                                // s is
-                        const float d = pair_decay(hi4[r], lo4[r], hi, lo);
-                        const bool on = t <= s && __float_as_int(st4[r]) <= t;
-                        o2[i][r] = on ? o2[i][r] * (d * a.scale) : 0.0f;
-                        v2[i][r] = on && t < s ? -v2[i][r] * d : 0.0f;
-                    }
+                    const float d = later ? pair_decay(hi4[r], lo4[r], hi, lo) : pair_decay(hi, lo, hi4[r], lo4[r]);
+                    const bool on = later ? t <= s && __float_as_int(st4[r]) <= t : s <= t && start <= s;
+                    o[r] = on ? o[r] * (d * a.scale) : 0.0f;
+                    v[r] = on && s != t ? -v[r] * d : 0.0f;
                 }
-            }
-        }
-        const f32x4 in = c4(kCoefIn, w), up = c4(kCoefUp, w);
+            };
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            dq[f] += weighted(sq[f], in) * a.scale;
-            dk[f] += weighted(gk[f], up) - weighted(sk[f], in);
+            for (int i = 0; i < 4; ++i) weigh(i, i > w, mo[i], mv[i]);
+            weigh(w, true, mo_d, mv_d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i == w) mv[i] += mv_d;               // each is 0 where the other is not
         }
         if (__builtin_amdgcn_readfirstlane(__float_as_int(sm.coef[kCoefA + 1])) == 0) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {                        // pairs of token tiles
-                const auto terms = [&](const f32x4& v, Frag (&to)[NM]) { M::template split<NM>(v, to); };
-                Frag a0[NM], a1[NM], b0[NM], b1[NM], e0[NM], e1[NM], g0[NM], g1[NM];
-                terms(o1[2 * p], a0);
-                terms(o1[2 * p + 1], a1);
-                terms(o2[2 * p], b0);
-                terms(o2[2 * p + 1], b1);
-                terms(v1[2 * p] + v2[2 * p], e0);               // v1 and v2 meet only on the diagonal tile, where each is 0 at the other's
-                terms(v1[2 * p + 1] + v2[2 * p + 1], e1);
+                Frag a0[NM], a1[NM], b0[NM], b1[NM], e0[NM], e1[NM];
+                const auto rows_of = [&](int i, Frag (&q)[NM], Frag (&k)[NM], Frag (&v)[NM]) {
+                    const f32x4 none = {0, 0, 0, 0};
+                    M::template split<NM>(i <= w ? mo[i] : none, q);
+                    M::template split<NM>(i == w ? mo_d : i > w ? mo[i] : none, k);
+                    M::template split<NM>(mv[i], v);
+                };
+                rows_of(2 * p, a0, b0, e0);
+                rows_of(2 * p + 1, a1, b1, e1);
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
                     const Frag k0 = M::direct(l, sm.k + f * 16 * kC, 2 * p), k1 = M::direct(l, sm.k + f * 16 * kC, 2 * p + 1);
@@ -265,27 +284,35 @@ __global__ __launch_bounds__(256, 2) void delta_grads_kernel(DeltaArgs a) {
                     }
                 }
             }
-        } else {                                                 // k or q not finite: pair by pair
+        } else {                                                 // k or q not finite: pair by pair, a wave's rows of M in LDS
+            float* rows16 = reinterpret_cast<float*>(sm.s) + w * 16 * kC;
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int which = 0; which < 3; ++which) {            // dq from k, dk from q, dk from k
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 none = {0, 0, 0, 0};
+                    const f32x4 v = which == 0 ? (i <= w ? mo[i] : none) : which == 1 ? (i == w ? mo_d : i > w ? mo[i] : none) : mv[i];
+                    *reinterpret_cast<f32x4*>(rows16 + col * kC + i * 16 + g4) = v;
+                }
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-                    for (int g = 0; g < 4; ++g) {
-                        const int s = i * 16 + g * 4 + r;
+                for (int s = 0; s < kC; ++s)
+#pragma unroll 1
+                    for (int x = 0; x < 4; ++x) {
+                        const float m = rows16[(g4 + x) * kC + s];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int from = (g << 4) | (g4 + x);
-                            const float mo = __shfl(o1[i][r], from), mt = __shfl(o2[i][r], from), mv = __shfl(v1[i][r] + v2[i][r], from);
+                        for (int f = 0; f < 4; ++f) {
+                            const float v = m == 0.0f ? 0.0f : m * tile_value((which == 1 ? sm.q : sm.k) + f * 16 * kC, col, s);
 #pragma unroll
-                            for (int f = 0; f < 4; ++f) {
-                                const float ks = tile_value(sm.k + f * 16 * kC, col, s), qs = tile_value(sm.q + f * 16 * kC, col, s);
-                                if (mo != 0.0f) dq[f][x] = fmaf(mo, ks, dq[f][x]);
-                                if (mt != 0.0f) dk[f][x] = fmaf(mt, qs, dk[f][x]);
-                                if (mv != 0.0f) dk[f][x] = fmaf(mv, ks, dk[f][x]);
+                            for (int r = 0; r < 4; ++r) {
+                                if (which == 0) dq[f][r] += x == r ? v : 0.0f;
+                                else dk[f][r] += x == r ? v : 0.0f;
                             }
                         }
                     }
+                __builtin_amdgcn_wave_barrier();
+            }
         }
     }
     const int64_t out = ((b * a.groups + grp) * parts + part) * a.dk + f0;

@@ -99,6 +99,10 @@ struct TokenRegs {
         if constexpr (sizeof(T) == 2) return Raw{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         else return Raw{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     }
+    __device__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = Raw{};
+    }
     __device__ f32x4 get(int i) const { return Mat<T>::widen(__builtin_bit_cast(typename Mat<T>::Frag, w[i])); }
 };
 
@@ -207,7 +211,8 @@ __device__ __forceinline__ void multiply_product(int l, const typename Mat<T>::F
                                                  const typename Mat<T>::Frag (&y)[4][NB], f32x4 (&acc)[4]) {
     using Frag = typename Mat<T>::Frag;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int jp = 0; jp < 2; ++jp) {
             const auto in = [&](int j) { return REV ? j >= i : j <= i; };
@@ -221,6 +226,7 @@ __device__ __forceinline__ void multiply_product(int l, const typename Mat<T>::F
             }
             acc[i] = mma_terms<T, NA, NB>(a0, a1, y[2 * jp], y[2 * jp + 1], acc[i]);
         }
+    }
 }
 
 // S += rows of a tile times w, over the chunk's tokens
@@ -231,6 +237,7 @@ __device__ __forceinline__ void add_tokens(int l, DeltaState<KF>& S, const T* ti
     for (int p = 0; p < 2; ++p)
 #pragma unroll
         for (int k = 0; k < KF; ++k) {
+            if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
             const typename M::Frag y0 = M::direct(l, tile + k * 16 * kC, 2 * p), y1 = M::direct(l, tile + k * 16 * kC, 2 * p + 1);
 #pragma unroll
             for (int n = NS - 1; n >= 0; --n) S.s[k] = M::mma(y0, y1, w[2 * p][n], w[2 * p + 1][n], S.s[k]);
@@ -327,7 +334,6 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         const float* cf = a.coef + unit * kDeltaCoef;
         cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
         vr.load(vp, (int64_t)chunk * kC, g4, L);
-        if constexpr (MODE == kDeltaStates) dr.load(dop, (int64_t)chunk * kC, g4, L);
     };
     const auto flush = [&](int chunk) {
         if constexpr (MODE == kDeltaStates) {
@@ -355,13 +361,11 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         }
         hr.store(tid, sm.h);
         if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
-        f32x4 x[4], dov[4];
+        f32x4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = live ? vr.get(i) : f32x4{0, 0, 0, 0};
-            if constexpr (MODE == kDeltaStates) dov[i] = live ? dr.get(i) : f32x4{0, 0, 0, 0};
-        }
+        for (int i = 0; i < 4; ++i) x[i] = live ? vr.get(i) : f32x4{0, 0, 0, 0};
         __syncthreads();
+        if constexpr (MODE == kDeltaStates) dr.load(dop, ct, g4, L);      // needed late in the chunk
         if (chunk < last) load(chunk + 1);
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
@@ -381,6 +385,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         for (int i = 0; i < 4; ++i) ak[i] = aq[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KF; k += 2) {
+            __builtin_amdgcn_sched_barrier(0);
             Frag s0[NS], s1[NS];
             M::template split<NS>(S.s[k], s0);
             M::template split<NS>(S.s[k + 1], s1);
@@ -434,7 +439,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16(o[i] * dov[i]));
+                        store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16(o[i] * (live ? dr.get(i) : f32x4{0, 0, 0, 0})));
                         if (live) store_tokens(up, ct + i * 16 + g4, L, u[i]);
                         *reinterpret_cast<f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4) = x[i];
                     }
@@ -539,11 +544,6 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         const float* cf = a.coef + unit * kDeltaCoef;
         cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
         dr.load(dop, (int64_t)chunk * kC, g4, L);
-        if constexpr (!SUM) {
-            vr.load(vp, (int64_t)chunk * kC, g4, L);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) er[i] = *reinterpret_cast<const f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4);
-        }
     };
     const auto flush = [&](int chunk) {
         if constexpr (!SUM) {
@@ -572,15 +572,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         pr.store(tid, sm.p);
         hr.store(tid, sm.h);
         if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
-        f32x4 dov[4], vv[4], ev[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            dov[i] = live ? dr.get(i) : f32x4{0, 0, 0, 0};
-            if constexpr (!SUM) {
-                vv[i] = live ? vr.get(i) : f32x4{0, 0, 0, 0};
-                ev[i] = er[i];
-            }
-        }
+        TokenRegs<T> dc = dr;
+        if (!live) dc.clear();
         if constexpr (!SUM) {
             // a boundary at the chunk's end: the product of the state and its gradient there
             const int next = chunk + 1;
@@ -608,6 +601,11 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             D.keep(static_cast<T*>(a.grads) + unit * KC * VP, zf);
         }
         __syncthreads();
+        if constexpr (!SUM) {                            // needed late in the chunk
+            vr.load(vp, ct, g4, L);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) er[i] = *reinterpret_cast<const f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4);
+        }
         if (chunk > first) load(chunk - 1);
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
@@ -617,6 +615,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         for (int i = 0; i < 4; ++i) ak[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KF; k += 2) {
+            __builtin_amdgcn_sched_barrier(0);
             Frag s0[NS], s1[NS];
             M::template split<NS>(D.s[k], s0);
             M::template split<NS>(D.s[k + 1], s1);
@@ -633,7 +632,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             Frag df[4][1];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                df[i][0] = M::round(dov[i]);             // exact: dout is of this type
+                df[i][0] = __builtin_bit_cast(Frag, dc.w[i]);
                 x[i] = weighted(ak[i], four(1, i));
             }
             multiply_product<T, true, NS, 1>(l, sm.p, df, x);
@@ -654,8 +653,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             if constexpr (!SUM) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16(vv[i] * dv[i]));
-                    store_sum16(l, &sm.dot[1][w][i * 16 + g4], sum16(x[i] * ev[i]));
+                    store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16((live ? vr.get(i) : f32x4{0, 0, 0, 0}) * dv[i]));
+                    store_sum16(l, &sm.dot[1][w][i * 16 + g4], sum16(x[i] * er[i]));
                     if (live) {
                         store_tokens(op, ct + i * 16 + g4, L, dv[i]);
                         if (wp) store_tokens(wp, ct + i * 16 + g4, L, dv[i]);
@@ -664,7 +663,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             }
             D.decay(cut, A);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) M::template split<NS>(weighted(dov[i], four(0, i)) * a.scale, y[i]);
+            for (int i = 0; i < 4; ++i) M::template split<NS>(weighted(dc.get(i), four(0, i)) * a.scale, y[i]);
             add_tokens<T, KF, NS>(l, D, sm.q, y);
 #pragma unroll
             for (int i = 0; i < 4; ++i) M::template split<NS>(-weighted(dv[i], four(0, i)), y[i]);
