@@ -98,6 +98,14 @@ __global__ __launch_bounds__(256) void delta_chain(DeltaArgs a) {
 // are made in both directions by the wave that needs them, as the operands they are next.
 // In bf16 u, dv and the states are rounded once; Mo and Mv are split into two terms.
 // --------------------------------------------------------------------------------------------
+// v where the weight is not 0, which a masked infinity or NaN must not pass
+__device__ __forceinline__ f32x4 weighted(const f32x4& v, const f32x4& weight) {
+    f32x4 o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = weight[r] == 0.0f ? 0.0f : v[r] * weight[r];
+    return o;
+}
+
 template <typename T>
 struct GradSmem {
     __attribute__((aligned(16))) T k[64 * kC];

@@ -21,8 +21,9 @@
 // Rounding in bf16: operands that the state holds are split into two or three bf16 terms (16 or all 24 bits), H
 // and P too where they meet them; a plain forward rounds P, its u and the S that q meets to bf16 once.
 //
-// Infinities and NaN: masks select.  A chunk whose k or q holds one, or whose u a wave finds it in, is walked by that
-// wave token by token from the definition, so that 0 times it reaches no other token or sequence.
+// Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
+// by token from the definition, so that 0 times it reaches no other token or sequence.  A state that holds one makes x
+// and with it u such, whatever the weights, 0 among them.
 #pragma once
 
 #include "linear_walk.hpp"
@@ -32,8 +33,9 @@ namespace pm {
 
 enum DeltaMode : int { kDeltaOut = 0, kDeltaSum = 1, kDeltaStates = 2 };
 
-template <typename T, int KC, int VP, int NH, int NP, bool Q, int DOTS>
-struct DeltaSmem {
+// A chunk's operands.
+template <typename T, int KC, int NH, int NP, bool Q>
+struct DeltaTiles {
     using Frag = typename Mat<T>::Frag;
     __attribute__((aligned(16))) T k[KC * kC];
     __attribute__((aligned(16))) T q[Q ? KC * kC : 8];
@@ -41,7 +43,18 @@ struct DeltaSmem {
     Frag p[NP ? NP : 1][NP ? kDeltaTiles : 1][64];
     __attribute__((aligned(16))) float coef[3][kC];
     __attribute__((aligned(16))) float misc[4];
-    __attribute__((aligned(16))) float dot[DOTS ? DOTS : 1][VP / 16][kC];
+};
+// Two of them where a CU holds as many blocks all the same: the next chunk's are written during this one, with one barrier a
+// chunk and not two.
+template <typename T, int KC, int VP, int NH, int NP, bool Q>
+constexpr int delta_buffers() {
+    return (int)sizeof(DeltaTiles<T, KC, NH, NP, Q>) * 2 <= (VP == 128 ? 156 : 78) * 1024 ? 2 : 1;
+}
+template <typename T, int KC, int VP, int NH, int NP, bool Q, int DOTS>
+struct DeltaSmem {
+    static constexpr int kBuffers = delta_buffers<T, KC, VP, NH, NP, Q>();
+    DeltaTiles<T, KC, NH, NP, Q> b[kBuffers];
+    __attribute__((aligned(16))) float dot[2][DOTS ? DOTS : 1][VP / 16][kC];
     float xdot[VP / 16];
 };
 
@@ -71,39 +84,90 @@ struct ProductRegs {
     }
 };
 
-// Four consecutive tokens of one feature's row at a time, for the four tiles of a chunk: what a lane's result
-// registers hold of it.
+// A chunk of one feature's row, as a lane's result registers hold it: tokens 16 i + 4 (lane / 16) .. + 3 of row lane % 16, for the
+// four tiles i.  In bf16 those are 8 bytes each; 16-byte vectors of memory serve two tiles, whose halves the lanes of
+// neighbouring rows of 16 swap, so that a row's bytes move in pieces of 64 and not of 32.
 template <typename T>
 struct TokenRegs {
-    using Raw = std::conditional_t<sizeof(T) == 2, u32x2, u32x4>;
-    Raw w[4];
-    // p: the feature's row, t0: the chunk's first token, g4: the lane's first in a tile
-    __device__ void load(const T* p, int64_t t0, int g4, int64_t L) {
+    using Frag = typename Mat<T>::Frag;
+    static constexpr bool kPairs = sizeof(T) == 2;
+    static constexpr int kVecs = kPairs ? 2 : 4, kPer = Storage<T>::kPerVec;
+    u32x4 w[kVecs];
+
+    // a vector's first token
+    __device__ static int at(int l, int i) {
+        return kPairs ? i * 32 + ((l >> 4) & 1) * 16 + (l >> 5) * 8 : i * 16 + (l >> 4) * 4;
+    }
+    // p: the feature's row, t0: the chunk's first token
+    __device__ void load(const T* p, int64_t t0, int l, int64_t L) {
         if (t0 + kC <= L) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = load_vec<T, 4>(p + t0 + i * 16 + g4);
+            for (int i = 0; i < kVecs; ++i) w[i] = load_vec<T, kPer>(p + t0 + at(l, i));
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[4];
+            for (int i = 0; i < kVecs; ++i) {
+                float v[kPer];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t t = t0 + i * 16 + g4 + r;
+                for (int r = 0; r < kPer; ++r) {
+                    const int64_t t = t0 + at(l, i) + r;
                     v[r] = t < L ? Storage<T>::load1(p + t) : 0.0f;
                 }
-                w[i] = pack(v);
+                w[i] = Storage<T>::pack(v);
             }
         }
     }
-    __device__ static Raw pack(const float* v) {
-        if constexpr (sizeof(T) == 2) return Raw{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-        else return Raw{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    }
-    __device__ void clear() {
+    __device__ void store(T* p, int64_t t0, int l, int64_t L) const {
+        if (t0 + kC <= L) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = Raw{};
+            for (int i = 0; i < kVecs; ++i) *reinterpret_cast<typename Storage<T>::Vec*>(p + t0 + at(l, i)) = w[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                float v[kPer];
+                Storage<T>::unpack(w[i], v);
+#pragma unroll
+                for (int r = 0; r < kPer; ++r)
+                    if (t0 + at(l, i) + r < L) Storage<T>::store1(p + t0 + at(l, i) + r, v[r]);     // of this type already
+            }
+        }
     }
-    __device__ f32x4 get(int i) const { return Mat<T>::widen(__builtin_bit_cast(typename Mat<T>::Frag, w[i])); }
+    __device__ static void swap(uint32_t& a, uint32_t& b) {      // a's odd rows of 16 lanes with b's even ones
+        const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+        a = r[0];
+        b = r[1];
+    }
+    // the tiles' values; mask: all ones, or 0 for a row that the tensor lacks
+    __device__ void get(uint32_t mask, Frag (&f)[4]) const {
+        if constexpr (kPairs) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                u32x4 v = w[i] & mask;
+                uint32_t a = v.x, b = v.y, c = v.z, d = v.w;
+                swap(a, c);
+                swap(b, d);
+                f[2 * i] = Frag{a, b};
+                f[2 * i + 1] = Frag{c, d};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = __builtin_bit_cast(f32x4, u32x4(w[i] & mask));
+        }
+    }
+    __device__ void set(const f32x4 (&v)[4]) {
+        if constexpr (kPairs) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const u32x2 x = Mat<T>::round(v[2 * i]), y = Mat<T>::round(v[2 * i + 1]);
+                uint32_t a = x.x, b = x.y, c = y.x, d = y.y;
+                swap(a, c);
+                swap(b, d);
+                w[i] = u32x4{a, b, c, d};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(u32x4, v[i]);
+        }
+    }
 };
 
 // v at four consecutive tokens t.. of a row
@@ -151,8 +215,13 @@ struct DeltaState {
         });
     }
     __device__ void decay(bool cut, float a) {
+        if (cut) {                                       // both the same for the whole wave
 #pragma unroll
-        for (int k = 0; k < KF; ++k) s[k] = cut ? f32x4{0, 0, 0, 0} : s[k] * a;
+            for (int k = 0; k < KF; ++k) s[k] = f32x4{0, 0, 0, 0};
+        } else {
+#pragma unroll
+            for (int k = 0; k < KF; ++k) s[k] *= a;
+        }
     }
     // transposed, rounded to T: column z is a row of KF * 16
     template <typename T>
@@ -190,58 +259,75 @@ struct DeltaState {
     }
 };
 
-// c + the terms' products, of operands split into NA and NB terms; those below the last term's size are left out.
-template <typename T, int NA, int NB>
-__device__ __forceinline__ f32x4 mma_terms(const typename Mat<T>::Frag (&a0)[NA], const typename Mat<T>::Frag (&a1)[NA],
-                                           const typename Mat<T>::Frag (&b0)[NB], const typename Mat<T>::Frag (&b1)[NB], f32x4 c) {
-    constexpr int kMost = NA > NB ? NA : NB;
-#pragma unroll
-    for (int n = kMost - 1; n >= 0; --n)
-#pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const int j = n - i;
-            if (j >= 0 && j < NB) c = Mat<T>::mma(a0[i], a1[i], b0[j], b1[j], c);
-        }
-    return c;
-}
-
-// acc[i] (token tile i) += product tiles (i, j) times y[j], over j <= i, or with REV over j >= i of the turned tiles
+// acc[i] (token tile i) += product tiles (i, j) times y[j], over j <= i, or with REV over j >= i of the turned tiles.  The tiles'
+// chains take turns: a matrix instruction that takes the result of the one before waits for it.
 template <typename T, bool REV, int NA, int NB>
-__device__ __forceinline__ void multiply_product(int l, const typename Mat<T>::Frag (*tiles)[kDeltaTiles][64],
+__device__ __forceinline__ void multiply_product(int lane, const typename Mat<T>::Frag (*tiles)[kDeltaTiles][64],
                                                  const typename Mat<T>::Frag (&y)[4][NB], f32x4 (&acc)[4]) {
     using Frag = typename Mat<T>::Frag;
+    const int l = here(lane);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int jp = 0; jp < 2; ++jp) {
         __builtin_amdgcn_sched_barrier(0);
+        const auto in = [&](int i, int j) { return REV ? j >= i : j <= i; };
+        const auto at = [&](int i, int j) { return REV ? delta_tile(j, i) : delta_tile(i, j); };
 #pragma unroll
-        for (int jp = 0; jp < 2; ++jp) {
-            const auto in = [&](int j) { return REV ? j >= i : j <= i; };
-            const auto at = [&](int j) { return REV ? delta_tile(j, i) : delta_tile(i, j); };
-            if (!in(2 * jp) && !in(2 * jp + 1)) continue;
-            Frag a0[NA], a1[NA];
+        for (int n = NA - 1; n >= 0; --n) {              // terms' products below the last term's size are left out
+            Frag f[4][2];
 #pragma unroll
-            for (int n = 0; n < NA; ++n) {
-                a0[n] = in(2 * jp) ? tiles[n][at(2 * jp)][l] : Frag{};
-                a1[n] = in(2 * jp + 1) ? tiles[n][at(2 * jp + 1)][l] : Frag{};
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) f[i][q] = in(i, 2 * jp + q) ? tiles[n][at(i, 2 * jp + q)][l] : Frag{};
+#pragma unroll
+            for (int m = NB - 1; m >= 0; --m) {
+                if (n + m >= (NA > NB ? NA : NB)) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (in(i, 2 * jp) || in(i, 2 * jp + 1)) acc[i] = Mat<T>::mma(f[i][0], f[i][1], y[2 * jp][m], y[2 * jp + 1][m], acc[i]);
             }
-            acc[i] = mma_terms<T, NA, NB>(a0, a1, y[2 * jp], y[2 * jp + 1], acc[i]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
 
 // S += rows of a tile times w, over the chunk's tokens
 template <typename T, int KF, int NS>
-__device__ __forceinline__ void add_tokens(int l, DeltaState<KF>& S, const T* tile, const typename Mat<T>::Frag (&w)[4][NS]) {
+__device__ __forceinline__ void add_tokens(int lane, DeltaState<KF>& S, const T* tile, const typename Mat<T>::Frag (&w)[4][NS]) {
     using M = Mat<T>;
+    const int l = here(lane);
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int k = 0; k < KF; ++k) {
-            if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-            const typename M::Frag y0 = M::direct(l, tile + k * 16 * kC, 2 * p), y1 = M::direct(l, tile + k * 16 * kC, 2 * p + 1);
+        for (int k = 0; k < KF; k += 4) {
+            __builtin_amdgcn_sched_barrier(0);
+            typename M::Frag y[4][2];
 #pragma unroll
-            for (int n = NS - 1; n >= 0; --n) S.s[k] = M::mma(y0, y1, w[2 * p][n], w[2 * p + 1][n], S.s[k]);
+            for (int q = 0; q < 4; ++q) {
+                y[q][0] = M::direct(l, tile + (k + q) * 16 * kC, 2 * p);
+                y[q][1] = M::direct(l, tile + (k + q) * 16 * kC, 2 * p + 1);
+            }
+#pragma unroll
+            for (int n = NS - 1; n >= 0; --n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) S.s[k + q] = M::mma(y[q][0], y[q][1], w[2 * p][n], w[2 * p + 1][n], S.s[k + q]);
         }
+}
+
+// acc[i] (token tile i) += a tile's columns times the state's rows 16 k .. + 31, split into terms.
+template <typename T, int NS>
+__device__ __forceinline__ void against_tokens(int l, const T* tile, int k, const typename Mat<T>::Frag (&s0)[NS],
+                                               const typename Mat<T>::Frag (&s1)[NS], f32x4 (&acc)[4]) {
+    using M = Mat<T>;
+    typename M::Frag f[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i][0] = M::transposed(l, tile + k * 16 * kC, i);
+        f[i][1] = M::transposed(l, tile + (k + 1) * 16 * kC, i);
+    }
+#pragma unroll
+    for (int n = NS - 1; n >= 0; --n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = M::mma(f[i][0], f[i][1], s0[n], s1[n], acc[i]);
 }
 
 __device__ __forceinline__ bool any_nonfinite(const f32x4 (&v)[4]) {
@@ -251,14 +337,6 @@ __device__ __forceinline__ bool any_nonfinite(const f32x4 (&v)[4]) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) z = fmaf(v[i][r], 0.0f, z);
     return __ballot(!(z == 0.0f)) != 0;
-}
-
-// v where the weight is not 0, which a masked infinity or NaN must not pass
-__device__ __forceinline__ f32x4 weighted(const f32x4& v, const f32x4& weight) {
-    f32x4 o;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) o[r] = weight[r] == 0.0f ? 0.0f : v[r] * weight[r];
-    return o;
 }
 
 // the multiplier of the state at one token
@@ -293,7 +371,9 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
     constexpr bool kQ = MODE != kDeltaSum;
     constexpr int NQ = MODE == kDeltaStates ? NS : 1;       // terms of what the outs are made of
-    __shared__ DeltaSmem<T, KC, VP, NS, kQ ? NQ : 0, kQ, MODE == kDeltaStates ? 1 : 0> sm;
+    using Smem = DeltaSmem<T, KC, VP, NS, kQ ? NQ : 0, kQ, MODE == kDeltaStates ? 1 : 0>;
+    constexpr bool kTwo = Smem::kBuffers == 2;
+    __shared__ Smem smem;
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
     const int64_t L = a.seqlen;
     const int mblocks = MODE == kDeltaSum ? (KC + VP - 1) / VP : 0, nseg = MODE == kDeltaSum ? a.sum_segs : a.nseg;
@@ -306,6 +386,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     const T* qp = static_cast<const T*>(a.q) + (b * a.groups + h / (a.heads / a.groups)) * a.dk * L;
     const int zf = w * 16, z = zf + col;
     const bool live = mb == 0 && z < a.dv;
+    const uint32_t mask = live ? ~0u : 0u;
     const int64_t zrow = bh * a.dv + min(z, a.dv - 1);
     const T* vp = static_cast<const T*>(a.v) + zrow * L;
     const T* dop = MODE == kDeltaStates ? static_cast<const T*>(a.dout) + zrow * L : nullptr;
@@ -324,49 +405,86 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     ProductRegs<T, NQ, kThreads> pr;
     TokenRegs<T> vr, dr;
     f32x4 cr;
+    // K, Q and the weights; H and P, which are needed later: half the loads at a time, each after products that
+    // the memory's queues can drain under
     const auto load = [&](int chunk) {
+        const int tid = here(threadIdx.x);
         const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
-        const int64_t unit = bh * a.chunks + chunk;
         kr.load(tid, at, kp, a.dk, (int)L);
         if constexpr (kQ) qr.load(tid, at, qp, a.dk, (int)L);
+        const float* cf = a.coef + (bh * a.chunks + chunk) * kDeltaCoef;
+        cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
+    };
+    const auto load_products = [&](int chunk) {
+        const int tid = here(threadIdx.x);
+        const int64_t unit = bh * a.chunks + chunk;
         hr.load(tid, a.h[0] + unit * kDeltaProduct);
         if constexpr (kQ) pr.load(tid, a.p[0] + unit * kDeltaProduct);
-        const float* cf = a.coef + unit * kDeltaCoef;
-        cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
-        vr.load(vp, (int64_t)chunk * kC, g4, L);
     };
-    const auto flush = [&](int chunk) {
-        if constexpr (MODE == kDeltaStates) {
-            const int64_t t = (int64_t)chunk * kC + tid;
-            if (tid < kC && t < L) {
-                float v = sm.dot[0][0][tid];
-#pragma unroll
-                for (int n = 1; n < kWaves; ++n) v += sm.dot[0][n][tid];
-                a.rq[bh * L + t] = v;
-            }
-        }
-    };
-    bool all_cut = false;
-    load(first);
-    for (int chunk = first; chunk <= last; ++chunk) {
-        const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
-        __syncthreads();
-        if (MODE == kDeltaStates && chunk > first) flush(chunk - 1);
+    const auto stage = [&](int chunk) {
+        const int tid = here(threadIdx.x);
+        auto& sm = smem.b[kTwo ? (chunk - first) & 1 : 0];
+        const int64_t ct = (int64_t)chunk * kC;
         kr.settle(tid, kp, a.dk, ct, L);
         kr.store(tid, sm.k);
         if constexpr (kQ) {
             qr.settle(tid, qp, a.dk, ct, L);
             qr.store(tid, sm.q);
-            pr.store(tid, sm.p);
         }
-        hr.store(tid, sm.h);
         if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
-        f32x4 x[4];
+    };
+    const auto stage_products = [&](int chunk) {
+        const int tid = here(threadIdx.x);
+        auto& sm = smem.b[kTwo ? (chunk - first) & 1 : 0];
+        hr.store(tid, sm.h);
+        if constexpr (kQ) pr.store(tid, sm.p);
+    };
+    const auto flush = [&](int chunk) {
+        if constexpr (MODE == kDeltaStates) {
+            const auto& dot = smem.dot[(chunk - first) & 1][0];
+            const int64_t t = (int64_t)chunk * kC + tid;
+            if (tid < kC && t < L) {
+                float v = dot[0][tid];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = live ? vr.get(i) : f32x4{0, 0, 0, 0};
+                for (int n = 1; n < kWaves; ++n) v += dot[n][tid];
+                a.rq[bh * L + t] = v;
+            }
+        }
+    };
+    // The outs of a chunk are stored in the next, after its operands are in LDS: to wait for those, loaded a chunk ago, is to wait
+    // for every store since.
+    TokenRegs<TO> pending;
+    bool any_pending = false;
+    const auto store_pending = [&](int chunk) {
+        if (MODE == kDeltaOut && any_pending && live) pending.store(op, (int64_t)chunk * kC, here(l), L);
+    };
+    bool all_cut = false;
+    load(first);
+    load_products(first);
+    if constexpr (kTwo) {
+        stage(first);
+        stage_products(first);
+        if (first < last) {
+            load(first + 1);
+            load_products(first + 1);
+        }
+    }
+    for (int chunk = first; chunk <= last; ++chunk) {
+        const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
+        auto& sm = smem.b[kTwo ? (chunk - first) & 1 : 0];
+        auto& dot = smem.dot[(chunk - first) & 1][0];
         __syncthreads();
-        if constexpr (MODE == kDeltaStates) dr.load(dop, ct, g4, L);      // needed late in the chunk
-        if (chunk < last) load(chunk + 1);
+        if (MODE == kDeltaStates && chunk > first) flush(chunk - 1);
+        if constexpr (kTwo) {
+            if (chunk < last) stage(chunk + 1);
+        } else {
+            stage(chunk);
+            stage_products(chunk);
+            __syncthreads();
+        }
+        store_pending(chunk - 1);
+        vr.load(vp, ct, here(l), L);                          // needed once K^T S is there
+        if constexpr (MODE == kDeltaStates) dr.load(dop, ct, here(l), L);
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
         all_cut = all_cut || cut;
@@ -380,7 +498,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
             }
         }
         // K^T S and Q^T S
-        f32x4 ak[4], aq[4];
+        const int lk = here(l);                          // offsets computed anew in each phase: registers are short
+        f32x4 ak[4], aq[4], x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) ak[i] = aq[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -389,33 +508,31 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
             Frag s0[NS], s1[NS];
             M::template split<NS>(S.s[k], s0);
             M::template split<NS>(S.s[k + 1], s1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Frag k0 = M::transposed(l, sm.k + k * 16 * kC, i), k1 = M::transposed(l, sm.k + (k + 1) * 16 * kC, i);
-#pragma unroll
-                for (int n = NS - 1; n >= 0; --n) ak[i] = M::mma(k0, k1, s0[n], s1[n], ak[i]);
-                if constexpr (kQ) {
-                    const Frag q0 = M::transposed(l, sm.q + k * 16 * kC, i), q1 = M::transposed(l, sm.q + (k + 1) * 16 * kC, i);
-                    if constexpr (NQ == 1 && NS > 1) {
-                        aq[i] = M::mma(q0, q1, M::round(S.s[k]), M::round(S.s[k + 1]), aq[i]);
-                    } else {
-#pragma unroll
-                        for (int n = NQ - 1; n >= 0; --n) aq[i] = M::mma(q0, q1, s0[n], s1[n], aq[i]);
-                    }
-                }
+            against_tokens<T, NS>(lk, sm.k, k, s0, s1, ak);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kQ && NQ == 1 && NS > 1) {
+                const Frag r0[1] = {M::round(S.s[k])}, r1[1] = {M::round(S.s[k + 1])};
+                against_tokens<T, 1>(lk, sm.q, k, r0, r1, aq);
+            } else if constexpr (kQ) {
+                against_tokens<T, NQ>(lk, sm.q, k, s0, s1, aq);
             }
         }
-        const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4]); };
-        Frag y[4][NS];
+        if (chunk + kTwo < last) load(chunk + 1 + kTwo);
+        if (kTwo && chunk < last) stage_products(chunk + 1);
+        const int g4c = (here(l) >> 4) * 4;
+        const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4c]); };
+        Frag y[4][NS], vf[4];
+        vr.get(mask, vf);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[i] -= weighted(ak[i], four(0, i));
+            x[i] = M::widen(vf[i]) - ak[i] * four(0, i);
             M::template split<NS>(x[i] * four(2, i), y[i]);
         }
         f32x4 hx[4], u[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
         multiply_product<T, false, NS, NS>(l, sm.h, y, hx);
+        if (chunk + kTwo < last) load_products(chunk + 1 + kTwo);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] -= hx[i];                               // the errors
@@ -423,26 +540,29 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         }
         if (!bad && !any_nonfinite(u)) {
             if constexpr (kQ) {
+                if constexpr (MODE == kDeltaStates) {
+                    TokenRegs<T> ur;
+                    ur.set(u);
+                    if (live) ur.store(up, ct, here(l), L);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4) = x[i];
+                }
                 Frag uf[4][NQ];
                 f32x4 o[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     M::template split<NQ>(u[i], uf[i]);
-                    o[i] = weighted(aq[i], four(0, i)) * a.scale;
+                    o[i] = aq[i] * (four(0, i) * a.scale);
                 }
                 multiply_product<T, false, NQ, NQ>(l, sm.p, uf, o);
                 if constexpr (MODE == kDeltaOut) {
-                    if (live) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) store_tokens(op, ct + i * 16 + g4, L, o[i]);
-                    }
+                    any_pending = true;
+                    pending.set(o);
                 } else {
+                    Frag df[4];
+                    dr.get(mask, df);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16(o[i] * (live ? dr.get(i) : f32x4{0, 0, 0, 0})));
-                        if (live) store_tokens(up, ct + i * 16 + g4, L, u[i]);
-                        *reinterpret_cast<f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4) = x[i];
-                    }
+                    for (int i = 0; i < 4; ++i) store_sum16(l, &dot[w][i * 16 + g4], sum16(o[i] * M::widen(df[i])));
                 }
             }
 #pragma unroll
@@ -450,6 +570,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
             S.decay(cut, A);
             add_tokens<T, KF, NS>(l, S, sm.k, y);
         } else {
+            any_pending = false;
 #pragma unroll 1
             for (int j = 0; j < kC; ++j) {
                 const int64_t t = ct + j;
@@ -467,7 +588,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                         if (mine) Storage<TO>::store1(op + t, o);
                     } else {
                         const float d = lanes16(live && t < L ? o * Storage<T>::load1(dop + t) : 0.0f);
-                        if (l == 0) sm.dot[0][w][j] = d;
+                        if (l == 0) dot[w][j] = d;
                         if (g4 == 0) {
                             if (mine) Storage<T>::store1(up + t, ut);
                             a.e[(((unit * kWaves + w) * 4 + j / 16) * 64 + (j % 16) / 4 * 16 + col) * 4 + j % 4] = t < L ? e : 0.0f;
@@ -477,6 +598,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
             }
         }
     }
+    store_pending(last);
     if constexpr (MODE == kDeltaStates) {
         __syncthreads();
         flush(last);
@@ -507,7 +629,9 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     using M = Mat<T>;
     using Frag = typename M::Frag;
     constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
-    __shared__ DeltaSmem<T, KC, VP, NS, NS, true, SUM ? 0 : 2> sm;
+    using Smem = DeltaSmem<T, KC, VP, NS, NS, true, SUM ? 0 : 2>;
+    constexpr bool kTwo = Smem::kBuffers == 2;
+    __shared__ Smem smem;
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
     const int64_t L = a.seqlen;
     const int nseg = SUM ? a.nseg - 1 : a.nseg;             // the first segment adds to nothing
@@ -519,6 +643,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const T* qp = static_cast<const T*>(a.q) + (b * a.groups + h / (a.heads / a.groups)) * a.dk * L;
     const int zf = w * 16, z = zf + col;
     const bool live = z < a.dv;
+    const uint32_t mask = live ? ~0u : 0u;
     const int64_t zrow = bh * a.dv + min(z, a.dv - 1);
     const T* vp = static_cast<const T*>(a.v) + zrow * L;
     const T* dop = static_cast<const T*>(a.dout) + zrow * L;
@@ -535,25 +660,45 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     TokenRegs<T> vr, dr;
     f32x4 cr, er[4];
     const auto load = [&](int chunk) {
+        const int tid = here(threadIdx.x);
         const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
-        const int64_t unit = bh * a.chunks + chunk;
         kr.load(tid, at, kp, a.dk, (int)L);
         qr.load(tid, at, qp, a.dk, (int)L);
+        const float* cf = a.coef + (bh * a.chunks + chunk) * kDeltaCoef;
+        cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
+    };
+    const auto load_products = [&](int chunk) {
+        const int tid = here(threadIdx.x);
+        const int64_t unit = bh * a.chunks + chunk;
         hr.load(tid, a.h[1] + unit * kDeltaProduct);
         pr.load(tid, a.p[1] + unit * kDeltaProduct);
-        const float* cf = a.coef + unit * kDeltaCoef;
-        cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
-        dr.load(dop, (int64_t)chunk * kC, g4, L);
+    };
+    const auto stage = [&](int chunk) {
+        const int tid = here(threadIdx.x);
+        auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
+        const int64_t ct = (int64_t)chunk * kC;
+        kr.settle(tid, kp, a.dk, ct, L);
+        kr.store(tid, sm.k);
+        qr.settle(tid, qp, a.dk, ct, L);
+        qr.store(tid, sm.q);
+        if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
+    };
+    const auto stage_products = [&](int chunk) {
+        const int tid = here(threadIdx.x);
+        auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
+        pr.store(tid, sm.p);
+        hr.store(tid, sm.h);
     };
     const auto flush = [&](int chunk) {
         if constexpr (!SUM) {
+            const auto& dot = smem.dot[(last - chunk) & 1];
             const int64_t t = (int64_t)chunk * kC + tid;
             if (tid < kC && t < L) {
-                float v = sm.dot[0][0][tid], d = sm.dot[1][0][tid];
+                float v = dot[0][0][tid], d = dot[1][0][tid];
 #pragma unroll
                 for (int n = 1; n < kWaves; ++n) {
-                    v += sm.dot[0][n][tid];
-                    d += sm.dot[1][n][tid];
+                    v += dot[0][n][tid];
+                    d += dot[1][n][tid];
                 }
                 a.rk[bh * L + t] = -v;
                 a.dbeta[bh * L + t] = d;
@@ -561,19 +706,28 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         }
     };
     load(last);
+    load_products(last);
+    if constexpr (kTwo) {
+        stage(last);
+        stage_products(last);
+        if (last > first) {
+            load(last - 1);
+            load_products(last - 1);
+        }
+    }
     for (int chunk = last; chunk >= first; --chunk) {
         const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
+        auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
+        auto& dot = smem.dot[(last - chunk) & 1];
         __syncthreads();
         if (!SUM && chunk < last) flush(chunk + 1);
-        kr.settle(tid, kp, a.dk, ct, L);
-        kr.store(tid, sm.k);
-        qr.settle(tid, qp, a.dk, ct, L);
-        qr.store(tid, sm.q);
-        pr.store(tid, sm.p);
-        hr.store(tid, sm.h);
-        if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
-        TokenRegs<T> dc = dr;
-        if (!live) dc.clear();
+        if constexpr (kTwo) {
+            if (chunk > first) stage(chunk - 1);
+        } else {
+            stage(chunk);
+            stage_products(chunk);
+        }
+        dr.load(dop, ct, here(l), L);
         if constexpr (!SUM) {
             // a boundary at the chunk's end: the product of the state and its gradient there
             const int next = chunk + 1;
@@ -589,27 +743,27 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                 }
 #pragma unroll
                 for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
-                if (l == 0) sm.xdot[w] = v;
+                if (l == 0) smem.xdot[w] = v;
                 __syncthreads();
                 if (tid == 0) {
-                    v = sm.xdot[0];
+                    v = smem.xdot[0];
 #pragma unroll
-                    for (int i = 1; i < kWaves; ++i) v += sm.xdot[i];
+                    for (int i = 1; i < kWaves; ++i) v += smem.xdot[i];
                     a.dot[bh * (a.nb + 1) + n] = v;
                 }
             }
             D.keep(static_cast<T*>(a.grads) + unit * KC * VP, zf);
         }
-        __syncthreads();
+        if constexpr (!kTwo) __syncthreads();
         if constexpr (!SUM) {                            // needed late in the chunk
-            vr.load(vp, ct, g4, L);
+            vr.load(vp, ct, here(l), L);
 #pragma unroll
             for (int i = 0; i < 4; ++i) er[i] = *reinterpret_cast<const f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4);
         }
-        if (chunk > first) load(chunk - 1);
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
         const bool bad = __builtin_amdgcn_readfirstlane(__float_as_int(sm.misc[1])) != 0;
+        const int lk = here(l);                          // offsets computed anew in each phase: registers are short
         f32x4 ak[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) ak[i] = f32x4{0, 0, 0, 0};
@@ -619,21 +773,21 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             Frag s0[NS], s1[NS];
             M::template split<NS>(D.s[k], s0);
             M::template split<NS>(D.s[k + 1], s1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Frag k0 = M::transposed(l, sm.k + k * 16 * kC, i), k1 = M::transposed(l, sm.k + (k + 1) * 16 * kC, i);
-#pragma unroll
-                for (int n = NS - 1; n >= 0; --n) ak[i] = M::mma(k0, k1, s0[n], s1[n], ak[i]);
-            }
+            against_tokens<T, NS>(lk, sm.k, k, s0, s1, ak);
         }
-        const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4]); };
+        if (chunk - kTwo > first) load(chunk - 1 - kTwo);
+        if (kTwo && chunk > first) stage_products(chunk - 1);
+        const int g4c = (here(l) >> 4) * 4;
+        const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4c]); };
         f32x4 x[4];
+        Frag df[4][1];                                   // exact: dout is of this type
         {
-            Frag df[4][1];
+            Frag f[4];
+            dr.get(mask, f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                df[i][0] = __builtin_bit_cast(Frag, dc.w[i]);
-                x[i] = weighted(ak[i], four(1, i));
+                df[i][0] = f[i];
+                x[i] = ak[i] * four(1, i);
             }
             multiply_product<T, true, NS, 1>(l, sm.p, df, x);
         }
@@ -644,6 +798,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
         multiply_product<T, true, NS, NS>(l, sm.h, y, hx);
+        if (chunk - kTwo > first) load_products(chunk - 1 - kTwo);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] -= hx[i];                               // du
@@ -651,22 +806,28 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         }
         if (!bad && !any_nonfinite(x)) {
             if constexpr (!SUM) {
+                TokenRegs<TO> out;
+                out.set(dv);
+                if (live) out.store(op, ct, here(l), L);
+                if constexpr (sizeof(TO) != sizeof(T)) {
+                    TokenRegs<T> copy;
+                    copy.set(dv);
+                    if (live) copy.store(wp, ct, here(l), L);
+                }
+                Frag vf[4];
+                vr.get(mask, vf);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    store_sum16(l, &sm.dot[0][w][i * 16 + g4], sum16((live ? vr.get(i) : f32x4{0, 0, 0, 0}) * dv[i]));
-                    store_sum16(l, &sm.dot[1][w][i * 16 + g4], sum16(x[i] * er[i]));
-                    if (live) {
-                        store_tokens(op, ct + i * 16 + g4, L, dv[i]);
-                        if (wp) store_tokens(wp, ct + i * 16 + g4, L, dv[i]);
-                    }
+                    store_sum16(l, &dot[0][w][i * 16 + g4], sum16(M::widen(vf[i]) * dv[i]));
+                    store_sum16(l, &dot[1][w][i * 16 + g4], sum16(x[i] * er[i]));
                 }
             }
             D.decay(cut, A);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) M::template split<NS>(weighted(dc.get(i), four(0, i)) * a.scale, y[i]);
+            for (int i = 0; i < 4; ++i) M::template split<NS>(M::widen(df[i][0]) * (four(0, i) * a.scale), y[i]);
             add_tokens<T, KF, NS>(l, D, sm.q, y);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) M::template split<NS>(-weighted(dv[i], four(0, i)), y[i]);
+            for (int i = 0; i < 4; ++i) M::template split<NS>(-dv[i] * four(0, i), y[i]);
             add_tokens<T, KF, NS>(l, D, sm.k, y);
         } else {
 #pragma unroll 1
@@ -682,8 +843,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                     const float et = a.e[(((unit * kWaves + w) * 4 + j / 16) * 64 + (j % 16) / 4 * 16 + col) * 4 + j % 4];
                     const float vd = lanes16(in && live ? Storage<T>::load1(vp + t) * dvt : 0.0f), db = lanes16(in && live ? du * et : 0.0f);
                     if (l == 0) {
-                        sm.dot[0][w][j] = vd;
-                        sm.dot[1][w][j] = db;
+                        dot[0][w][j] = vd;
+                        dot[1][w][j] = db;
                     }
                     if (g4 == 0 && live && in) {
                         Storage<TO>::store1(op + t, dvt);
