@@ -31,62 +31,58 @@ hipError_t walk(const DeltaArgs& a, DeltaWalk which, hipStream_t s) {
 // row and head, its waves 16 rows each; products in 32 bits.
 // --------------------------------------------------------------------------------------------
 template <int KC, bool REV>
-__global__ __launch_bounds__(256) void delta_chain(DeltaArgs a) {
-    constexpr int KF = KC / 16, kMine = KF / 4;
-    __shared__ f32x4 cur[KF][64];
+__global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
+    constexpr int KF = KC / 16;
+    __shared__ f32x4 cur[2][KF][64];
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4;
     const int cols = (a.dv + 15) / 16;
     const int64_t bh = blockIdx.x / cols;
     const int z = (int)(blockIdx.x - bh * cols) * 16 + col;
     const int64_t sz = (int64_t)a.dk * a.dv;
-    const auto at = [&](const float* p, int x) { return p && x < a.dk && z < a.dv ? p[(int64_t)x * a.dv + z] : 0.0f; };
-#pragma unroll
-    for (int m = 0; m < kMine; ++m) {
-        const int k = w + m * 4;
+    const auto seg = [&](int n) { return bh * a.nseg + (REV ? a.nseg - 1 - n : n); };
+    const auto at = [&](const float* p) {
         f32x4 v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = at(a.entry ? a.entry + bh * sz : nullptr, k * 16 + g4 + r);
-        cur[k][l] = v;
-    }
-    __syncthreads();
-    for (int n = 0; n < a.nseg; ++n) {
-        const int64_t seg = bh * a.nseg + (REV ? a.nseg - 1 - n : n);
-        float* p = a.seg + seg * sz;
-        const float* M = a.seg_m + seg * KC * KC;
-        const bool more = n + 1 < a.nseg, cut = more && a.seg_cut[seg] != 0;
-        f32x4 next[kMine];
+        for (int r = 0; r < 4; ++r) v[r] = p && w * 16 + g4 + r < a.dk && z < a.dv ? p[(int64_t)(w * 16 + g4 + r) * a.dv + z] : 0.0f;
+        return v;
+    };
+    f32x4 m[KF], added;                                 // the next segment's, on their way during this one
+    int cut = 0;
+    const auto load = [&](int n) {
+        const float* M = a.seg_m + seg(n) * KC * KC;
+        cut = a.seg_cut[seg(n)];
+        added = at(a.seg + seg(n) * sz);
 #pragma unroll
-        for (int m = 0; m < kMine; ++m) {
-            const int k = w + m * 4;
+        for (int j = 0; j < KF; ++j) {
+            if constexpr (REV) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) next[m][r] = more ? at(p, k * 16 + g4 + r) : 0.0f;
-            if (more && !cut) {
-#pragma unroll
-                for (int j = 0; j < KF; ++j) {
-                    f32x4 f;
-                    if constexpr (REV) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) f[r] = M[(j * 16 + g4 + r) * KC + k * 16 + col];
-                    } else {
-                        f = *reinterpret_cast<const f32x4*>(M + (k * 16 + col) * KC + j * 16 + g4);
-                    }
-                    const f32x4 c = cur[j][l];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) next[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], c[e], next[m], 0, 0, 0);
-                }
+                for (int r = 0; r < 4; ++r) m[j][r] = M[(j * 16 + g4 + r) * KC + w * 16 + col];
+            } else {
+                m[j] = *reinterpret_cast<const f32x4*>(M + (w * 16 + col) * KC + j * 16 + g4);
             }
         }
+    };
+    f32x4 own = at(a.entry ? a.entry + bh * sz : nullptr);
+    cur[0][w][l] = own;
+    load(0);
+    for (int n = 0; n < a.nseg; ++n) {
         __syncthreads();
+        float* p = a.seg + seg(n) * sz;
+        f32x4 next[2] = {added, f32x4{0, 0, 0, 0}};
+        if (!cut) {
 #pragma unroll
-        for (int m = 0; m < kMine; ++m) {
-            const int k = w + m * 4;
-            const f32x4 c = cur[k][l];
+            for (int j = 0; j < KF; ++j) {
+                const f32x4 c = cur[n & 1][j][l];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (k * 16 + g4 + r < a.dk && z < a.dv) p[(int64_t)(k * 16 + g4 + r) * a.dv + z] = c[r];
-            cur[k][l] = next[m];
+                for (int e = 0; e < 4; ++e) next[j & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[j][e], c[e], next[j & 1], 0, 0, 0);
+            }
         }
-        __syncthreads();
+        if (n + 2 < a.nseg) load(n + 1);                // the last segment adds to nothing
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (w * 16 + g4 + r < a.dk && z < a.dv) p[(int64_t)(w * 16 + g4 + r) * a.dv + z] = own[r];
+        own = next[0] + next[1];
+        cur[(n + 1) & 1][w][l] = own;
     }
 }
 
@@ -344,8 +340,8 @@ hipError_t grads_t(const DeltaArgs& a, hipStream_t s) {
 template <int KC>
 hipError_t chain_kc(const DeltaArgs& a, bool rev, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.batch * a.heads * ((a.dv + 15) / 16)));
-    if (rev) hipLaunchKernelGGL((delta_chain<KC, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((delta_chain<KC, false>), grid, dim3(256), 0, s, a);
+    if (rev) hipLaunchKernelGGL((delta_chain<KC, true>), grid, dim3(KC * 4), 0, s, a);
+    else hipLaunchKernelGGL((delta_chain<KC, false>), grid, dim3(KC * 4), 0, s, a);
     return hipGetLastError();
 }
 

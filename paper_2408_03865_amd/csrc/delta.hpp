@@ -8,9 +8,10 @@ namespace pm {
 
 // What a chunk's preparation (delta_prep.hip) leaves for the walks, per batch row, head and chunk: products of
 // 64 x 64 tokens as the 10 tiles of 16 x 16 on and below the diagonal, tile (i, j) at i (i + 1) / 2 + j, in the
-// order of a matrix operand: lane l, values 4 (l / 16) .. + 3 of row l % 16.
+// order of a matrix operand: lane l, values 4 (l / 16) .. + 3 of row l % 16; with bf16 inputs as a sum of bf16 terms, all tiles
+// of one term after the other.
 constexpr int kDeltaTiles = 10;
-constexpr int64_t kDeltaProduct = (int64_t)kDeltaTiles * 64 * 4;       // floats of one product
+constexpr int64_t kDeltaProduct = (int64_t)kDeltaTiles * 64 * 4;       // values of one product
 // and its tokens' weights: in, up, beta, hi, lo, start (linear_walk.hpp), then a and whether k or q is not finite
 enum : int { kCoefIn = 0, kCoefUp = 64, kCoefBeta = 128, kCoefHi = 192, kCoefLo = 256, kCoefStart = 320, kCoefA = 384, kDeltaCoef = 448 };
 
@@ -25,9 +26,9 @@ struct DeltaArgs {
     const float* entry;         // state that enters the row, or null (zeros); reverse: the final state's gradient
     float* leave;               // state that leaves it, or null; reverse: the initial state's gradient
     void* out;                  // forward: out; reverse: dv
-    // prepared products: fwd for walks in time, rev (rows and columns changed) for reverse ones
-    float* h[2];
-    float* p[2];
+    void* h;                    // prepared products
+    void* p;
+    int32_t h_terms, p_terms;
     float* coef;
     // split rows: (batch, heads, nseg) of
     float* seg;                 // the state that enters a segment (first what it adds), dk x dv
@@ -60,7 +61,7 @@ struct DeltaArgs {
 inline int32_t delta_pad(int32_t n) { return n <= 64 ? 64 : 128; }
 
 // exact: 32-bit accuracy of the states, else what a bf16 out shows of them
-hipError_t launch_delta_prep(const DeltaArgs& a, bool both, hipStream_t s);
+hipError_t launch_delta_prep(const DeltaArgs& a, hipStream_t s);
 hipError_t launch_delta_fwd(const DeltaArgs& a, bool exact, hipStream_t s);
 hipError_t launch_delta_states(const DeltaArgs& a, hipStream_t s);          // the backward's walk in time
 hipError_t launch_delta_rev(const DeltaArgs& a, hipStream_t s);

@@ -104,11 +104,16 @@ struct Taker {
     float* floats(int64_t n) { return static_cast<float*>(take(sizeof(float) * (size_t)n)); }
 };
 
+// terms of H and P: a forward takes P's first alone
+constexpr int32_t kTerms = 3;
+
 void take_common(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t rows, int64_t dk, int64_t dv, bool backward) {
-    for (int i = 0; i < (backward ? 2 : 1); ++i) {
-        a.h[i] = t.floats(p.units * pm::kDeltaProduct);
-        a.p[i] = t.floats(p.units * pm::kDeltaProduct);
-    }
+    // three terms of bf16 are more than a value of fp32
+    a.h_terms = kTerms;
+    a.p_terms = backward ? kTerms : 1;
+    const size_t h = 2 * kTerms * pm::kDeltaProduct, pr = backward ? h : 4 * pm::kDeltaProduct;
+    a.h = t.take((size_t)p.units * h);
+    a.p = t.take((size_t)p.units * pr);
     a.coef = t.floats(p.units * pm::kDeltaCoef);
     if (p.nseg > 1) {
         const int64_t pad = pm::delta_pad((int32_t)dk);
@@ -187,12 +192,14 @@ int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const 
     a.dk = (int32_t)dk; a.dv = (int32_t)dv; a.dtype = dtype;
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     set_plan(a, p);
+    const bool exact = final_state != nullptr;
+    a.h_terms = dtype == PACKMAMBA_F32 ? 1 : exact || p.nseg > 1 ? kTerms : 2;
     a.sum_segs = p.nseg - 1;
     const hipStream_t s = (hipStream_t)stream;
-    if (int e = launch_status(pm::launch_delta_prep(a, false, s))) return e;
+    if (int e = launch_status(pm::launch_delta_prep(a, s))) return e;
     if (p.nseg > 1)
         if (int e = launch_status(pm::launch_delta_segments(a, false, s))) return e;
-    return launch_status(pm::launch_delta_fwd(a, final_state != nullptr, s));
+    return launch_status(pm::launch_delta_fwd(a, exact, s));
 }
 
 size_t packmamba_delta_rule_bwd_workspace_size(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
@@ -230,9 +237,10 @@ int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const 
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     a.bound_end = dfinal_state != nullptr;
     set_plan(a, p);
+    if (dtype == PACKMAMBA_F32) a.h_terms = a.p_terms = 1;
     a.sum_segs = p.nseg;                // the reverse walk takes the last segment's multiplier too
     const hipStream_t s = (hipStream_t)stream;
-    if (int e = launch_status(pm::launch_delta_prep(a, true, s))) return e;
+    if (int e = launch_status(pm::launch_delta_prep(a, s))) return e;
     a.entry = initial_state;
     if (p.nseg > 1)
         if (int e = launch_status(pm::launch_delta_segments(a, false, s))) return e;

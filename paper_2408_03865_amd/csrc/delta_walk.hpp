@@ -39,8 +39,8 @@ struct DeltaTiles {
     using Frag = typename Mat<T>::Frag;
     __attribute__((aligned(16))) T k[KC * kC];
     __attribute__((aligned(16))) T q[Q ? KC * kC : 8];
-    Frag h[NH][kDeltaTiles][64];
-    Frag p[NP ? NP : 1][NP ? kDeltaTiles : 1][64];
+    __attribute__((aligned(16))) Frag h[NH][kDeltaTiles][64];
+    __attribute__((aligned(16))) Frag p[NP ? NP : 1][NP ? kDeltaTiles : 1][64];
     __attribute__((aligned(16))) float coef[3][kC];
     __attribute__((aligned(16))) float misc[4];
 };
@@ -60,27 +60,22 @@ struct DeltaSmem {
 
 __host__ __device__ constexpr int delta_tile(int i, int j) { return i * (i + 1) / 2 + j; }
 
-// A prepared product on its way into LDS.
+// A prepared product's first N terms on their way into LDS.
 template <typename T, int N, int THREADS>
 struct ProductRegs {
-    using M = Mat<T>;
-    static constexpr int kVecs = kDeltaTiles * 64, kPasses = (kVecs + THREADS - 1) / THREADS;
-    f32x4 w[kPasses];
-    __device__ void load(int tid, const float* p) {
-        const f32x4* v = reinterpret_cast<const f32x4*>(p);
+    using Frag = typename Mat<T>::Frag;
+    static constexpr int kVecs = N * kDeltaTiles * 64 * (int)sizeof(Frag) / 16, kPasses = (kVecs + THREADS - 1) / THREADS;
+    u32x4 w[kPasses];
+    __device__ void load(int tid, const void* p, int64_t unit, int terms) {
+        const u32x4* v = reinterpret_cast<const u32x4*>(static_cast<const Frag*>(p) + unit * terms * (kDeltaTiles * 64));
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) w[i] = v[min(i * THREADS + tid, kVecs - 1)];
     }
-    __device__ void store(int tid, typename M::Frag (*to)[kDeltaTiles][64]) const {
+    __device__ void store(int tid, Frag (*to)[kDeltaTiles][64]) const {
+        u32x4* v = reinterpret_cast<u32x4*>(to);
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int at = i * THREADS + tid;
-            if (at >= kVecs) continue;
-            typename M::Frag f[N];
-            M::template split<N>(w[i], f);
-#pragma unroll
-            for (int n = 0; n < N; ++n) to[n][0][at] = f[n];
-        }
+        for (int i = 0; i < kPasses; ++i)
+            if (kVecs % THREADS == 0 || i * THREADS + tid < kVecs) v[i * THREADS + tid] = w[i];
     }
 };
 
@@ -259,6 +254,22 @@ struct DeltaState {
     }
 };
 
+// A tile of a product as an operand, or turned: rows 4 (lane / 16) .. + 3 of it, column lane % 16.
+template <typename T, bool TURNED>
+__device__ __forceinline__ typename Mat<T>::Frag product_tile(int l, const typename Mat<T>::Frag* tile) {
+    using Frag = typename Mat<T>::Frag;
+    if constexpr (!TURNED) {
+        return tile[l];
+    } else if constexpr (sizeof(T) == 2) {
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(const_cast<Frag*>(tile + (l & 3) * 16 + (l >> 4) * 4 + ((l & 15) >> 2))));
+        return __builtin_bit_cast(u32x2, v);
+    } else {
+        const float* p = reinterpret_cast<const float*>(tile + ((l & 15) >> 2) * 16 + (l >> 4) * 4) + (l & 3);
+        return Frag{p[0], p[4], p[8], p[12]};
+    }
+}
+
 // acc[i] (token tile i) += product tiles (i, j) times y[j], over j <= i, or with REV over j >= i of the turned tiles.  The tiles'
 // chains take turns: a matrix instruction that takes the result of the one before waits for it.
 template <typename T, bool REV, int NA, int NB>
@@ -277,7 +288,7 @@ __device__ __forceinline__ void multiply_product(int lane, const typename Mat<T>
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) f[i][q] = in(i, 2 * jp + q) ? tiles[n][at(i, 2 * jp + q)][l] : Frag{};
+                for (int q = 0; q < 2; ++q) f[i][q] = in(i, 2 * jp + q) ? product_tile<T, REV>(l, tiles[n][at(i, 2 * jp + q)]) : Frag{};
 #pragma unroll
             for (int m = NB - 1; m >= 0; --m) {
                 if (n + m >= (NA > NB ? NA : NB)) continue;
@@ -418,8 +429,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     const auto load_products = [&](int chunk) {
         const int tid = here(threadIdx.x);
         const int64_t unit = bh * a.chunks + chunk;
-        hr.load(tid, a.h[0] + unit * kDeltaProduct);
-        if constexpr (kQ) pr.load(tid, a.p[0] + unit * kDeltaProduct);
+        hr.load(tid, a.h, unit, a.h_terms);
+        if constexpr (kQ) pr.load(tid, a.p, unit, a.p_terms);
     };
     const auto stage = [&](int chunk) {
         const int tid = here(threadIdx.x);
@@ -488,6 +499,10 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
         all_cut = all_cut || cut;
+        if (MODE == kDeltaSum && cut && mb > 0) {        // nothing that enters the segment leaves it
+            S.decay(true, 0.0f);
+            break;
+        }
         const bool bad = __builtin_amdgcn_readfirstlane(__float_as_int(sm.misc[1])) != 0;
         if constexpr (MODE == kDeltaStates) {
             S.keep(static_cast<T*>(a.states) + unit * KC * VP, zf);
@@ -670,8 +685,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const auto load_products = [&](int chunk) {
         const int tid = here(threadIdx.x);
         const int64_t unit = bh * a.chunks + chunk;
-        hr.load(tid, a.h[1] + unit * kDeltaProduct);
-        pr.load(tid, a.p[1] + unit * kDeltaProduct);
+        hr.load(tid, a.h, unit, a.h_terms);
+        pr.load(tid, a.p, unit, a.p_terms);
     };
     const auto stage = [&](int chunk) {
         const int tid = here(threadIdx.x);
