@@ -19,7 +19,8 @@
 // takes.  So do x, e, u and the outs: four consecutive tokens of a feature a lane.  A block's waves share the chunk's
 // K, Q, H and P in LDS, which the next chunk's loads pass through registers.
 // Rounding in bf16: operands that the state holds are split into two or three bf16 terms (16 or all 24 bits), H
-// and P too where they meet them; a plain forward rounds P, its u and the S that q meets to bf16 once.
+// and P too where they meet them; the forward rounds P and the u that it meets to bf16 once, which the outs show as
+// they show their own rounding.
 //
 // Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
 // by token from the definition, so that 0 times it reaches no other token or sequence.  A state that holds one makes x
@@ -76,6 +77,25 @@ struct ProductRegs {
 #pragma unroll
         for (int i = 0; i < kPasses; ++i)
             if (kVecs % THREADS == 0 || i * THREADS + tid < kVecs) v[i * THREADS + tid] = w[i];
+    }
+};
+
+// K's or Q's chunk on its way into LDS: as TileRegs, with one address a vector whatever the head's features are, so that no branch
+// stands between the loads and the products that they run under.
+template <typename T, int ROWS, int THREADS>
+struct FeatureRegs : TileRegs<T, ROWS, THREADS> {
+    using Base = TileRegs<T, ROWS, THREADS>;
+    __device__ void load(int tid, const T* p, int rows, int t0, int L) {
+        typedef const __attribute__((address_space(1))) char* Bytes;
+        typedef const __attribute__((address_space(1))) typename Storage<T>::Vec* Global;
+        const bool tiny = L < Base::kPer;               // rows shorter than a vector: settle() reads them
+        const Bytes base = (Bytes)(uintptr_t)(tiny ? reinterpret_cast<const T*>(&walk_zero) : p);
+        const uint32_t tok = tiny ? 0u : (uint32_t)min(t0 + (tid % Base::kLanes) * Base::kPer, L - Base::kPer), step = tiny ? 0u : (uint32_t)L;
+#pragma unroll
+        for (int i = 0; i < Base::kPasses; ++i) {
+            const uint32_t row = (uint32_t)min(tid / Base::kLanes + i * Base::kRowsPass, rows - 1);
+            Base::w[i] = *(Global)(base + (row * step + tok) * (uint32_t)sizeof(T));
+        }
     }
 };
 
@@ -209,14 +229,13 @@ struct DeltaState {
             for (int r = 0; r < 4; ++r) v[r] = x + r == zf + z ? 1.0f : 0.0f;
         });
     }
-    __device__ void decay(bool cut, float a) {
-        if (cut) {                                       // both the same for the whole wave
+    __device__ void decay(float a) {
 #pragma unroll
-            for (int k = 0; k < KF; ++k) s[k] = f32x4{0, 0, 0, 0};
-        } else {
+        for (int k = 0; k < KF; ++k) s[k] *= a;
+    }
+    __device__ void clear() {
 #pragma unroll
-            for (int k = 0; k < KF; ++k) s[k] *= a;
-        }
+        for (int k = 0; k < KF; ++k) s[k] = f32x4{0, 0, 0, 0};
     }
     // transposed, rounded to T: column z is a row of KF * 16
     template <typename T>
@@ -254,12 +273,19 @@ struct DeltaState {
     }
 };
 
+// A read that stays by itself: two of them in one instruction leave the halves of two operands side by side, and moves to part
+// them cost more than the instruction.
+template <typename F>
+__device__ __forceinline__ F alone(const F* p) {
+    return *(const volatile __attribute__((address_space(3))) F*)p;
+}
+
 // A tile of a product as an operand, or turned: rows 4 (lane / 16) .. + 3 of it, column lane % 16.
 template <typename T, bool TURNED>
 __device__ __forceinline__ typename Mat<T>::Frag product_tile(int l, const typename Mat<T>::Frag* tile) {
     using Frag = typename Mat<T>::Frag;
     if constexpr (!TURNED) {
-        return tile[l];
+        return alone(tile + l);
     } else if constexpr (sizeof(T) == 2) {
         const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (__attribute__((address_space(3))) s16x4*)(const_cast<Frag*>(tile + (l & 3) * 16 + (l >> 4) * 4 + ((l & 15) >> 2))));
@@ -314,8 +340,9 @@ __device__ __forceinline__ void add_tokens(int lane, DeltaState<KF>& S, const T*
             typename M::Frag y[4][2];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                y[q][0] = M::direct(l, tile + (k + q) * 16 * kC, 2 * p);
-                y[q][1] = M::direct(l, tile + (k + q) * 16 * kC, 2 * p + 1);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    y[q][h] = alone(reinterpret_cast<const typename M::Frag*>(tile + (k + q) * 16 * kC + M::direct_at(l, 2 * p + h)));
             }
 #pragma unroll
             for (int n = NS - 1; n >= 0; --n)
@@ -411,7 +438,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     else if (MODE == kDeltaSum) S.identity((int)(mb - 1) * VP + zf);
     else S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
 
-    TileRegs<T, KC, kThreads> kr, qr;
+    FeatureRegs<T, KC, kThreads> kr, qr;
     ProductRegs<T, NS, kThreads> hr;
     ProductRegs<T, NQ, kThreads> pr;
     TokenRegs<T> vr, dr;
@@ -420,9 +447,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     // the memory's queues can drain under
     const auto load = [&](int chunk) {
         const int tid = here(threadIdx.x);
-        const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
-        kr.load(tid, at, kp, a.dk, (int)L);
-        if constexpr (kQ) qr.load(tid, at, qp, a.dk, (int)L);
+        kr.load(tid, kp, a.dk, chunk * kC, (int)L);
+        if constexpr (kQ) qr.load(tid, qp, a.dk, chunk * kC, (int)L);
         const float* cf = a.coef + (bh * a.chunks + chunk) * kDeltaCoef;
         cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
     };
@@ -475,10 +501,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     if constexpr (kTwo) {
         stage(first);
         stage_products(first);
-        if (first < last) {
-            load(first + 1);
-            load_products(first + 1);
-        }
+        load(min(first + 1, last));
+        load_products(min(first + 1, last));
     }
     for (int chunk = first; chunk <= last; ++chunk) {
         const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
@@ -487,7 +511,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         __syncthreads();
         if (MODE == kDeltaStates && chunk > first) flush(chunk - 1);
         if constexpr (kTwo) {
-            if (chunk < last) stage(chunk + 1);
+            stage(chunk + 1);
         } else {
             stage(chunk);
             stage_products(chunk);
@@ -500,7 +524,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         const bool cut = A < 0.0f;
         all_cut = all_cut || cut;
         if (MODE == kDeltaSum && cut && mb > 0) {        // nothing that enters the segment leaves it
-            S.decay(true, 0.0f);
+            S.clear();
             break;
         }
         const bool bad = __builtin_amdgcn_readfirstlane(__float_as_int(sm.misc[1])) != 0;
@@ -525,15 +549,10 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
             M::template split<NS>(S.s[k + 1], s1);
             against_tokens<T, NS>(lk, sm.k, k, s0, s1, ak);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (kQ && NQ == 1 && NS > 1) {
-                const Frag r0[1] = {M::round(S.s[k])}, r1[1] = {M::round(S.s[k + 1])};
-                against_tokens<T, 1>(lk, sm.q, k, r0, r1, aq);
-            } else if constexpr (kQ) {
-                against_tokens<T, NQ>(lk, sm.q, k, s0, s1, aq);
-            }
+            if constexpr (kQ) against_tokens<T, NS>(lk, sm.q, k, s0, s1, aq);
         }
-        if (chunk + kTwo < last) load(chunk + 1 + kTwo);
-        if (kTwo && chunk < last) stage_products(chunk + 1);
+        load(min(chunk + 1 + kTwo, last));              // without a branch: the last chunks load theirs again
+        if (kTwo) stage_products(chunk + 1);
         const int g4c = (here(l) >> 4) * 4;
         const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4c]); };
         Frag y[4][NS], vf[4];
@@ -547,7 +566,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
         multiply_product<T, false, NS, NS>(l, sm.h, y, hx);
-        if (chunk + kTwo < last) load_products(chunk + 1 + kTwo);
+        load_products(min(chunk + 1 + kTwo, last));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] -= hx[i];                               // the errors
@@ -582,7 +601,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) M::template split<NS>(u[i] * four(1, i), y[i]);
-            S.decay(cut, A);
+            S.decay(cut ? 0.0f : A);                     // finite here
             add_tokens<T, KF, NS>(l, S, sm.k, y);
         } else {
             any_pending = false;
@@ -591,7 +610,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                 const int64_t t = ct + j;
                 bool start;
                 const float mult = token_decay(a, b, h, t, start);
-                S.decay(start, mult);
+                if (start) S.clear();
+                else S.decay(mult);
                 const float beta = t < L ? betap[t] : 0.0f;
                 const float e = (live && t < L ? Storage<T>::load1(vp + t) : 0.0f) - S.against(sm.k, j);
                 const float ut = t < L ? beta * e : 0.0f;
@@ -670,15 +690,14 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const int64_t sz = (int64_t)a.dk * a.dv;
     D.load(SUM ? nullptr : a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
 
-    TileRegs<T, KC, kThreads> kr, qr;
+    FeatureRegs<T, KC, kThreads> kr, qr;
     ProductRegs<T, NS, kThreads> hr, pr;
     TokenRegs<T> vr, dr;
     f32x4 cr, er[4];
     const auto load = [&](int chunk) {
         const int tid = here(threadIdx.x);
-        const uint32_t at = TileRegs<T, KC, kThreads>::offset_of(tid, chunk * kC, (int)L);
-        kr.load(tid, at, kp, a.dk, (int)L);
-        qr.load(tid, at, qp, a.dk, (int)L);
+        kr.load(tid, kp, a.dk, chunk * kC, (int)L);
+        qr.load(tid, qp, a.dk, chunk * kC, (int)L);
         const float* cf = a.coef + (bh * a.chunks + chunk) * kDeltaCoef;
         cr = *reinterpret_cast<const f32x4*>(cf + (tid < 48 ? tid * 4 : kCoefA));
     };
@@ -725,10 +744,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     if constexpr (kTwo) {
         stage(last);
         stage_products(last);
-        if (last > first) {
-            load(last - 1);
-            load_products(last - 1);
-        }
+        load(max(last - 1, first));
+        load_products(max(last - 1, first));
     }
     for (int chunk = last; chunk >= first; --chunk) {
         const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
@@ -737,7 +754,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         __syncthreads();
         if (!SUM && chunk < last) flush(chunk + 1);
         if constexpr (kTwo) {
-            if (chunk > first) stage(chunk - 1);
+            stage(chunk - 1);
         } else {
             stage(chunk);
             stage_products(chunk);
@@ -790,8 +807,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             M::template split<NS>(D.s[k + 1], s1);
             against_tokens<T, NS>(lk, sm.k, k, s0, s1, ak);
         }
-        if (chunk - kTwo > first) load(chunk - 1 - kTwo);
-        if (kTwo && chunk > first) stage_products(chunk - 1);
+        load(max(chunk - 1 - kTwo, first));             // without a branch: the last chunks load theirs again
+        if (kTwo) stage_products(chunk - 1);
         const int g4c = (here(l) >> 4) * 4;
         const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4c]); };
         f32x4 x[4];
@@ -813,7 +830,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
         multiply_product<T, true, NS, NS>(l, sm.h, y, hx);
-        if (chunk - kTwo > first) load_products(chunk - 1 - kTwo);
+        load_products(max(chunk - 1 - kTwo, first));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] -= hx[i];                               // du
@@ -837,7 +854,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                     store_sum16(l, &dot[1][w][i * 16 + g4], sum16(x[i] * er[i]));
                 }
             }
-            D.decay(cut, A);
+            D.decay(cut ? 0.0f : A);                     // finite here
 #pragma unroll
             for (int i = 0; i < 4; ++i) M::template split<NS>(M::widen(df[i][0]) * (four(0, i) * a.scale), y[i]);
             add_tokens<T, KF, NS>(l, D, sm.q, y);
@@ -867,7 +884,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                     }
                 }
                 D.add(sm.k, j, -dvt);
-                D.decay(start, mult);
+                if (start) D.clear();
+                else D.decay(mult);
             }
         }
     }
