@@ -90,9 +90,10 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
 // dq and dk of a chunk, from the states before and the gradients after it.  With Mo = scale (dout . u) D (pairs s <= t)
 // and Mv = -(dv . u) D (s < t), D the decay between the two tokens:
 //   dq = Mo k + scale in (S dout),   dk = Mo^T q + Mv k + Mv^T k - in (S dv) + up (D u)
-// One block a chunk, 64 features and grad_per heads of a group, whose sums stay in registers; wave w owns 16 tokens.  Mo and Mv
-// are made in both directions by the wave that needs them, as the operands they are next.
-// In bf16 u, dv and the states are rounded once; Mo and Mv are split into two terms.
+// One block a chunk, 64 features of k and grad_per heads of a group, whose sums stay in registers; wave w owns 16 tokens.  Mo
+// and Mv are made in both directions by the wave that needs them, as the operands they are next.  u is beta e: the
+// errors are what lies in memory.
+// In bf16 e, dv and the states are rounded once; Mo and Mv are split into two terms.
 // --------------------------------------------------------------------------------------------
 // v where the weight is not 0, which a masked infinity or NaN must not pass
 __device__ __forceinline__ f32x4 weighted(const f32x4& v, const f32x4& weight) {
@@ -107,10 +108,12 @@ struct GradSmem {
     __attribute__((aligned(16))) T k[64 * kC];
     __attribute__((aligned(16))) T q[64 * kC];
     __attribute__((aligned(16))) T dout[64 * kC];
-    __attribute__((aligned(16))) T u[64 * kC];
+    __attribute__((aligned(16))) T e[64 * kC];
     __attribute__((aligned(16))) T w[64 * kC];
-    __attribute__((aligned(16))) T s[64 * 64];       // the state before, features of v by features of k
-    __attribute__((aligned(16))) T d[64 * 64];       // the gradient after
+    struct {
+        __attribute__((aligned(16))) T s[64 * 64];       // the state before, features of v by features of k
+        __attribute__((aligned(16))) T d[64 * 64];       // the gradient after
+    } st;
     __attribute__((aligned(16))) float coef[kDeltaCoef];
 };
 
@@ -132,25 +135,15 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     const int f0 = half * 64, frows = min(64, a.dk - f0);
     const int vpad = a.dv <= 64 ? 64 : 128, vhalves = vpad / 64;
     const int h0 = (int)grp * rep + part * a.grad_per, h1 = min((int)(grp + 1) * rep, h0 + a.grad_per);
-    if (frows <= 0) return;
     const T* kp = static_cast<const T*>(a.k) + ((b * a.groups + grp) * a.dk + f0) * L;
     const T* qp = static_cast<const T*>(a.q) + ((b * a.groups + grp) * a.dk + f0) * L;
     const uint32_t at = Regs::offset_of(tid, (int)t0, (int)L), sat = Regs::offset_of(tid, 0, KC);
 
-    {
-        Regs kr, qr;
-        kr.load(tid, at, kp, frows, (int)L);
-        qr.load(tid, at, qp, frows, (int)L);
-        kr.settle(tid, kp, frows, t0, L);
-        qr.settle(tid, qp, frows, t0, L);
-        kr.store(tid, sm.k);
-        qr.store(tid, sm.q);
-    }
     f32x4 dq[4], dk[4];
 #pragma unroll
     for (int f = 0; f < 4; ++f) dq[f] = dk[f] = f32x4{0, 0, 0, 0};
 
-    Regs dor, ur, wr, sr, gr;
+    Regs dor, er, wr, sr, gr;
     float cr[2];
     const int steps = (h1 - h0) * vhalves;
     const auto base = [&](const void* p, int step) {
@@ -161,33 +154,42 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
         const int h = h0 + step / vhalves, v0 = step % vhalves * 64, rows = min(64, a.dv - v0);
         const int64_t unit = (b * a.heads + h) * a.chunks + chunk;
         dor.load(tid, at, base(a.dout, step), rows, (int)L);
-        ur.load(tid, at, base(a.u, step), rows, (int)L);
+        er.load(tid, at, base(a.e, step), rows, (int)L);
         wr.load(tid, at, base(a.w, step), rows, (int)L);
         sr.load(tid, sat, static_cast<const T*>(a.states) + (unit * vpad + v0) * KC + f0, 64, KC);
         gr.load(tid, sat, static_cast<const T*>(a.grads) + (unit * vpad + v0) * KC + f0, 64, KC);
         cr[0] = a.coef[unit * kDeltaCoef + tid];
         cr[1] = a.coef[unit * kDeltaCoef + min(tid + 256, kDeltaCoef - 1)];
     };
-    load(0);
+    {
+        Regs kr, qr;
+        kr.load(tid, at, kp, frows, (int)L);
+        qr.load(tid, at, qp, frows, (int)L);
+        load(0);                                        // blocks are short: all their first loads at once
+        kr.settle(tid, kp, frows, t0, L);
+        qr.settle(tid, qp, frows, t0, L);
+        kr.store(tid, sm.k);
+        qr.store(tid, sm.q);
+    }
     // Mo's tiles of the wave's 16 tokens: with the earlier ones (and its own) as rows of dq, with the later ones of dk; the
     // diagonal tile a second time for dk.  Mv's the same way.
     f32x4 mo[4], mv[4], mo_d, mv_d;
     for (int step = 0; step < steps; ++step) {
         const bool first = step % vhalves == 0, done = step % vhalves == vhalves - 1;
-        const int v0 = step % vhalves * 64, rows = min(64, a.dv - v0);
+        const int rows = min(64, a.dv - step % vhalves * 64);
         __syncthreads();
         dor.settle(tid, base(a.dout, step), rows, t0, L);
-        ur.settle(tid, base(a.u, step), rows, t0, L);
+        er.settle(tid, base(a.e, step), rows, t0, L);
         wr.settle(tid, base(a.w, step), rows, t0, L);
         dor.store(tid, sm.dout);
-        ur.store(tid, sm.u);
+        er.store(tid, sm.e);
         wr.store(tid, sm.w);
-        sr.store(tid, sm.s);
-        gr.store(tid, sm.d);
+        sr.store(tid, sm.st.s);
+        gr.store(tid, sm.st.d);
         sm.coef[tid] = cr[0];
         if (tid + 256 < kDeltaCoef) sm.coef[tid + 256] = cr[1];
         __syncthreads();
-        if (step + 1 < steps) load(step + 1);
+        load(min(step + 1, steps - 1));
         const auto c4 = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which + i * 16 + g4]); };
         const auto tok = [&](const T* tile, int k, int i) { return M::transposed(l, tile + k * 16 * kC, i); };
         if (first) {
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             dw[n] = tok(sm.dout, n, w);
-            uw[n] = tok(sm.u, n, w);
+            uw[n] = tok(sm.e, n, w);
             ww[n] = tok(sm.w, n, w);
         }
 #pragma unroll
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             if (i <= w) {
 #pragma unroll
                 for (int n = 0; n < 4; n += 2) {
-                    const Frag x0 = tok(sm.u, n, i), x1 = tok(sm.u, n + 1, i);
+                    const Frag x0 = tok(sm.e, n, i), x1 = tok(sm.e, n + 1, i);
                     mo[i] = M::mma(x0, x1, dw[n], dw[n + 1], mo[i]);
                     mv[i] = M::mma(x0, x1, ww[n], ww[n + 1], mv[i]);
                 }
@@ -225,16 +227,16 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             mv_d = M::mma(ww[n], ww[n + 1], uw[n], uw[n + 1], mv_d);
         }
         {
-            const f32x4 in = c4(kCoefIn, w), up = c4(kCoefUp, w);
+            const f32x4 in = c4(kCoefIn, w), up = c4(kCoefUp, w) * c4(kCoefBeta, w);
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
                 f32x4 q = {0, 0, 0, 0}, g = q, x = q;
 #pragma unroll
                 for (int n = 0; n < 4; n += 2) {
-                    const Frag s0 = tok(sm.s, n, f), s1 = tok(sm.s, n + 1, f);
+                    const Frag s0 = tok(sm.st.s, n, f), s1 = tok(sm.st.s, n + 1, f);
                     q = M::mma(dw[n], dw[n + 1], s0, s1, q);
                     x = M::mma(ww[n], ww[n + 1], s0, s1, x);
-                    g = M::mma(uw[n], uw[n + 1], tok(sm.d, n, f), tok(sm.d, n + 1, f), g);
+                    g = M::mma(uw[n], uw[n + 1], tok(sm.st.d, n, f), tok(sm.st.d, n + 1, f), g);
                 }
                 dq[f] += weighted(q, in) * a.scale;
                 dk[f] += weighted(g, up) - weighted(x, in);
@@ -245,13 +247,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
         {
             const int t = w * 16 + col;
             const float hi = sm.coef[kCoefHi + t], lo = sm.coef[kCoefLo + t];
+            const float beta = sm.coef[kCoefBeta + t];
             const int start = __float_as_int(sm.coef[kCoefStart + t]);
             const auto weigh = [&](int i, bool later, f32x4& o, f32x4& v) {       // later: tile i has the later tokens
-                const f32x4 hi4 = c4(kCoefHi, i), lo4 = c4(kCoefLo, i), st4 = c4(kCoefStart, i);
+                const f32x4 hi4 = c4(kCoefHi, i), lo4 = c4(kCoefLo, i), st4 = c4(kCoefStart, i), b4 = c4(kCoefBeta, i);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int s = i * 16 + g4 + r;
-                    const float d = later ? pair_decay(hi4[r], lo4[r], hi, lo) : pair_decay(hi, lo, hi4[r], lo4[r]);
+                    const float d = later ? pair_decay(hi4[r], lo4[r], hi, lo) * beta : pair_decay(hi, lo, hi4[r], lo4[r]) * b4[r];    // the earlier one's beta
                     const bool on = later ? t <= s && __float_as_int(st4[r]) <= t : s <= t && start <= s;
                     o[r] = on ? o[r] * (d * a.scale) : 0.0f;
                     v[r] = on && s != t ? -v[r] * d : 0.0f;
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
                 }
             }
         } else {                                                 // k or q not finite: pair by pair, a wave's rows of M in LDS
-            float* rows16 = reinterpret_cast<float*>(sm.s) + w * 16 * kC;
+            float* rows16 = reinterpret_cast<float*>(&sm.st) + w * 16 * kC;
             __syncthreads();
 #pragma unroll
             for (int which = 0; which < 3; ++which) {            // dq from k, dk from q, dk from k

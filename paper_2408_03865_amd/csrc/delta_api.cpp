@@ -62,8 +62,6 @@ struct Plan {
     int32_t nseg, seg_chunks, nb, heads_per, grad_per, grad_parts;
 };
 constexpr int32_t kBoundChunks = 8;     // chunks between the boundaries at which the backward multiplies the two states
-constexpr int64_t kSplitChunks = 16;    // rows of fewer are walked whole
-
 // heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks
 int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
     int64_t per = rep;
@@ -71,17 +69,45 @@ int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
     return (int32_t)per;
 }
 
-Plan make_plan(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv, int64_t seqlen) {
+// The cheapest split, in units of a chunk walked alone on a CU:
+//   - a CU holds two blocks of heads with up to 64 features of v, one with more; a chunk in company takes 1.6, and
+//     blocks beyond a round add to it;
+//   - a sum walk takes 0.75 of one in time (0.6 backwards) and needs a block more for every 64 or 128 columns of the multiplier; the
+//     chain of the segments' states 0.45 a segment, 0.6 with keys of more than 64 features;
+//   - a block costs a chunk besides its own, the launches three.
+// Us of a bf16 call by chunks a segment (batch x heads x tokens, dk x dv):
+//   forward   1 x 24 x 30001, 128 x 64: unsplit 2690, 16 856, 24 741, 32 724, 48 826    1 x 8 x 16384, 64 x 64: 687, 4 172, 8 132, 16 144
+//             1 x 64 x 8192, 128 x 128: 686, 16 579, 32 542, 64 667    2 x 24 x 4096, 64 x 64: 214, 4 146, 8 132, 16 153
+//             1 x 4 x 1024, 64 x 64: 56, 2 42, 4 46, 8 63    1 x 4 x 512: 35, 2 35, 4 43    4 x 32 x 4096, 128 x 128: 400, 16 507, 32 403
+//   backward  4 x 24 x 2048, 64 x 64: 483, 4 402, 8 384, 16 460    1 x 32 x 4096, 128 x 128: 1289, 4 616, 8 533, 16 660
+//             1 x 4 x 1024, 64 x 64: 191, 2 101, 4 122, 8 180    4 x 32 x 4096, 128 x 128: 1714, 16 1766, 32 1652
+int64_t segment_chunks(int64_t rows, int64_t dk, int64_t dv, int64_t chunks, bool backward) {
+    const double slots = dv <= 64 ? 512 : 256, company = dv <= 64 ? 1.6 : 1.0;
+    const int64_t columns = 1 + ((dk <= 64 ? 64 : 128) + (dv <= 64 ? 64 : 128) - 1) / (dv <= 64 ? 64 : 128);
+    const auto load = [&](int64_t n) { return n <= 256 ? 1.0 : (double)n <= slots ? company : company * (double)n / slots; };
+    const double walks = backward ? 2.0 : 1.0, chain = dk <= 64 ? 0.45 : 0.6;
+    int64_t best = chunks;
+    double least = walks * load(rows) * (double)(chunks + 1);
+    if (rows > 256) return best;
+    for (int64_t per = 2; per < chunks; per += (per + 2) / 3) {      // 2, 3, 4, 6, 8, 11, 15, 20, 27, ...
+        const int64_t nseg = (chunks + per - 1) / per;
+        const double block = (double)(per + 1);
+        double cost = walks * block * load(rows * nseg) + 0.75 * block * load(rows * (backward ? nseg : nseg - 1) * columns) +
+                      chain * (double)nseg + 3.0;
+        if (backward) cost += 0.6 * block * load(rows * (nseg - 1)) + chain * (double)nseg + 3.0;
+        if (cost < least) {
+            least = cost;
+            best = per;
+        }
+    }
+    return best;
+}
+
+Plan make_plan(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv, int64_t seqlen, bool backward) {
     Plan p;
     p.chunks = (seqlen + pm::kLinChunk - 1) / pm::kLinChunk;
-    const int64_t rows = batch * heads, slots = dv <= 64 ? 512 : 256;
+    const int64_t rows = batch * heads, per = segment_chunks(rows, dk, dv, p.chunks, backward);
     p.units = rows * p.chunks;
-    int64_t per = p.chunks;
-    if (p.chunks >= kSplitChunks && rows * 4 <= slots) {
-        const int64_t n = slots / rows, least = kSplitChunks / 2;
-        per = (p.chunks + n - 1) / n;
-        if (per < least) per = least;
-    }
     p.seg_chunks = (int32_t)per;
     p.nseg = (int32_t)((p.chunks + per - 1) / per);
     p.nb = (int32_t)((p.chunks + kBoundChunks - 1) / kBoundChunks);
@@ -135,9 +161,9 @@ BwdExtra take_bwd(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t batch, int6
     a.grads = t.take(size * (size_t)(p.units * state));
     a.bound = t.floats(rows * p.nb * state);
     a.dot = t.floats(rows * (p.nb + 1));
-    a.u = t.take(size * (size_t)(rows * dv * seqlen));
+    a.e = t.take(size * (size_t)(rows * dv * seqlen));
+    if (dtype != PACKMAMBA_F32) a.e_low = static_cast<uint16_t*>(t.take(2 * (size_t)(p.units * pm::kLinChunk * pm::delta_pad((int32_t)dv))));
     a.w = dtype == PACKMAMBA_BF16_F32OUT ? t.take(size * (size_t)(rows * dv * seqlen)) : nullptr;
-    a.e = t.floats(p.units * pm::kLinChunk * pm::delta_pad((int32_t)dv));
     a.rq = t.floats(rows * seqlen);
     a.rk = t.floats(rows * seqlen);
     BwdExtra x{};
@@ -168,7 +194,7 @@ size_t packmamba_delta_rule_fwd_workspace_size(int64_t batch, int64_t heads, int
     if (check_heads(batch, heads, groups, dk, dv, seqlen)) return 0;
     Taker t{nullptr};
     pm::DeltaArgs a{};
-    take_common(t, a, make_plan(batch, heads, groups, dk, dv, seqlen), batch * heads, dk, dv, false);
+    take_common(t, a, make_plan(batch, heads, groups, dk, dv, seqlen, false), batch * heads, dk, dv, false);
     return t.at;
 }
 
@@ -181,7 +207,7 @@ int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const 
     if (int e = check_heads(batch, heads, groups, dk, dv, seqlen)) return e;
     if (int e = check_dtype(dtype)) return e;
     if (!aligned16(q, k, v, beta, decay, position_indices, initial_state, out, final_state, workspace)) return PACKMAMBA_ERR_ALIGN;
-    const Plan p = make_plan(batch, heads, groups, dk, dv, seqlen);
+    const Plan p = make_plan(batch, heads, groups, dk, dv, seqlen, false);
     Taker t{static_cast<char*>(workspace)};
     pm::DeltaArgs a{};
     take_common(t, a, p, batch * heads, dk, dv, false);
@@ -207,7 +233,7 @@ size_t packmamba_delta_rule_bwd_workspace_size(int64_t batch, int64_t heads, int
     if (check_heads(batch, heads, groups, dk, dv, seqlen) || check_dtype(dtype)) return 0;
     Taker t{nullptr};
     pm::DeltaArgs a{};
-    take_bwd(t, a, make_plan(batch, heads, groups, dk, dv, seqlen), batch, heads, groups, dk, dv, seqlen, dtype);
+    take_bwd(t, a, make_plan(batch, heads, groups, dk, dv, seqlen, true), batch, heads, groups, dk, dv, seqlen, dtype);
     return t.at;
 }
 
@@ -225,7 +251,7 @@ int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const 
     if (!aligned16(q, k, v, beta, decay, position_indices, initial_state, dout, dfinal_state) ||
         !aligned16(dq, dk, dv, dbeta, ddecay, dinitial_state, workspace))
         return PACKMAMBA_ERR_ALIGN;
-    const Plan p = make_plan(batch, heads, groups, dk_size, dv_size, seqlen);
+    const Plan p = make_plan(batch, heads, groups, dk_size, dv_size, seqlen, true);
     Taker t{static_cast<char*>(workspace)};
     pm::DeltaArgs a{};
     const BwdExtra x = take_bwd(t, a, p, batch, heads, groups, dk_size, dv_size, seqlen, dtype);

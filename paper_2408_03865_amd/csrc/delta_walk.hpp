@@ -185,6 +185,79 @@ struct TokenRegs {
     }
 };
 
+// Errors whole in 32 bits: as bf16, rounded half up, which the products take, and the lower halves of the fp32 patterns, which
+// make up the rest: a pattern is the rounded one's plus its own lower half, taken for a signed number.
+__device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, bool upper) {     // of b and a, b's above
+    return __builtin_amdgcn_perm(b, a, upper ? 0x07060302u : 0x05040100u);
+}
+template <typename T>
+struct ErrorRegs {
+    TokenRegs<T> hi;
+    u32x4 lo[2];
+    __device__ void set(const f32x4 (&e)[4]) {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const u32x4 x = __builtin_bit_cast(u32x4, e[2 * i]), y = __builtin_bit_cast(u32x4, e[2 * i + 1]);
+                const u32x4 xr = x + 0x8000u, yr = y + 0x8000u;
+                uint32_t a = halves(xr.x, xr.y, true), b = halves(xr.z, xr.w, true), c = halves(yr.x, yr.y, true), d = halves(yr.z, yr.w, true);
+                TokenRegs<T>::swap(a, c);
+                TokenRegs<T>::swap(b, d);
+                hi.w[i] = u32x4{a, b, c, d};
+                lo[i] = u32x4{halves(x.x, x.y, false), halves(x.z, x.w, false), halves(y.x, y.y, false), halves(y.z, y.w, false)};
+            }
+        } else {
+            hi.set(e);
+        }
+    }
+    __device__ void get(uint32_t mask, f32x4 (&e)[4]) const {
+        typename Mat<T>::Frag f[4];
+        hi.get(mask, f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[i] = Mat<T>::widen(f[i]);
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t two = lo[i / 2][(i % 2) * 2 + r / 2] & mask;
+                    const int32_t half = r % 2 ? (int32_t)two >> 16 : (int32_t)(two << 16) >> 16;
+                    e[i][r] = __uint_as_float(__float_as_uint(e[i][r]) + (uint32_t)half);
+                }
+            }
+        }
+    }
+    // low: the chunk's and wave's
+    __device__ void store(T* row, uint16_t* low, int64_t t0, int l, int64_t L, bool live) const {
+        if (live) hi.store(row, t0, l, L);
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<u32x4*>(low + l * 16) = lo[0];
+            *reinterpret_cast<u32x4*>(low + l * 16 + 8) = lo[1];
+        }
+    }
+    __device__ void load(const T* row, const uint16_t* low, int64_t t0, int l, int64_t L) {
+        hi.load(row, t0, l, L);
+        if constexpr (sizeof(T) == 2) {
+            lo[0] = *reinterpret_cast<const u32x4*>(low + l * 16);
+            lo[1] = *reinterpret_cast<const u32x4*>(low + l * 16 + 8);
+        }
+    }
+    // one token's of the chunk, token j in a column
+    __device__ static int low_at(int j, int col) { return ((j % 16) / 4 * 16 + col) * 16 + j / 16 * 4 + j % 4; }
+    __device__ static void put(T* at, uint16_t* low, int j, int col, float e) {
+        if constexpr (sizeof(T) == 2) {
+            at->bits = (uint16_t)((__float_as_uint(e) + 0x8000u) >> 16);
+            low[low_at(j, col)] = (uint16_t)__float_as_uint(e);
+        } else {
+            *at = e;
+        }
+    }
+    __device__ static float take(const T* at, const uint16_t* low, int j, int col) {
+        if constexpr (sizeof(T) == 2)
+            return __uint_as_float(((uint32_t)at->bits << 16) + (uint32_t)(int32_t)(int16_t)low[low_at(j, col)]);
+        else return *at;
+    }
+};
+
 // v at four consecutive tokens t.. of a row
 template <typename TO>
 __device__ __forceinline__ void store_tokens(TO* row, int64_t t, int64_t L, const f32x4& v) {
@@ -429,7 +502,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     const T* vp = static_cast<const T*>(a.v) + zrow * L;
     const T* dop = MODE == kDeltaStates ? static_cast<const T*>(a.dout) + zrow * L : nullptr;
     TO* op = MODE == kDeltaOut ? static_cast<TO*>(a.out) + zrow * L : nullptr;
-    T* up = MODE == kDeltaStates ? static_cast<T*>(a.u) + zrow * L : nullptr;
+    T* ep = MODE == kDeltaStates ? static_cast<T*>(a.e) + zrow * L : nullptr;
+    const auto low = [&](int64_t unit) { return a.e_low + (unit * kWaves + w) * 1024; };
     const float* betap = a.beta + bh * L;
 
     DeltaState<KF> S;
@@ -575,11 +649,9 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         if (!bad && !any_nonfinite(u)) {
             if constexpr (kQ) {
                 if constexpr (MODE == kDeltaStates) {
-                    TokenRegs<T> ur;
-                    ur.set(u);
-                    if (live) ur.store(up, ct, here(l), L);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4) = x[i];
+                    ErrorRegs<T> er;
+                    er.set(x);
+                    er.store(ep, low(unit), ct, here(l), L, live);
                 }
                 Frag uf[4][NQ];
                 f32x4 o[4];
@@ -624,10 +696,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                     } else {
                         const float d = lanes16(live && t < L ? o * Storage<T>::load1(dop + t) : 0.0f);
                         if (l == 0) dot[w][j] = d;
-                        if (g4 == 0) {
-                            if (mine) Storage<T>::store1(up + t, ut);
-                            a.e[(((unit * kWaves + w) * 4 + j / 16) * 64 + (j % 16) / 4 * 16 + col) * 4 + j % 4] = t < L ? e : 0.0f;
-                        }
+                        if (mine) ErrorRegs<T>::put(ep + t, low(unit), j, col, e);
                     }
                 }
             }
@@ -683,6 +752,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const T* vp = static_cast<const T*>(a.v) + zrow * L;
     const T* dop = static_cast<const T*>(a.dout) + zrow * L;
     TO* op = SUM ? nullptr : static_cast<TO*>(a.out) + zrow * L;
+    const T* ep = SUM ? nullptr : static_cast<const T*>(a.e) + zrow * L;
+    const auto low = [&](int64_t unit) { return a.e_low + (unit * kWaves + w) * 1024; };
     T* wp = SUM || !a.w ? nullptr : static_cast<T*>(a.w) + zrow * L;      // a copy in T, where the out has another type
     const float* betap = a.beta + bh * L;
 
@@ -693,7 +764,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     FeatureRegs<T, KC, kThreads> kr, qr;
     ProductRegs<T, NS, kThreads> hr, pr;
     TokenRegs<T> vr, dr;
-    f32x4 cr, er[4];
+    ErrorRegs<T> er;
+    f32x4 cr;
     const auto load = [&](int chunk) {
         const int tid = here(threadIdx.x);
         kr.load(tid, kp, a.dk, chunk * kC, (int)L);
@@ -789,8 +861,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         if constexpr (!kTwo) __syncthreads();
         if constexpr (!SUM) {                            // needed late in the chunk
             vr.load(vp, ct, here(l), L);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) er[i] = *reinterpret_cast<const f32x4*>(a.e + (((unit * kWaves + w) * 4 + i) * 64 + l) * 4);
+            er.load(ep, low(unit), ct, here(l), L);
         }
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
@@ -849,10 +920,11 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                 Frag vf[4];
                 vr.get(mask, vf);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    store_sum16(l, &dot[0][w][i * 16 + g4], sum16(M::widen(vf[i]) * dv[i]));
-                    store_sum16(l, &dot[1][w][i * 16 + g4], sum16(x[i] * er[i]));
-                }
+                for (int i = 0; i < 4; ++i) store_sum16(l, &dot[0][w][i * 16 + g4], sum16(M::widen(vf[i]) * dv[i]));
+                f32x4 e[4];
+                er.get(mask, e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) store_sum16(l, &dot[1][w][i * 16 + g4], sum16(x[i] * e[i]));
             }
             D.decay(cut ? 0.0f : A);                     // finite here
 #pragma unroll
@@ -872,7 +944,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                 D.add(sm.q, j, d * a.scale);
                 const float du = D.against(sm.k, j), dvt = in ? betap[t] * du : 0.0f;
                 if constexpr (!SUM) {
-                    const float et = a.e[(((unit * kWaves + w) * 4 + j / 16) * 64 + (j % 16) / 4 * 16 + col) * 4 + j % 4];
+                    const float et = in && live ? ErrorRegs<T>::take(ep + t, low(unit), j, col) : 0.0f;
                     const float vd = lanes16(in && live ? Storage<T>::load1(vp + t) * dvt : 0.0f), db = lanes16(in && live ? du * et : 0.0f);
                     if (l == 0) {
                         dot[0][w][j] = vd;
