@@ -130,13 +130,13 @@ struct Taker {
     float* floats(int64_t n) { return static_cast<float*>(take(sizeof(float) * (size_t)n)); }
 };
 
-// terms of H and P: a forward takes P's first alone
-constexpr int32_t kTerms = 3;
+// terms of H and P, and of a forward's P
+constexpr int32_t kTerms = 3, kOutTerms = 2;
 
 void take_common(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t rows, int64_t dk, int64_t dv, bool backward) {
     // three terms of bf16 are more than a value of fp32
     a.h_terms = kTerms;
-    a.p_terms = backward ? kTerms : 1;
+    a.p_terms = backward ? kTerms : kOutTerms;
     const size_t h = 2 * kTerms * pm::kDeltaProduct, pr = backward ? h : 4 * pm::kDeltaProduct;
     a.h = t.take((size_t)p.units * h);
     a.p = t.take((size_t)p.units * pr);
@@ -219,7 +219,8 @@ int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const 
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     set_plan(a, p);
     const bool exact = final_state != nullptr;
-    a.h_terms = dtype == PACKMAMBA_F32 ? 1 : exact || p.nseg > 1 ? kTerms : 2;
+    a.h_terms = exact || p.nseg > 1 ? kTerms : 2;
+    if (dtype == PACKMAMBA_F32) a.h_terms = a.p_terms = 1;
     a.sum_segs = p.nseg - 1;
     const hipStream_t s = (hipStream_t)stream;
     if (int e = launch_status(pm::launch_delta_prep(a, s))) return e;

@@ -18,9 +18,9 @@
 // k's features, in registers, in the layout that an MFMA result has and, four rows of it a lane, an MFMA operand
 // takes.  So do x, e, u and the outs: four consecutive tokens of a feature a lane.  A block's waves share the chunk's
 // K, Q, H and P in LDS, which the next chunk's loads pass through registers.
-// Rounding in bf16: operands that the state holds are split into two or three bf16 terms (16 or all 24 bits), H
-// and P too where they meet them; the forward rounds P and the u that it meets to bf16 once, which the outs show as
-// they show their own rounding.
+// Rounding in bf16: what is no input is split into two or three bf16 terms (16 or all 24 bits): the state, H, P, x and u.  The
+// outs and the errors are small differences of their terms where keys are near each other, and a term rounded to
+// bf16 would show (heads of one feature, P and u rounded once: outs 4.9e-3 off in the 2-norm, split 1.7e-3).
 //
 // Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
 // by token from the definition, so that 0 times it reaches no other token or sequence.  A state that holds one makes x
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     using Frag = typename M::Frag;
     constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
     constexpr bool kQ = MODE != kDeltaSum;
-    constexpr int NQ = MODE == kDeltaStates ? NS : 1;       // terms of what the outs are made of
+    constexpr int NQ = MODE == kDeltaStates || NS == 1 ? NS : 2;        // terms of what the outs are made of
     using Smem = DeltaSmem<T, KC, VP, NS, kQ ? NQ : 0, kQ, MODE == kDeltaStates ? 1 : 0>;
     constexpr bool kTwo = Smem::kBuffers == 2;
     __shared__ Smem smem;

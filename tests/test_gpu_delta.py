@@ -10,7 +10,8 @@ Tolerances, element by element, with M the budgets of delta_reference and u = 2^
 The budgets are sums of norms, far above most elements, so results of 1000 elements and more are held in the 2-norm as well:
 roundings to bf16 (four at most, each of at most 2^-8 and spread over it evenly: 2^-8 / sqrt 3 of the norm) 2 2^-8 / sqrt 3,
 32-bit ones 2e-5.  That is a mean over elements: a single one can be the small difference of two rounded terms (0.13 of
-2.4, with one token and one feature), where the element's bound alone says something.
+2.4, with one token and one feature), where the element's bound alone says something.  So is ddecay where decays are strong: it is
+what sums of out . dout and v . dv leave, of the size of a token's multiplier; at e^-7 of those sums their 1e-6 is 1e-3 of it.
 """
 import numpy as np
 import pytest
@@ -69,7 +70,7 @@ def bound_of(ref, mag, shape, name, rounded):
     return bound + 3 * HALF * mag + HALF * ref.abs() if rounded else bound
 
 
-def check(got, ref, mag, shape, name, rounded):
+def check(got, ref, mag, shape, name, rounded, norm=1.0):
     got = got.double().cpu()
     assert got.shape == ref.shape, (name, got.shape, ref.shape)
     assert bool(got.isfinite().all()), name
@@ -77,8 +78,8 @@ def check(got, ref, mag, shape, name, rounded):
     rel = ((got - ref).norm() / ref.norm().clamp(min=1e-300)).item()
     note(f"  {name} {over:.2g} of its bound, {rel:.2g} off")
     assert over <= 1, f"{name}: error {over:.2f} of its bound"
-    if ref.numel() >= 1000 and ref.norm() > 0:
-        assert rel <= (2 * HALF / 3 ** 0.5 if rounded else 2e-5), f"{name}: {rel:.2g} off"
+    if norm and ref.numel() >= 1000 and ref.norm() > 0:
+        assert rel <= norm * (2 * HALF / 3 ** 0.5 if rounded else 2e-5), f"{name}: {rel:.2g} off"
 
 
 def rounded_name(name, dtype):
