@@ -354,7 +354,7 @@ int packmamba_layernorm_fwd(const void* x, const float* weight, const float* bia
 
 size_t packmamba_layernorm_bwd_workspace_size(int64_t batch, int64_t dim, int64_t seqlen, int32_t dtype) {
     if (check_norm(batch, dim, seqlen, 1) || check_dtype(dtype)) return 0;
-    return floats(pm::norm_tiles(batch, dim, seqlen, dtype == PACKMAMBA_F32) * 2 * dim);
+    return floats(pm::norm_tiles(batch, seqlen, dtype == PACKMAMBA_F32) * 2 * dim);
 }
 
 int packmamba_layernorm_bwd(const void* x, const float* weight, const float* mean, const float* rstd, const void* dout,

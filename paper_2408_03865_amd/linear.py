@@ -29,7 +29,7 @@ def _check(device, tensors):
             continue
         if t.dtype != dtype:
             raise TypeError(f"{name} is {t.dtype}, not {dtype}")
-        if tuple(t.shape) != shape:
+        if t.shape != shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, not {shape}")
         if t.device != device:
             raise ValueError(f"{name} is on {t.device}, not on {device}")

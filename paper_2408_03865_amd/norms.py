@@ -59,7 +59,8 @@ def layernorm_fwd(x, weight, bias=None, eps: float = 1e-5, out_f32: bool = False
     _check(device, [("weight", weight, (Dn,), torch.float32), ("bias", bias, (Dn,), torch.float32)])
     code = _code(x, out_f32)
     out = _empty_out(x, out_f32)
-    mean, rstd = (torch.empty((Nb, L), dtype=torch.float32, device=device) for _ in range(2))
+    mean = torch.empty((Nb, L), dtype=torch.float32, device=device)
+    rstd = torch.empty_like(mean)
     _call(device, "packmamba_layernorm_fwd", _p(x), _p(weight), _p(bias), float(eps), _p(out), _p(mean), _p(rstd), Nb, Dn, L,
           code, _stream(x))
     return out, mean, rstd
