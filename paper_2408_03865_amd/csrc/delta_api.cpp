@@ -71,7 +71,7 @@ int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
 
 // The cheapest split, in units of a chunk walked alone on a CU:
 //   - a CU holds two blocks of heads with up to 64 features of v, one with more; a chunk in company takes 1.6, and
-//     blocks beyond a round add to it;
+//     blocks beyond a round follow as others end, with half a block's wait;
 //   - a sum walk takes 0.75 of one in time (0.6 backwards) and needs a block more for every 64 or 128 columns of the multiplier; the
 //     chain of the segments' states 0.45 a segment, 0.6 with keys of more than 64 features;
 //   - a block costs a chunk besides its own, the launches three.
@@ -84,7 +84,7 @@ int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
 int64_t segment_chunks(int64_t rows, int64_t dk, int64_t dv, int64_t chunks, bool backward) {
     const double slots = dv <= 64 ? 512 : 256, company = dv <= 64 ? 1.6 : 1.0;
     const int64_t columns = 1 + ((dk <= 64 ? 64 : 128) + (dv <= 64 ? 64 : 128) - 1) / (dv <= 64 ? 64 : 128);
-    const auto load = [&](int64_t n) { return n <= 256 ? 1.0 : (double)n <= slots ? company : company * (double)n / slots; };
+    const auto load = [&](int64_t n) { return n <= 256 ? 1.0 : (double)n <= slots ? company : company * (double)n / slots + 0.5; };
     const double walks = backward ? 2.0 : 1.0, chain = dk <= 64 ? 0.45 : 0.6;
     int64_t best = chunks;
     double least = walks * load(rows) * (double)(chunks + 1);

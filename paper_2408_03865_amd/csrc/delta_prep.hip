@@ -14,16 +14,12 @@
 namespace pm {
 namespace {
 
-#ifndef PREP_WAVES
-#define PREP_WAVES 3
-#endif
-
 __host__ __device__ constexpr int tile_at(int i, int j) { return i * (i + 1) / 2 + j; }
 
-__device__ __forceinline__ f32x4 mma16(const f32x4& a, const f32x4& b, f32x4 c) {
+// A product of blocks, added to two sums in turns: an instruction that takes the result of the one before waits for it.
+__device__ __forceinline__ void mma16(const f32x4& a, const f32x4& b, f32x4 (&c)[2]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-    return c;
+    for (int e = 0; e < 4; ++e) c[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c[e & 1], 0, 0, 0);
 }
 
 // The keys and queries are done with once their products are in registers.
@@ -36,7 +32,7 @@ struct PrepSmem {
     struct Solve {
         f32x4 a[kDeltaTiles][64];           // A as operands
         f32x4 hd[4][64];                    // H's diagonal blocks as operands
-        __attribute__((aligned(16))) float rows[4][16][16];     // A's diagonal blocks
+        __attribute__((aligned(16))) float cols[4][16][20];     // A's diagonal blocks by columns
         __attribute__((aligned(16))) float turn[4][16][20];
     };
     union {
@@ -71,12 +67,13 @@ __device__ __forceinline__ void put_tile(void* p, int64_t unit, int terms, int t
 
 // One block a chunk and heads_per heads of one group.  Wave j takes the tiles of column j.
 template <typename T, int KC>
-__global__ __launch_bounds__(256, PREP_WAVES) void delta_prep_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(256, 3) void delta_prep_kernel(DeltaArgs a) {
     using M = Mat<T>;
     using Frag = typename M::Frag;
     constexpr int KT = KC / 16;
     __shared__ PrepSmem<T, KC> sm;
-    const int l = lane_id(), w = wave_id(), g4 = (l >> 4) * 4, col = l & 15;
+    // the columns have four to one tiles: blocks of a CU start with different ones, so that no SIMD has all the long ones
+    const int l = lane_id(), w = (wave_id() + (int)blockIdx.x) & 3, g4 = (l >> 4) * 4, col = l & 15;
     const int64_t L = a.seqlen;
     const int rep = a.heads / a.groups, parts = (rep + a.heads_per - 1) / a.heads_per;
     const uint32_t id = blockIdx.x, per = (uint32_t)(a.groups * parts);
@@ -116,22 +113,21 @@ __global__ __launch_bounds__(256, PREP_WAVES) void delta_prep_kernel(DeltaArgs a
         __syncthreads();
         if (qr.zero_sum(kr.zero_sum(0.0f)) != 0.0f) sm.bad = 1;
     }
-    // products of column w's tokens with the later ones: as operands (f: lane = later token) and as results (c)
-    f32x4 kf[4], kc[4], qf[4];
+    // products of column w's tokens with the later ones, as operands (a lane is a later token)
+    f32x4 kf[4], qf[4];
     {
         Frag ks[KT];
 #pragma unroll
         for (int k = 0; k < KT; ++k) ks[k] = M::transposed(l, sm.in.k + k * 16 * kC, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            kf[i] = kc[i] = qf[i] = f32x4{0, 0, 0, 0};
+            kf[i] = qf[i] = f32x4{0, 0, 0, 0};
             if (i < w) continue;
 #pragma unroll
             for (int k = 0; k < KT; k += 2) {
                 const Frag k0 = M::transposed(l, sm.in.k + k * 16 * kC, i), k1 = M::transposed(l, sm.in.k + (k + 1) * 16 * kC, i);
                 const Frag q0 = M::transposed(l, sm.in.q + k * 16 * kC, i), q1 = M::transposed(l, sm.in.q + (k + 1) * 16 * kC, i);
                 kf[i] = M::mma(ks[k], ks[k + 1], k0, k1, kf[i]);
-                kc[i] = M::mma(k0, k1, ks[k], ks[k + 1], kc[i]);
                 qf[i] = M::mma(ks[k], ks[k + 1], q0, q1, qf[i]);
             }
         }
@@ -163,32 +159,28 @@ __global__ __launch_bounds__(256, PREP_WAVES) void delta_prep_kernel(DeltaArgs a
             }
         }
         // weighted: A and P
-        f32x4 ac[4];
         {
-            const int s1 = w * 16 + col, s4 = w * 16 + g4;
-            const float hi1 = c.hi[s1], lo1 = c.lo[s1];
+            const int s4 = w * 16 + g4;
             const f32x4 hi4 = *reinterpret_cast<const f32x4*>(&c.hi[s4]), lo4 = *reinterpret_cast<const f32x4*>(&c.lo[s4]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                ac[i] = f32x4{0, 0, 0, 0};
                 if (i < w) continue;
-                const int t1 = i * 16 + col, t4 = i * 16 + g4;
+                const int t1 = i * 16 + col, start = c.start[t1];
                 const float thi = c.hi[t1], tlo = c.lo[t1];
-                const f32x4 thi4 = *reinterpret_cast<const f32x4*>(&c.hi[t4]), tlo4 = *reinterpret_cast<const f32x4*>(&c.lo[t4]);
                 f32x4 af, pv;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float d = pair_decay(thi, tlo, hi4[r], lo4[r]);
-                    const bool on = takes<false>(c, t1, s4 + r);
+                    const bool on = s4 + r <= t1 && start <= s4 + r;
                     af[r] = on && s4 + r < t1 ? kf[i][r] * d : 0.0f;
                     pv[r] = on ? qf[i][r] * (d * a.scale) : 0.0f;
-                    const float d4 = pair_decay(thi4[r], tlo4[r], hi1, lo1);
-                    const bool on4 = takes<false>(c, t4 + r, s1);
-                    ac[i][r] = on4 && s1 < t4 + r ? kc[i][r] * d4 : 0.0f;
                 }
                 sm.at.a[tile_at(i, w)][l] = af;
                 put_tile<T>(a.p, unit, a.p_terms, tile_at(i, w), pv);
-                if (i == w) *reinterpret_cast<f32x4*>(&sm.at.rows[w][col][g4]) = af;
+                if (i == w) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sm.at.cols[w][g4 + r][col] = af[r];
+                }
             }
         }
         __syncthreads();
@@ -206,14 +198,24 @@ __global__ __launch_bounds__(256, PREP_WAVES) void delta_prep_kernel(DeltaArgs a
         };
         f32x4 own;
         {
-            float x[16], xb[16];
+            float x[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float v = sm.at.rows[w][i][col];
+            for (int i = 0; i < 16; i += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(&sm.at.cols[w][col][i]);
 #pragma unroll
-                for (int m = 0; m < i; ++m) v = fmaf(-sm.at.rows[w][i][m], xb[m], v);
-                x[i] = v;
-                xb[i] = v * betas[w * 16 + i];
+                for (int r = 0; r < 4; ++r) x[i + r] = v[r];
+            }
+            // a row that is done leaves those below it: what waits for the row before is one product a row
+#pragma unroll
+            for (int i = 0; i < 15; ++i) {
+                const float xb = x[i] * betas[w * 16 + i];
+#pragma unroll
+                for (int q = i / 4 * 4; q < 16; q += 4) {
+                    const f32x4 below = *reinterpret_cast<const f32x4*>(&sm.at.cols[w][i][q]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (q + r > i) x[q + r] = fmaf(-below[r], xb, x[q + r]);
+                }
             }
             const int g = l >> 4;
 #pragma unroll
@@ -235,11 +237,17 @@ __global__ __launch_bounds__(256, PREP_WAVES) void delta_prep_kernel(DeltaArgs a
             if (i < w) continue;
             f32x4 hc = own;
             if (i != w) {
-                f32x4 y = ac[i];
+                f32x4 y[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};      // A_ij as a result: the operand turned
+                const float* at = reinterpret_cast<const float*>(&sm.at.a[tile_at(i, w)][(col >> 2) * 16 + g4]) + (col & 3);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[0][r] = at[r * 4];
 #pragma unroll
                 for (int k = 0; k < i; ++k)
-                    if (k >= w) y = mma16(sm.at.a[tile_at(i, k)][l], nb[k], y);
-                hc = mma16(sm.at.hd[i][l], y * -beta4(i), y);
+                    if (k >= w) mma16(sm.at.a[tile_at(i, k)][l], nb[k], y);
+                y[0] += y[1];
+                y[1] = f32x4{0, 0, 0, 0};
+                mma16(sm.at.hd[i][l], y[0] * -beta4(i), y);
+                hc = y[0] + y[1];
                 put_tile<T>(a.h, unit, a.h_terms, tile_at(i, w), turned(hc));
             }
             nb[i] = hc * -beta4(i);
