@@ -32,7 +32,7 @@
  * Arithmetic: products accumulate in 32 bits and the state is held in 32 bits.  With bf16 inputs out, dq, dk
  * and dv have bf16's accuracy, also where PACKMAMBA_BF16_F32OUT returns 32 bits; final states, the initial
  * state's gradient and those of beta and the decays have 32-bit accuracy for all types (a decay's gradient
- * that of the sums of out . dout and v . dv that it is left of, over up to 512 tokens).  The same call
+ * that of the sums of out . dout and v . dv that it is left of, over up to 256 tokens).  The same call
  * gives the same bits; with another choice of the optional outputs other kernels may run, and bf16
  * results may differ within their accuracy.
  * An infinity or NaN at token t reaches no other sequence and no other head (of q or k: no other group), and in

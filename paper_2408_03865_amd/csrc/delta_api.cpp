@@ -61,7 +61,11 @@ struct Plan {
     int64_t chunks, units;
     int32_t nseg, seg_chunks, nb, heads_per, grad_per, grad_parts;
 };
-constexpr int32_t kBoundChunks = 8;     // chunks between the boundaries at which the backward multiplies the two states
+// Chunks between the boundaries at which the backward multiplies the two states.  A decay's gradient is a sum over the tokens up
+// to the next, of terms that cancel: its error grows with their number, and the boundaries' fp32 states move memory.  8 rows of
+// 4096 tokens, 32 heads of 128 x 128: 2 chunks 2480 us, 4 chunks 2375 us and 7.8e-7 off in the 2-norm, 8 chunks 2340 us and 1.0e-6
+// (token by token in fp32: 5.6e-7).
+constexpr int32_t kBoundChunks = 4;
 // heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks
 int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
     int64_t per = rep;
@@ -69,32 +73,32 @@ int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
     return (int32_t)per;
 }
 
-// The cheapest split, in units of a chunk walked alone on a CU:
-//   - a CU holds two blocks of heads with up to 64 features of v, one with more; a chunk in company takes 1.6, and
-//     blocks beyond a round follow as others end, with half a block's wait;
-//   - a sum walk takes 0.75 of one in time (0.6 backwards) and needs a block more for every 64 or 128 columns of the multiplier; the
-//     chain of the segments' states 0.45 a segment, 0.6 with keys of more than 64 features;
-//   - a block costs a chunk besides its own, the launches three.
+// The cheapest split, in units of a chunk walked alone on a CU (with these, the figures below to within 10%):
+//   - a CU holds two blocks of heads with up to 64 features of v, one with more; a chunk in company takes 1.35, and
+//     blocks beyond a round add to it, in the walks that end a call with a quarter of a block's wait besides;
+//   - a sum walk takes 0.7 of one in time (0.3 backwards) and needs a block more for every 64 or 128 columns of the
+//     multiplier; the chain of the segments' states 0.5 a segment;
+//   - a block costs a chunk besides its own, the launches two.
 // Us of a bf16 call by chunks a segment (batch x heads x tokens, dk x dv):
-//   forward   1 x 24 x 30001, 128 x 64: unsplit 2690, 16 856, 24 741, 32 724, 48 826    1 x 8 x 16384, 64 x 64: 687, 4 172, 8 132, 16 144
+//   forward   1 x 24 x 30001, 128 x 64: unsplit 2690, 20 815, 22 805, 27 736, 36 765    1 x 8 x 16384, 64 x 64: 687, 4 172, 8 132, 16 144
 //             1 x 64 x 8192, 128 x 128: 686, 16 579, 32 542, 64 667    2 x 24 x 4096, 64 x 64: 214, 4 146, 8 132, 16 153
 //             1 x 4 x 1024, 64 x 64: 56, 2 42, 4 46, 8 63    1 x 4 x 512: 35, 2 35, 4 43    4 x 32 x 4096, 128 x 128: 400, 16 507, 32 403
 //   backward  4 x 24 x 2048, 64 x 64: 483, 4 402, 8 384, 16 460    1 x 32 x 4096, 128 x 128: 1289, 4 616, 8 533, 16 660
 //             1 x 4 x 1024, 64 x 64: 191, 2 101, 4 122, 8 180    4 x 32 x 4096, 128 x 128: 1714, 16 1766, 32 1652
 int64_t segment_chunks(int64_t rows, int64_t dk, int64_t dv, int64_t chunks, bool backward) {
-    const double slots = dv <= 64 ? 512 : 256, company = dv <= 64 ? 1.6 : 1.0;
+    const double slots = dv <= 64 ? 512 : 256, company = dv <= 64 ? 1.35 : 1.0;
     const int64_t columns = 1 + ((dk <= 64 ? 64 : 128) + (dv <= 64 ? 64 : 128) - 1) / (dv <= 64 ? 64 : 128);
-    const auto load = [&](int64_t n) { return n <= 256 ? 1.0 : (double)n <= slots ? company : company * (double)n / slots + 0.5; };
-    const double walks = backward ? 2.0 : 1.0, chain = dk <= 64 ? 0.45 : 0.6;
+    const auto load = [&](int64_t n) { return n <= 256 ? 1.0 : (double)n <= slots ? company : company * (double)n / slots; };
+    const double walks = backward ? 2.0 : 1.0, chain = 0.5;
     int64_t best = chunks;
     double least = walks * load(rows) * (double)(chunks + 1);
     if (rows > 256) return best;
     for (int64_t per = 2; per < chunks; per += (per + 2) / 3) {      // 2, 3, 4, 6, 8, 11, 15, 20, 27, ...
         const int64_t nseg = (chunks + per - 1) / per;
         const double block = (double)(per + 1);
-        double cost = walks * block * load(rows * nseg) + 0.75 * block * load(rows * (backward ? nseg : nseg - 1) * columns) +
-                      chain * (double)nseg + 3.0;
-        if (backward) cost += 0.6 * block * load(rows * (nseg - 1)) + chain * (double)nseg + 3.0;
+        const double walk = load(rows * nseg) + ((double)(rows * nseg) > slots ? 0.25 : 0.0);
+        double cost = walks * block * walk + 0.7 * block * load(rows * (backward ? nseg : nseg - 1) * columns) + chain * (double)nseg + 2.0;
+        if (backward) cost += 0.3 * block * load(rows * (nseg - 1)) + chain * (double)nseg + 2.0;
         if (cost < least) {
             least = cost;
             best = per;
