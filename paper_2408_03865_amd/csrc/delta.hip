@@ -127,13 +127,12 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
     const int64_t L = a.seqlen;
     const int rep = a.heads / a.groups, parts = (rep + a.grad_per - 1) / a.grad_per;
-    const uint32_t id = blockIdx.x, n_in = (uint32_t)(a.groups * parts * kHalves);
-    const uint32_t bc = id / n_in, in_id = id - bc * n_in;
-    const int64_t b = bc / (uint32_t)a.chunks, chunk = bc - b * a.chunks;
-    const int half = (int)(in_id % kHalves), gp = (int)(in_id / kHalves), part = gp % parts;
-    const int64_t grp = gp / parts, t0 = chunk * kC;
+    const uint32_t id = chunk_block(kHalves), unit_id = id / kHalves, row = unit_id / (uint32_t)a.chunks;
+    const uint32_t bg = row / (uint32_t)parts, bat = bg / (uint32_t)a.groups;
+    const int64_t b = bat, chunk = unit_id - row * (uint32_t)a.chunks, grp = bg - bat * (uint32_t)a.groups, t0 = chunk * kC;
+    const int half = (int)(id % kHalves), part = (int)(row - bg * (uint32_t)parts);
     const int f0 = half * 64, frows = min(64, a.dk - f0);
-    const int vpad = a.dv <= 64 ? 64 : 128, vhalves = vpad / 64;
+    const int vpad = a.dv <= 64 ? 64 : 128, vshift = a.dv <= 64 ? 0 : 1;
     const int h0 = (int)grp * rep + part * a.grad_per, h1 = min((int)(grp + 1) * rep, h0 + a.grad_per);
     const T* kp = static_cast<const T*>(a.k) + ((b * a.groups + grp) * a.dk + f0) * L;
     const T* qp = static_cast<const T*>(a.q) + ((b * a.groups + grp) * a.dk + f0) * L;
@@ -145,13 +144,13 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
 
     Regs dor, er, wr, sr, gr;
     float cr[2];
-    const int steps = (h1 - h0) * vhalves;
+    const int steps = (h1 - h0) << vshift;
     const auto base = [&](const void* p, int step) {
-        const int h = h0 + step / vhalves, v0 = step % vhalves * 64;
+        const int h = h0 + (step >> vshift), v0 = (step & vshift) * 64;
         return static_cast<const T*>(p) + ((b * a.heads + h) * a.dv + v0) * L;
     };
     const auto load = [&](int step) {
-        const int h = h0 + step / vhalves, v0 = step % vhalves * 64, rows = min(64, a.dv - v0);
+        const int h = h0 + (step >> vshift), v0 = (step & vshift) * 64, rows = min(64, a.dv - v0);
         const int64_t unit = (b * a.heads + h) * a.chunks + chunk;
         dor.load(tid, at, base(a.dout, step), rows, (int)L);
         er.load(tid, at, base(a.e, step), rows, (int)L);
@@ -175,8 +174,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     // diagonal tile a second time for dk.  Mv's the same way.
     f32x4 mo[4], mv[4], mo_d, mv_d;
     for (int step = 0; step < steps; ++step) {
-        const bool first = step % vhalves == 0, done = step % vhalves == vhalves - 1;
-        const int rows = min(64, a.dv - step % vhalves * 64);
+        const bool first = (step & vshift) == 0, done = (step & vshift) == vshift;
+        const int rows = min(64, a.dv - (step & vshift) * 64);
         __syncthreads();
         dor.settle(tid, base(a.dout, step), rows, t0, L);
         er.settle(tid, base(a.e, step), rows, t0, L);
@@ -249,20 +248,26 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             const float hi = sm.coef[kCoefHi + t], lo = sm.coef[kCoefLo + t];
             const float beta = sm.coef[kCoefBeta + t];
             const int start = __float_as_int(sm.coef[kCoefStart + t]);
-            const auto weigh = [&](int i, bool later, f32x4& o, f32x4& v) {       // later: tile i has the later tokens
+            // tile i's pairs, whose tokens are the later ones or the earlier: no condition is a branch
+            const auto weigh = [&](auto side, int i, f32x4& o, f32x4& v) {
+                constexpr bool kLater = decltype(side)::value;
                 const f32x4 hi4 = c4(kCoefHi, i), lo4 = c4(kCoefLo, i), st4 = c4(kCoefStart, i), b4 = c4(kCoefBeta, i);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int s = i * 16 + g4 + r;
-                    const float d = later ? pair_decay(hi4[r], lo4[r], hi, lo) * beta : pair_decay(hi, lo, hi4[r], lo4[r]) * b4[r];    // the earlier one's beta
-                    const bool on = later ? t <= s && __float_as_int(st4[r]) <= t : s <= t && start <= s;
-                    o[r] = on ? o[r] * (d * a.scale) : 0.0f;
-                    v[r] = on && s != t ? -v[r] * d : 0.0f;
+                    const float d = kLater ? pair_decay(hi4[r], lo4[r], hi, lo) * beta : pair_decay(hi, lo, hi4[r], lo4[r]) * b4[r];    // the earlier one's beta
+                    const int on = kLater ? (int)(t <= s) & (int)(__float_as_int(st4[r]) <= t) : (int)(s <= t) & (int)(start <= s);
+                    const float od = o[r] * (d * a.scale), vd = -v[r] * d;
+                    o[r] = on ? od : 0.0f;
+                    v[r] = on & (int)(s != t) ? vd : 0.0f;
                 }
             };
 #pragma unroll
-            for (int i = 0; i < 4; ++i) weigh(i, i > w, mo[i], mv[i]);
-            weigh(w, true, mo_d, mv_d);
+            for (int i = 0; i < 4; ++i) {
+                if (i <= w) weigh(std::false_type{}, i, mo[i], mv[i]);
+                else weigh(std::true_type{}, i, mo[i], mv[i]);
+            }
+            weigh(std::true_type{}, w, mo_d, mv_d);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (i == w) mv[i] += mv_d;               // each is 0 where the other is not

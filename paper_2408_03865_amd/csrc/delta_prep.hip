@@ -76,11 +76,10 @@ __global__ __launch_bounds__(256, 3) void delta_prep_kernel(DeltaArgs a) {
     const int l = lane_id(), w = (wave_id() + (int)blockIdx.x) & 3, g4 = (l >> 4) * 4, col = l & 15;
     const int64_t L = a.seqlen;
     const int rep = a.heads / a.groups, parts = (rep + a.heads_per - 1) / a.heads_per;
-    const uint32_t id = blockIdx.x, per = (uint32_t)(a.groups * parts);
-    const uint32_t bc = id / per, gp = id - bc * per;
-    const int64_t b = bc / (uint32_t)a.chunks, chunk = bc - b * a.chunks, grp = gp / (uint32_t)parts;
-    const int part = (int)(gp - grp * parts);
-    const int64_t t0 = chunk * kC;
+    const uint32_t id = chunk_block(1), row = id / (uint32_t)a.chunks;
+    const uint32_t bg = row / (uint32_t)parts, bat = bg / (uint32_t)a.groups;
+    const int64_t b = bat, chunk = id - row * (uint32_t)a.chunks, grp = bg - bat * (uint32_t)a.groups, t0 = chunk * kC;
+    const int part = (int)(row - bg * (uint32_t)parts);
     const T* kp = static_cast<const T*>(a.k) + (b * a.groups + grp) * a.dk * L;
     const T* qp = static_cast<const T*>(a.q) + (b * a.groups + grp) * a.dk * L;
     const int h0 = (int)grp * rep + part * a.heads_per, h1 = min((int)(grp + 1) * rep, h0 + a.heads_per);

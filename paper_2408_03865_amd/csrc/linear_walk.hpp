@@ -412,6 +412,13 @@ __device__ __forceinline__ uint32_t walk_block(uint32_t n) {
     return id < per * 8 ? (id % 8) * per + id / 8 : id;
 }
 
+// The same for blocks of single chunks, `inner` blocks a chunk: eight chunks in a row to an XCD, whose pieces of 128 bytes make
+// up 1 KB of a feature's row, and all blocks of a chunk.
+__device__ __forceinline__ uint32_t chunk_block(uint32_t inner) {
+    const uint32_t id = blockIdx.x, span = 64 * inner, r = id % span, first = id - r;
+    return first + span <= gridDim.x ? first + (r % 8) * (8 * inner) + r / 8 : id;
+}
+
 // --------------------------------------------------------------------------------------------
 // the state: 16 z features a wave, and of the x features all or half: KF tiles of 16 by 16
 // --------------------------------------------------------------------------------------------
