@@ -8,8 +8,7 @@ namespace pm {
 
 // What a chunk's preparation (delta_prep.hip) leaves for the walks, per batch row, head and chunk: products of
 // 64 x 64 tokens as the 10 tiles of 16 x 16 on and below the diagonal, tile (i, j) at i (i + 1) / 2 + j, in the
-// order of a matrix operand: lane l, values 4 (l / 16) .. + 3 of row l % 16; with bf16 inputs as a sum of bf16 terms, all tiles
-// of one term after the other.
+// order of a matrix operand: lane l, values 4 (l / 16) .. + 3 of row l % 16.
 constexpr int kDeltaTiles = 10;
 constexpr int64_t kDeltaProduct = (int64_t)kDeltaTiles * 64 * 4;       // values of one product
 // and its tokens' weights: in, up, beta, hi, lo, start (linear_walk.hpp), then a and whether k or q is not finite
@@ -26,9 +25,7 @@ struct DeltaArgs {
     const float* entry;         // state that enters the row, or null (zeros); reverse: the final state's gradient
     float* leave;               // state that leaves it, or null; reverse: the initial state's gradient
     void* out;                  // forward: out; reverse: dv
-    void* h;                    // prepared products
-    void* p;
-    int32_t h_terms, p_terms;
+    float* products;            // H, then P, of every chunk
     float* coef;
     // split rows: (batch, heads, nseg) of
     float* seg;                 // the state that enters a segment (first what it adds), dk x dv

@@ -138,16 +138,8 @@ struct Taker {
     float* floats(int64_t n) { return static_cast<float*>(take(sizeof(float) * (size_t)n)); }
 };
 
-// terms of H and P, and of a forward's P
-constexpr int32_t kTerms = 3, kOutTerms = 2;
-
-void take_common(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t rows, int64_t dk, int64_t dv, bool backward) {
-    // three terms of bf16 are more than a value of fp32
-    a.h_terms = kTerms;
-    a.p_terms = backward ? kTerms : kOutTerms;
-    const size_t h = 2 * kTerms * pm::kDeltaProduct, pr = backward ? h : 4 * pm::kDeltaProduct;
-    a.h = t.take((size_t)p.units * h);
-    a.p = t.take((size_t)p.units * pr);
+void take_common(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t rows, int64_t dk, int64_t dv) {
+    a.products = t.floats(p.units * 2 * pm::kDeltaProduct);
     a.coef = t.floats(p.units * pm::kDeltaCoef);
     if (p.nseg > 1) {
         const int64_t pad = pm::delta_pad((int32_t)dk);
@@ -164,7 +156,7 @@ BwdExtra take_bwd(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t batch, int6
                   int64_t seqlen, int32_t dtype) {
     const int64_t rows = batch * heads, state = (int64_t)pm::delta_pad((int32_t)dk) * pm::delta_pad((int32_t)dv);
     const size_t size = dtype == PACKMAMBA_F32 ? 4 : 2;
-    take_common(t, a, p, rows, dk, dv, true);
+    take_common(t, a, p, rows, dk, dv);
     a.states = t.take(size * (size_t)(p.units * state));
     a.grads = t.take(size * (size_t)(p.units * state));
     a.bound = t.floats(rows * p.nb * state);
@@ -202,7 +194,7 @@ size_t packmamba_delta_rule_fwd_workspace_size(int64_t batch, int64_t heads, int
     if (check_heads(batch, heads, groups, dk, dv, seqlen)) return 0;
     Taker t{nullptr};
     pm::DeltaArgs a{};
-    take_common(t, a, make_plan(batch, heads, groups, dk, dv, seqlen, false), batch * heads, dk, dv, false);
+    take_common(t, a, make_plan(batch, heads, groups, dk, dv, seqlen, false), batch * heads, dk, dv);
     return t.at;
 }
 
@@ -218,7 +210,7 @@ int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const 
     const Plan p = make_plan(batch, heads, groups, dk, dv, seqlen, false);
     Taker t{static_cast<char*>(workspace)};
     pm::DeltaArgs a{};
-    take_common(t, a, p, batch * heads, dk, dv, false);
+    take_common(t, a, p, batch * heads, dk, dv);
     if (!workspace || workspace_bytes < t.at) return PACKMAMBA_ERR_WORKSPACE;
     a.q = q; a.k = k; a.v = v; a.beta = beta; a.decay = decay; a.pos = position_indices;
     a.entry = initial_state; a.leave = final_state; a.out = out; a.scale = scale;
@@ -227,8 +219,6 @@ int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const 
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     set_plan(a, p);
     const bool exact = final_state != nullptr;
-    a.h_terms = exact || p.nseg > 1 ? kTerms : 2;
-    if (dtype == PACKMAMBA_F32) a.h_terms = a.p_terms = 1;
     a.sum_segs = p.nseg - 1;
     const hipStream_t s = (hipStream_t)stream;
     if (int e = launch_status(pm::launch_delta_prep(a, s))) return e;
@@ -272,7 +262,6 @@ int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const 
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     a.bound_end = dfinal_state != nullptr;
     set_plan(a, p);
-    if (dtype == PACKMAMBA_F32) a.h_terms = a.p_terms = 1;
     a.sum_segs = p.nseg;                // the reverse walk takes the last segment's multiplier too
     const hipStream_t s = (hipStream_t)stream;
     if (int e = launch_status(pm::launch_delta_prep(a, s))) return e;

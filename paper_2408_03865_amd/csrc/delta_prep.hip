@@ -44,25 +44,9 @@ struct PrepSmem {
     int bad;
 };
 
-// A product's tile, in `terms` terms.
-template <typename T>
-__device__ __forceinline__ void put_tile(void* p, int64_t unit, int terms, int tile, const f32x4& v) {
-    using M = Mat<T>;
-    typename M::Frag* to = static_cast<typename M::Frag*>(p) + (unit * terms * kDeltaTiles + tile) * 64 + lane_id();
-    const auto put = [&](auto n) {
-        constexpr int N = decltype(n)::value;
-        typename M::Frag f[N];
-        M::template split<N>(v, f);
-#pragma unroll
-        for (int i = 0; i < N; ++i) to[i * kDeltaTiles * 64] = f[i];
-    };
-    if constexpr (M::kSplit) {
-        if (terms == 3) put(std::integral_constant<int, 3>{});
-        else if (terms == 2) put(std::integral_constant<int, 2>{});
-        else put(std::integral_constant<int, 1>{});
-    } else {
-        put(std::integral_constant<int, 1>{});
-    }
+// A tile of one of the two products.
+__device__ __forceinline__ void put_tile(const DeltaArgs& a, int64_t unit, int which, int tile, const f32x4& v) {
+    reinterpret_cast<f32x4*>(a.products)[(unit * 2 + which) * (kDeltaProduct / 4) + tile * 64 + lane_id()] = v;
 }
 
 // One block a chunk and heads_per heads of one group.  Wave j takes the tiles of column j.
@@ -175,7 +159,7 @@ __global__ __launch_bounds__(256, 3) void delta_prep_kernel(DeltaArgs a) {
                     pv[r] = on ? qf[i][r] * (d * a.scale) : 0.0f;
                 }
                 sm.at.a[tile_at(i, w)][l] = af;
-                put_tile<T>(a.p, unit, a.p_terms, tile_at(i, w), pv);
+                put_tile(a, unit, 1, tile_at(i, w), pv);
                 if (i == w) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) sm.at.cols[w][g4 + r][col] = af[r];
@@ -223,7 +207,7 @@ __global__ __launch_bounds__(256, 3) void delta_prep_kernel(DeltaArgs a) {
         {
             const f32x4 f = turned(own);
             sm.at.hd[w][l] = f;
-            put_tile<T>(a.h, unit, a.h_terms, tile_at(w, w), f);
+            put_tile(a, unit, 0, tile_at(w, w), f);
         }
         __syncthreads();
         if (w == 3 && h + 1 < h1) {                     // this wave has no blocks below its diagonal one
@@ -247,7 +231,7 @@ __global__ __launch_bounds__(256, 3) void delta_prep_kernel(DeltaArgs a) {
                 y[1] = f32x4{0, 0, 0, 0};
                 mma16(sm.at.hd[i][l], y[0] * -beta4(i), y);
                 hc = y[0] + y[1];
-                put_tile<T>(a.h, unit, a.h_terms, tile_at(i, w), turned(hc));
+                put_tile(a, unit, 0, tile_at(i, w), turned(hc));
             }
             nb[i] = hc * -beta4(i);
         }

@@ -61,22 +61,35 @@ struct DeltaSmem {
 
 __host__ __device__ constexpr int delta_tile(int i, int j) { return i * (i + 1) / 2 + j; }
 
-// A prepared product's first N terms on their way into LDS.
-template <typename T, int N, int THREADS>
+// The prepared products on their way into LDS, H in NH terms and, unless NP is 0, P in NP.
+template <typename T, int NH, int NP, int THREADS>
 struct ProductRegs {
-    using Frag = typename Mat<T>::Frag;
-    static constexpr int kVecs = N * kDeltaTiles * 64 * (int)sizeof(Frag) / 16, kPasses = (kVecs + THREADS - 1) / THREADS;
-    u32x4 w[kPasses];
-    __device__ void load(int tid, const void* p, int64_t unit, int terms) {
-        const u32x4* v = reinterpret_cast<const u32x4*>(static_cast<const Frag*>(p) + unit * terms * (kDeltaTiles * 64));
+    using M = Mat<T>;
+    using Frag = typename M::Frag;
+    static constexpr int kOne = (int)kDeltaProduct / 4, kVecs = (NP ? 2 : 1) * kOne, kPasses = (kVecs + THREADS - 1) / THREADS;
+    f32x4 w[kPasses];
+    __device__ void load(int tid, const float* p, int64_t unit) {
+        const f32x4* v = reinterpret_cast<const f32x4*>(p) + unit * (2 * kOne);
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) w[i] = v[min(i * THREADS + tid, kVecs - 1)];
     }
-    __device__ void store(int tid, Frag (*to)[kDeltaTiles][64]) const {
-        u32x4* v = reinterpret_cast<u32x4*>(to);
+    template <int N>
+    __device__ static void put(const f32x4& v, Frag* to) {
+        Frag f[N];
+        M::template split<N>(v, f);
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i)
-            if (kVecs % THREADS == 0 || i * THREADS + tid < kVecs) v[i * THREADS + tid] = w[i];
+        for (int n = 0; n < N; ++n) to[n * kOne] = f[n];
+    }
+    __device__ void store(int tid, Frag* h, Frag* p) const {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {             // a wave's lanes have one tile
+            const int at = i * THREADS + tid;
+            if ((i + 1) * THREADS <= kOne || __builtin_amdgcn_readfirstlane(at) < kOne) {
+                put<NH>(w[i], h + at);
+            } else if constexpr (NP != 0) {
+                if (kVecs % THREADS == 0 || __builtin_amdgcn_readfirstlane(at) < kVecs) put<NP>(w[i], p + (at - kOne));
+            }
+        }
     }
 };
 
@@ -513,8 +526,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     else S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
 
     FeatureRegs<T, KC, kThreads> kr, qr;
-    ProductRegs<T, NS, kThreads> hr;
-    ProductRegs<T, NQ, kThreads> pr;
+    ProductRegs<T, NS, kQ ? NQ : 0, kThreads> hr;
     TokenRegs<T> vr, dr;
     f32x4 cr;
     // K, Q and the weights; H and P, which are needed later: half the loads at a time, each after products that
@@ -529,8 +541,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     const auto load_products = [&](int chunk) {
         const int tid = here(threadIdx.x);
         const int64_t unit = bh * a.chunks + chunk;
-        hr.load(tid, a.h, unit, a.h_terms);
-        if constexpr (kQ) pr.load(tid, a.p, unit, a.p_terms);
+        hr.load(tid, a.products, unit);
     };
     const auto stage = [&](int chunk) {
         const int tid = here(threadIdx.x);
@@ -547,8 +558,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     const auto stage_products = [&](int chunk) {
         const int tid = here(threadIdx.x);
         auto& sm = smem.b[kTwo ? (chunk - first) & 1 : 0];
-        hr.store(tid, sm.h);
-        if constexpr (kQ) pr.store(tid, sm.p);
+        hr.store(tid, &sm.h[0][0][0], &sm.p[0][0][0]);
     };
     const auto flush = [&](int chunk) {
         if constexpr (MODE == kDeltaStates) {
@@ -762,7 +772,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     D.load(SUM ? nullptr : a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
 
     FeatureRegs<T, KC, kThreads> kr, qr;
-    ProductRegs<T, NS, kThreads> hr, pr;
+    ProductRegs<T, NS, NS, kThreads> hr;
     TokenRegs<T> vr, dr;
     ErrorRegs<T> er;
     f32x4 cr;
@@ -776,8 +786,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const auto load_products = [&](int chunk) {
         const int tid = here(threadIdx.x);
         const int64_t unit = bh * a.chunks + chunk;
-        hr.load(tid, a.h, unit, a.h_terms);
-        pr.load(tid, a.p, unit, a.p_terms);
+        hr.load(tid, a.products, unit);
     };
     const auto stage = [&](int chunk) {
         const int tid = here(threadIdx.x);
@@ -792,8 +801,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const auto stage_products = [&](int chunk) {
         const int tid = here(threadIdx.x);
         auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
-        pr.store(tid, sm.p);
-        hr.store(tid, sm.h);
+        hr.store(tid, &sm.h[0][0][0], &sm.p[0][0][0]);
     };
     const auto flush = [&](int chunk) {
         if constexpr (!SUM) {

@@ -30,10 +30,10 @@ def test_header_and_binding_agree():
 def test_sizes():
     lib = _lib()
     fwd, bwd = lib.packmamba_delta_rule_fwd_workspace_size, lib.packmamba_delta_rule_bwd_workspace_size
-    one = 2 * 10 * 64 * 4                                       # a term of a chunk's product: 10 tiles of 64 x 4 bf16
-    assert fwd(8, 64, 8, 128, 64, 4096) >= 8 * 64 * 64 * (5 * one + 448 * 4)
-    assert fwd(1, 4, 4, 64, 64, 64 * 64) >= 4 * 64 * (5 * one + 448 * 4) + 4 * 3 * (2 * 64 * 64 + 1) * 4    # segments
-    assert bwd(2, 6, 2, 128, 64, 300, 0) >= 2 * 6 * 5 * (6 * one + 2 * 128 * 64 * 4) + 2 * 6 * 64 * 300 * 4
+    two = 2 * 10 * 64 * 4 * 4                                   # a chunk's two products: 10 tiles of 64 x 4 values
+    assert fwd(8, 64, 8, 128, 64, 4096) >= 8 * 64 * 64 * (two + 448 * 4)
+    assert fwd(1, 4, 4, 64, 64, 64 * 64) >= 4 * 64 * (two + 448 * 4) + 4 * 3 * (2 * 64 * 64 + 1) * 4        # segments
+    assert bwd(2, 6, 2, 128, 64, 300, 0) >= 2 * 6 * 5 * (two + 2 * 128 * 64 * 4) + 2 * 6 * 64 * 300 * 4
     assert bwd(2, 6, 2, 128, 64, 300, 1) < bwd(2, 6, 2, 128, 64, 300, 2) < bwd(2, 6, 2, 128, 64, 300, 0)
     assert bwd(2, 6, 2, 128, 64, 300, 3) == 0
     bad = [(0, 8, 8, 64, 64, 64), (1, 8, 3, 64, 64, 64), (1, 8, 8, 129, 64, 64), (1, 8, 8, 64, 0, 64), (1, 8, 8, 64, 64, -1),
@@ -42,7 +42,7 @@ def test_sizes():
     for shape in bad:
         assert fwd(*shape) == 0 and bwd(*shape, 1) == 0, shape
     assert fwd(1, 16, 16, 8, 8, 1 << 22) > 0 and fwd(1 << 20, 1, 1, 8, 8, 64) > 0       # the limits themselves
-    # linear in the chunks, whatever the split: products 32 KB, two states 128, errors 32, pieces of two gradients 64, a boundary 8,
+    # linear in the chunks, whatever the split: products 22 KB, two states 128, errors 32, pieces of two gradients 64, a boundary 16,
     # a segment of two chunks or more 128
     for shape in ((1, 1, 1, 128, 128, 1 << 22), (1, 16, 2, 128, 128, 1 << 22), (1 << 10, 64, 64, 128, 128, 1024), (3, 5, 5, 128, 128, 100)):
         units = shape[0] * shape[1] * -(-shape[5] // 64)
