@@ -29,60 +29,88 @@ hipError_t walk(const DeltaArgs& a, DeltaWalk which, hipStream_t s) {
 // split rows: the state that enters each segment, cur <- M cur + added (nothing of cur where a sequence starts in
 // the segment), in place of what is added; backwards with M's transpose.  A block takes 16 columns of the state of one
 // row and head, its waves 16 rows each; products in 32 bits.
+// What bounds it: a step's way through LDS, 32 matrix instructions in 32 bits (16 with keys of 64) and a block's 64 KB of M, on their
+// way for one step: 24 heads of 128 x 64 in 18 segments 51 us (the sums one after the other, M loaded after the products: 66),
+// 96 of 64 x 64 in four 8.6.
 // --------------------------------------------------------------------------------------------
 template <int KC, bool REV>
 __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
     constexpr int KF = KC / 16;
     __shared__ f32x4 cur[2][KF][64];
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4;
-    const int cols = (a.dv + 15) / 16;
-    const int64_t bh = blockIdx.x / cols;
-    const int z = (int)(blockIdx.x - bh * cols) * 16 + col;
+    const uint32_t cols = (uint32_t)(a.dv + 15) / 16, id = walk_block(gridDim.x);      // a state's blocks on one XCD: they read the same M
+    const int64_t bh = id / cols;
+    const int z = (int)(id % cols) * 16 + col;
     const int64_t sz = (int64_t)a.dk * a.dv;
     const auto seg = [&](int n) { return bh * a.nseg + (REV ? a.nseg - 1 - n : n); };
+    bool live[4];
+    int place[4];                                       // in the state, of a row and column that it has
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        live[r] = w * 16 + g4 + r < a.dk && z < a.dv;
+        place[r] = min(w * 16 + g4 + r, a.dk - 1) * a.dv + min(z, a.dv - 1);
+    }
     const auto at = [&](const float* p) {
         f32x4 v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = p && w * 16 + g4 + r < a.dk && z < a.dv ? p[(int64_t)(w * 16 + g4 + r) * a.dv + z] : 0.0f;
+        for (int r = 0; r < 4; ++r) v[r] = p[place[r]];
         return v;
     };
-    f32x4 m[KF], added;                                 // the next segment's, on their way during this one
-    int cut = 0;
-    const auto load = [&](int n) {
+    const auto lives = [&](f32x4 v) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = live[r] ? v[r] : 0.0f;
+        return v;
+    };
+    f32x4 m[2][KF], added[2];                           // the segment's and the next one's, on their way
+    int cut[2];
+    const auto load = [&](auto slot, int n) {           // without a branch, which would have all loads waited for at once
+        constexpr int i = decltype(slot)::value;
+        n = min(n, a.nseg - 2);                         // the last segment adds to nothing
         const float* M = a.seg_m + seg(n) * KC * KC;
-        cut = a.seg_cut[seg(n)];
-        added = at(a.seg + seg(n) * sz);
+        cut[i] = a.seg_cut[seg(n)];
+        added[i] = at(a.seg + seg(n) * sz);
 #pragma unroll
         for (int j = 0; j < KF; ++j) {
             if constexpr (REV) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) m[j][r] = M[(j * 16 + g4 + r) * KC + w * 16 + col];
+                for (int r = 0; r < 4; ++r) m[i][j][r] = M[(j * 16 + g4 + r) * KC + w * 16 + col];
             } else {
-                m[j] = *reinterpret_cast<const f32x4*>(M + (w * 16 + col) * KC + j * 16 + g4);
+                m[i][j] = *reinterpret_cast<const f32x4*>(M + (w * 16 + col) * KC + j * 16 + g4);
             }
         }
     };
-    f32x4 own = at(a.entry ? a.entry + bh * sz : nullptr);
-    cur[0][w][l] = own;
-    load(0);
-    for (int n = 0; n < a.nseg; ++n) {
+    f32x4 own = {0, 0, 0, 0};
+    if (a.entry) own = lives(at(a.entry + bh * sz));
+    using std::integral_constant;
+    const auto step = [&](auto slot, int n) {
+        constexpr int i = decltype(slot)::value;
+        const f32x4 before = own;
+        load(integral_constant<int, 1 - i>{}, n + 1);
+        cur[i][w][l] = own;
         __syncthreads();
-        float* p = a.seg + seg(n) * sz;
-        f32x4 next[2] = {added, f32x4{0, 0, 0, 0}};
-        if (!cut) {
+        f32x4 c[KF], sum[4];
 #pragma unroll
-            for (int j = 0; j < KF; ++j) {
-                const f32x4 c = cur[n & 1][j][l];
+        for (int j = 0; j < KF; ++j) c[j] = cur[i][j][l];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) next[j & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[j][e], c[e], next[j & 1], 0, 0, 0);
-            }
+        for (int j = 0; j < 4; ++j) sum[j] = f32x4{0, 0, 0, 0};
+        if (!cut[i]) {                                  // the sums in turns: a matrix instruction waits for the one whose result it takes
+#pragma unroll
+            for (int j = 0; j < KF; j += 4)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) sum[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i][j + q][e], c[j + q][e], sum[q], 0, 0, 0);
         }
-        if (n + 2 < a.nseg) load(n + 1);                // the last segment adds to nothing
+        own = lives(added[i]) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        float* p = a.seg + seg(n) * sz;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (w * 16 + g4 + r < a.dk && z < a.dv) p[(int64_t)(w * 16 + g4 + r) * a.dv + z] = own[r];
-        own = next[0] + next[1];
-        cur[(n + 1) & 1][w][l] = own;
+            if (live[r]) p[place[r]] = before[r];
+    };
+    load(integral_constant<int, 0>{}, 0);
+    for (int n = 0; n < a.nseg; n += 2) {               // what follows the last segment is left
+        step(integral_constant<int, 0>{}, n);
+        if (n + 1 < a.nseg) step(integral_constant<int, 1>{}, n + 1);
     }
 }
 
