@@ -123,7 +123,7 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
 // errors are what lies in memory.
 // In bf16 e, dv and the states are rounded once; Mo and Mv are split into two terms.
 // What bounds it: the waves' own work between two barriers a step, with two blocks a CU (59 KB of LDS): 8 x 4096 tokens, 32 heads
-// of 128 x 128 in 16 groups, 665 to 692 us for 2.4 GB, 3.5 TB/s; masks of the weights where there are no zeros and conditions as
+// of 128 x 128 in 16 groups, 665 to 692 us for 2.4 GB, 3.5 TB/s (VALU 52%, LDS 32%, matrix 22%); masks of the weights where there are no zeros and conditions as
 // branches 815 us; all 128 features of k in a block of eight waves 836 (then 755).
 // --------------------------------------------------------------------------------------------
 // 0 where the weight is, which an infinity or NaN must not pass

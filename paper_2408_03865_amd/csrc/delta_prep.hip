@@ -10,8 +10,8 @@
 // all in 32 bits: A's inverse can be far larger than A where keys repeat.  P = scale D_ts q_t . k_s, on the diagonal too.
 // A block takes a chunk and the heads of a group in turn, whose keys' products it makes once.
 // What bounds it: 8 x 4096 tokens, 32 heads in 16 groups of 128 features, 181 us for 630 MB, 3.5 TB/s, with the waves at the barriers
-// between weights, diagonal blocks and the others half the time (VALU 36%, LDS 32%, matrix 13%); four blocks a CU and not three
-// 178 to 183.  Blocks that start with the same column on each SIMD: 230; the 32-bit products kept as three bf16 terms, as the
+// between weights, diagonal blocks and the others half the time (VALU 38%, LDS 34%, matrix 13%); four blocks a CU and not three
+// change calls by less than 1%.  Blocks that start with the same column on each SIMD: 230; the 32-bit products kept as three bf16 terms, as the
 // walks take them: 205, and 20 KB more of memory a chunk and walk.
 #include "linear_walk.hpp"
 #include "delta.hpp"

@@ -27,8 +27,8 @@
 //   outs    443 us   VALU 53%, matrix 36%, LDS 28%; 1.13 GB, 2.5 TB/s
 //   states  730 us   VALU 46%, matrix 32%, LDS 18%; 2.45 GB, 3.3 TB/s
 //   reverse 860 us   VALU 43%, matrix 24%, LDS 19%; 2.74 GB, 3.2 TB/s
-// VALU work is three quarters splitting of states, errors and products; three terms hold the gradients' accuracy.  One set of operands
-// in LDS and two barriers a chunk took 600 us for the forward (then 540), loads that branch on a head's size 427 (then 405).
+// Nearly half of the VALU work is splitting of states, errors and products, in three terms for the gradients' accuracy.  Loads that
+// branch on a head's size: outs 427 (then 405).
 //
 // Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
 // by token from the definition, so that 0 times it reaches no other token or sequence.  A state that holds one makes x
