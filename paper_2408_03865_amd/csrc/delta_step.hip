@@ -1,11 +1,10 @@
 // delta_step.hip -- the gated delta rule for one token a sequence, in 32 bits: with S' = a S,
 //   u = beta (v - S'^T k),  S <- S' + k u^T,  out = scale S^T q = scale (S'^T q + (k . q) u),
 // the state (dk, dv) of every batch row and head read and written in place.
-// Bound by the state's bytes, 8 dk dv a head.  A block takes one head of one batch row, or some of its columns where heads
-// are few: LPR lanes of four consecutive columns side by side, 256 / LPR rows at once.  All of a thread's rows, eight
-// at most, stay in registers between the two products with the state, which are summed over the rows
-// together, and its update; 96 registers a thread leave room for five blocks a CU (64 x 32 heads of 128 x 128: 61 us, 4.4 TB/s of
-// states read and written; with the 203 that the compiler takes by itself 92).
+// Bound by the state's bytes, 8 dk dv a head.  A block takes 64 columns of one head of one batch row: 16 lanes of four consecutive
+// ones side by side, 16 rows at once.  All of a thread's rows, eight at most, stay in registers between the two products with the
+// state, which are summed over the rows together, and its update; 96 registers a thread leave room for five blocks a CU (64 x 32
+// heads of 128 x 128: 59 us, 4.6 TB/s of states read and written; with the 203 that the compiler takes by itself 92).
 #include "common.hpp"
 #include "delta.hpp"
 
@@ -13,12 +12,13 @@ namespace pm {
 namespace {
 
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
-constexpr int kThreads = 256;
+// Lanes beside each other: with four, 24 heads of 64 x 64 take 3.9 us and not 4.1, 64 of 128 x 128 6.6 and not 4.8.
+constexpr int kThreads = 256, LPR = 16;
 constexpr float kStepCut = -104.0f;      // as a chunk's decays: exp of it is 0 in 32 bits
 
 // WHOLE: a row of the state is whole vectors, 16-byte aligned; else vectors have an element's alignment and a row's
 // last columns go one by one.
-template <typename T, typename TO, bool WHOLE, int LPR>
+template <typename T, typename TO, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 5) void delta_step_kernel(DeltaStepArgs a) {
     constexpr int VEC = 4, R = kThreads / LPR, kCols = LPR * VEC, kRows = (kLinMaxHead + R - 1) / R, kWaves = kThreads / 64;
     __shared__ float qk[2][kLinMaxHead];
@@ -131,18 +131,11 @@ __global__ __launch_bounds__(kThreads, 5) void delta_step_kernel(DeltaStepArgs a
     }
 }
 
-template <typename T, typename TO, bool WHOLE, int LPR>
-hipError_t step_one(const DeltaStepArgs& a, hipStream_t s) {
-    const int64_t parts = (a.dv + LPR * 4 - 1) / (LPR * 4);
-    hipLaunchKernelGGL((delta_step_kernel<T, TO, WHOLE, LPR>), dim3((unsigned)((int64_t)a.batch * a.heads * parts)), dim3(kThreads),
-                       0, s, a);
-    return hipGetLastError();
-}
-
-// 64 columns of the state in 16-byte vectors, or 16 where the heads alone leave most CUs idle.
 template <typename T, typename TO, bool WHOLE>
 hipError_t step_w(const DeltaStepArgs& a, hipStream_t s) {
-    return (int64_t)a.batch * a.heads <= 64 ? step_one<T, TO, WHOLE, 4>(a, s) : step_one<T, TO, WHOLE, 16>(a, s);
+    const int64_t parts = (a.dv + LPR * 4 - 1) / (LPR * 4);
+    hipLaunchKernelGGL((delta_step_kernel<T, TO, WHOLE>), dim3((unsigned)((int64_t)a.batch * a.heads * parts)), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
 }
 template <typename T, typename TO>
 hipError_t step_t(const DeltaStepArgs& a, hipStream_t s) {

@@ -421,6 +421,7 @@ hipError_t bwd_one(const NormArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// 64 threads a row or 256.  Us of the layer norm: 64 x 512 4.0, 4.3; 64 x 768 4.9, 4.5.
 template <typename T, typename TO, int KIND>
 hipError_t token_t(const NormArgs& a, hipStream_t s) {
     if (a.dim <= 64 * Storage<T>::kPerVec)
@@ -430,13 +431,18 @@ hipError_t token_t(const NormArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Threads of a layer norm's block by its features, many with more of them kept or few.  Us (batch x features x tokens, bf16;
+// forward, backward) with 1024 threads and with 256, tiles of 128 bytes: 8 x 256 x 4096 17, 23 and 9.6, 16; x 512 21, 32 and
+// 17, 33; x 768 26, 40 and 29, 43.  With 1024 and with 512, tiles of 64 bytes: 4 x 512 x 2048 9.8, 13 and 8.0, 11; x 768 11, 15
+// and 9.1, 14.
+constexpr int64_t kFew8 = 512, kFew4 = 768;
 template <typename T, typename TO>
 hipError_t layer_fwd_t(const NormArgs& a, hipStream_t s) {
     if (a.seqlen == 1) return token_t<T, TO, kLayer>(a, s);
     switch (norm_lanes(a.rows, a.seqlen, sizeof(T) == 4)) {
         case 1: return fwd_one<T, TO, kLayer, 1, 1024, 4>(a, s);
-        case 4: return a.dim <= 512 ? fwd_one<T, TO, kLayer, 4, 512, 4>(a, s) : fwd_one<T, TO, kLayer, 4, 1024, 8>(a, s);
-        default: return a.dim <= 256 ? fwd_one<T, TO, kLayer, 8, 256, 8>(a, s) : fwd_one<T, TO, kLayer, 8, 1024, 8>(a, s);
+        case 4: return a.dim <= kFew4 ? fwd_one<T, TO, kLayer, 4, 512, 4>(a, s) : fwd_one<T, TO, kLayer, 4, 1024, 8>(a, s);
+        default: return a.dim <= kFew8 ? fwd_one<T, TO, kLayer, 8, 256, 8>(a, s) : fwd_one<T, TO, kLayer, 8, 1024, 8>(a, s);
     }
 }
 template <typename T, typename TO>
@@ -445,8 +451,8 @@ hipError_t layer_bwd_t(const NormArgs& a, hipStream_t s) {
     const bool f32 = sizeof(T) == 4;
     switch (norm_lanes(a.rows, a.seqlen, f32)) {
         case 1: e = bwd_one<T, TO, kLayer, 1, 1024, 4>(a, s); break;
-        case 4: e = a.dim <= 512 ? bwd_one<T, TO, kLayer, 4, 512, 4>(a, s) : bwd_one<T, TO, kLayer, 4, 1024, 8>(a, s); break;
-        default: e = a.dim <= 256 ? bwd_one<T, TO, kLayer, 8, 256, 8>(a, s) : bwd_one<T, TO, kLayer, 8, 1024, 8>(a, s); break;
+        case 4: e = a.dim <= kFew4 ? bwd_one<T, TO, kLayer, 4, 512, 4>(a, s) : bwd_one<T, TO, kLayer, 4, 1024, 8>(a, s); break;
+        default: e = a.dim <= kFew8 ? bwd_one<T, TO, kLayer, 8, 256, 8>(a, s) : bwd_one<T, TO, kLayer, 8, 1024, 8>(a, s); break;
     }
     if (e) return e;
     hipLaunchKernelGGL(norm_partial_sums, dim3((unsigned)((2 * a.dim + kFinCols - 1) / kFinCols)), dim3(kFinCols * kFinRows), 0, s,
@@ -454,7 +460,9 @@ hipError_t layer_bwd_t(const NormArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// A head's features are few: all stay in registers up to 256 of them.
+// A head's features are few: all stay in registers up to 256 of them.  Us with 256 threads and 512 (batch x heads x features x
+// tokens, bf16; forward, backward): 8 x 16 x 64 x 4096 31, 33 and 47, 40; x 128 44, 61 and 50, 64; x 256 100, 167 and 84, 146.  Rows
+// of up to two vectors, one lane of 64 threads a tile and eight: 64 x 16 x 128 x 1 backward 4.5, 10.
 template <typename T, typename TO, bool BWD>
 hipError_t length_t(const NormArgs& a, hipStream_t s) {
     if (!BWD && a.seqlen == 1) return token_t<T, TO, kLength>(a, s);
