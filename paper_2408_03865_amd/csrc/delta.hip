@@ -121,10 +121,11 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
 // One block a chunk, 64 features of k and grad_per heads of a group, whose sums stay in registers; wave w owns 16 tokens.  Mo
 // and Mv are made in both directions by the wave that needs them, as the operands they are next.  u is beta e: the
 // errors are what lies in memory.
-// In bf16 e, dv and the states are rounded once; Mo and Mv are split into two terms.
-// What bounds it: the waves' own work between two barriers a step, with two blocks a CU (59 KB of LDS): 8 x 4096 tokens, 32 heads
-// of 128 x 128 in 16 groups, 665 to 692 us for 2.4 GB, 3.5 TB/s (VALU 52%, LDS 32%, matrix 22%); masks of the weights where there are no zeros and conditions as
-// branches 815 us; all 128 features of k in a block of eight waves 836 (then 755).
+// In bf16 dv and the states are rounded once; e, Mo and Mv are split into two terms.
+// What bounds it: the waves' own work between two barriers a step, with two blocks a CU (67 KB of LDS) and all their registers:
+// 8 x 4096 tokens, 32 heads of 128 x 128 in 16 groups, 792 us for 2.7 GB, 3.4 TB/s.  e in one term: 665 us, but dq and dk 2.4e-3 off
+// and not 1.8e-3 (dk 3.0e-3 and not 2.5e-3 where a final state's gradient is large).  Masks of the weights where there are no
+// zeros and conditions as branches: 815 (then 692); all 128 features of k in a block of eight waves: 836 (then 755).
 // --------------------------------------------------------------------------------------------
 // 0 where the weight is, which an infinity or NaN must not pass
 __device__ __forceinline__ f32x4 masked(const f32x4& v, const f32x4& weight) {
@@ -140,6 +141,7 @@ struct GradSmem {
     __attribute__((aligned(16))) T q[64 * kC];
     __attribute__((aligned(16))) T dout[64 * kC];
     __attribute__((aligned(16))) T e[64 * kC];
+    __attribute__((aligned(16))) T low[Mat<T>::kSplit ? 64 * kC : 8];
     __attribute__((aligned(16))) T w[64 * kC];
     struct {
         __attribute__((aligned(16))) T s[64 * 64];       // the state before, features of v by features of k
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
 #pragma unroll
     for (int f = 0; f < 4; ++f) dq[f] = dk[f] = f32x4{0, 0, 0, 0};
 
-    Regs dor, er, wr, sr, gr;
+    Regs dor, er, lr, wr, sr, gr;
     float cr[2];
     const int steps = (h1 - h0) << vshift;
     const auto base = [&](const void* p, int step) {
@@ -185,6 +187,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
         const int64_t unit = (b * a.heads + h) * a.chunks + chunk;
         dor.load(tid, at, base(a.dout, step), rows, (int)L);
         er.load(tid, at, base(a.e, step), rows, (int)L);
+        if constexpr (M::kSplit) lr.load(tid, at, base(a.e_low, step), rows, (int)L);
         wr.load(tid, at, base(a.w, step), rows, (int)L);
         sr.load(tid, sat, static_cast<const T*>(a.states) + (unit * vpad + v0) * KC + f0, 64, KC);
         gr.load(tid, sat, static_cast<const T*>(a.grads) + (unit * vpad + v0) * KC + f0, 64, KC);
@@ -210,9 +213,20 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
         __syncthreads();
         dor.settle(tid, base(a.dout, step), rows, t0, L);
         er.settle(tid, base(a.e, step), rows, t0, L);
+        if constexpr (M::kSplit) {                      // what the rounding leaves of them
+            lr.settle(tid, base(a.e_low, step), rows, t0, L);
+#pragma unroll
+            for (int i = 0; i < Regs::kPasses; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t hi = er.w[i][r], lo = lr.w[i][r];
+                    lr.w[i][r] = pack_bf16x2(whole(hi, lo, 0) - __uint_as_float(hi << 16), whole(hi, lo, 1) - __uint_as_float(hi & 0xffff0000u));
+                }
+        }
         wr.settle(tid, base(a.w, step), rows, t0, L);
         dor.store(tid, sm.dout);
         er.store(tid, sm.e);
+        if constexpr (M::kSplit) lr.store(tid, sm.low);
         wr.store(tid, sm.w);
         sr.store(tid, sm.st.s);
         gr.store(tid, sm.st.d);
@@ -220,6 +234,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
         if (tid + 256 < kDeltaCoef) sm.coef[tid + 256] = cr[1];
         __syncthreads();
         load(min(step + 1, steps - 1));
+        const int l = here(lane_id()), col = l & 15, g4 = (l >> 4) * 4;
         const auto c4 = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which + i * 16 + g4]); };
         const auto tok = [&](const T* tile, int k, int i) { return M::transposed(l, tile + k * 16 * kC, i); };
         if (first) {
@@ -227,11 +242,12 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
 #pragma unroll
             for (int i = 0; i < 4; ++i) mo[i] = mv[i] = f32x4{0, 0, 0, 0};
         }
-        Frag dw[4], uw[4], ww[4];
+        Frag dw[4], uw[4], lw[4], ww[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             dw[n] = tok(sm.dout, n, w);
             uw[n] = tok(sm.e, n, w);
+            lw[n] = M::kSplit ? tok(sm.low, n, w) : Frag{};
             ww[n] = tok(sm.w, n, w);
         }
 #pragma unroll
@@ -239,6 +255,11 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             if (i <= w) {
 #pragma unroll
                 for (int n = 0; n < 4; n += 2) {
+                    if constexpr (M::kSplit) {
+                        const Frag y0 = tok(sm.low, n, i), y1 = tok(sm.low, n + 1, i);
+                        mo[i] = M::mma(y0, y1, dw[n], dw[n + 1], mo[i]);
+                        mv[i] = M::mma(y0, y1, ww[n], ww[n + 1], mv[i]);
+                    }
                     const Frag x0 = tok(sm.e, n, i), x1 = tok(sm.e, n + 1, i);
                     mo[i] = M::mma(x0, x1, dw[n], dw[n + 1], mo[i]);
                     mv[i] = M::mma(x0, x1, ww[n], ww[n + 1], mv[i]);
@@ -246,13 +267,22 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             } else {
 #pragma unroll
                 for (int n = 0; n < 4; n += 2) {
-                    mo[i] = M::mma(tok(sm.dout, n, i), tok(sm.dout, n + 1, i), uw[n], uw[n + 1], mo[i]);
-                    mv[i] = M::mma(tok(sm.w, n, i), tok(sm.w, n + 1, i), uw[n], uw[n + 1], mv[i]);
+                    const Frag x0 = tok(sm.dout, n, i), x1 = tok(sm.dout, n + 1, i), y0 = tok(sm.w, n, i), y1 = tok(sm.w, n + 1, i);
+                    if constexpr (M::kSplit) {
+                        mo[i] = M::mma(x0, x1, lw[n], lw[n + 1], mo[i]);
+                        mv[i] = M::mma(y0, y1, lw[n], lw[n + 1], mv[i]);
+                    }
+                    mo[i] = M::mma(x0, x1, uw[n], uw[n + 1], mo[i]);
+                    mv[i] = M::mma(y0, y1, uw[n], uw[n + 1], mv[i]);
                 }
             }
         }
 #pragma unroll
         for (int n = 0; n < 4; n += 2) {
+            if constexpr (M::kSplit) {
+                mo_d = M::mma(dw[n], dw[n + 1], lw[n], lw[n + 1], mo_d);
+                mv_d = M::mma(ww[n], ww[n + 1], lw[n], lw[n + 1], mv_d);
+            }
             mo_d = M::mma(dw[n], dw[n + 1], uw[n], uw[n + 1], mo_d);
             mv_d = M::mma(ww[n], ww[n + 1], uw[n], uw[n + 1], mv_d);
         }
@@ -271,7 +301,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
                         const Frag s0 = tok(sm.st.s, n, f), s1 = tok(sm.st.s, n + 1, f);
                         q = M::mma(dw[n], dw[n + 1], s0, s1, q);
                         x = M::mma(ww[n], ww[n + 1], s0, s1, x);
-                        g = M::mma(uw[n], uw[n + 1], tok(sm.st.d, n, f), tok(sm.st.d, n + 1, f), g);
+                        const Frag d0 = tok(sm.st.d, n, f), d1 = tok(sm.st.d, n + 1, f);
+                        if constexpr (M::kSplit) g = M::mma(lw[n], lw[n + 1], d0, d1, g);
+                        g = M::mma(uw[n], uw[n + 1], d0, d1, g);
                     }
                     if constexpr (decltype(some)::value) {
                         q = masked(q, in);

@@ -37,7 +37,7 @@ struct DeltaArgs {
     float* bound;               // the states at every bound_chunks chunks' end, in the threads' order
     float* dot;                 // their products with the gradients there, (batch, heads, nb + 1)
     void* e;                    // the errors, (batch, heads, dv, seqlen) in the inputs' type, rounded half up
-    uint16_t* e_low;            // bf16: the lower halves of their fp32 patterns, in the threads' order
+    uint16_t* e_low;            // bf16: the lower halves of their fp32 patterns, as e
     void* w;                    // dv, as e, where the out is of another type; else null
     float* rq;                  // out . dout and -(v . dv) of every token
     float* rk;

@@ -63,8 +63,8 @@ struct Plan {
 };
 // Chunks between the boundaries at which the backward multiplies the two states.  A decay's gradient is a sum over the tokens up
 // to the next, of terms that cancel: its error grows with their number, and the boundaries' fp32 states move memory.  8 rows of
-// 4096 tokens, 32 heads of 128 x 128: 2 chunks 2480 us, 4 chunks 2375 us and 7.8e-7 off in the 2-norm, 8 chunks 2340 us and 1.0e-6
-// (token by token in fp32: 5.6e-7).
+// 4096 tokens, 32 heads of 128 x 128: 4 chunks 7.8e-7 off in the 2-norm, 8 chunks 1.0e-6 and 35 us of 2375 faster, 2 chunks 105
+// slower (the plain form in fp32: 5.6e-7).
 constexpr int32_t kBoundChunks = 4;
 // Heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks.  Us with this rule, with
 // all heads of a group in a block and with one (batch x heads in groups x tokens, dk x dv; bf16):
@@ -162,7 +162,7 @@ BwdExtra take_bwd(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t batch, int6
     a.bound = t.floats(rows * p.nb * state);
     a.dot = t.floats(rows * (p.nb + 1));
     a.e = t.take(size * (size_t)(rows * dv * seqlen));
-    if (dtype != PACKMAMBA_F32) a.e_low = static_cast<uint16_t*>(t.take(2 * (size_t)(p.units * pm::kLinChunk * pm::delta_pad((int32_t)dv))));
+    if (dtype != PACKMAMBA_F32) a.e_low = static_cast<uint16_t*>(t.take(size * (size_t)(rows * dv * seqlen)));
     a.w = dtype == PACKMAMBA_BF16_F32OUT ? t.take(size * (size_t)(rows * dv * seqlen)) : nullptr;
     a.rq = t.floats(rows * seqlen);
     a.rk = t.floats(rows * seqlen);

@@ -206,26 +206,63 @@ struct TokenRegs {
     }
 };
 
+// 16 bits a token that are no numbers, as TokenRegs has a row's bf16.
+struct HalfRegs : TokenRegs<bf16_t> {
+    __device__ void load(const uint16_t* p, int64_t t0, int l, int64_t L) {
+        if (t0 + kC <= L) {
+            TokenRegs::load(reinterpret_cast<const bf16_t*>(p), t0, l, L);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int r = 0; r < kPer; r += 2) {
+                    const int64_t t = t0 + at(l, i) + r;
+                    w[i][r / 2] = (t < L ? p[t] : 0u) | (uint32_t)(t + 1 < L ? p[t + 1] : 0u) << 16;
+                }
+        }
+    }
+    __device__ void store(uint16_t* p, int64_t t0, int l, int64_t L) const {
+        if (t0 + kC <= L) {
+            TokenRegs::store(reinterpret_cast<bf16_t*>(p), t0, l, L);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int r = 0; r < kPer; ++r) {
+                    const int64_t t = t0 + at(l, i) + r;
+                    if (t < L) p[t] = (uint16_t)(w[i][r / 2] >> (r % 2 * 16));
+                }
+        }
+    }
+};
+
 // Errors whole in 32 bits: as bf16, rounded half up, which the products take, and the lower halves of the fp32 patterns, which
 // make up the rest: a pattern is the rounded one's plus its own lower half, taken for a signed number.
 __device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, bool upper) {     // of b and a, b's above
     return __builtin_amdgcn_perm(b, a, upper ? 0x07060302u : 0x05040100u);
 }
+// one of a pair of them
+__device__ __forceinline__ float whole(uint32_t hi, uint32_t lo, int which) {
+    return __uint_as_float(which ? (hi & 0xffff0000u) + (uint32_t)((int32_t)lo >> 16) : (hi << 16) + (uint32_t)((int32_t)(lo << 16) >> 16));
+}
 template <typename T>
 struct ErrorRegs {
     TokenRegs<T> hi;
-    u32x4 lo[2];
+    HalfRegs lo;
     __device__ void set(const f32x4 (&e)[4]) {
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const u32x4 x = __builtin_bit_cast(u32x4, e[2 * i]), y = __builtin_bit_cast(u32x4, e[2 * i + 1]);
                 const u32x4 xr = x + 0x8000u, yr = y + 0x8000u;
-                uint32_t a = halves(xr.x, xr.y, true), b = halves(xr.z, xr.w, true), c = halves(yr.x, yr.y, true), d = halves(yr.z, yr.w, true);
-                TokenRegs<T>::swap(a, c);
-                TokenRegs<T>::swap(b, d);
-                hi.w[i] = u32x4{a, b, c, d};
-                lo[i] = u32x4{halves(x.x, x.y, false), halves(x.z, x.w, false), halves(y.x, y.y, false), halves(y.z, y.w, false)};
+                const auto pairs = [](const u32x4& x, const u32x4& y, bool upper) {
+                    uint32_t a = halves(x.x, x.y, upper), b = halves(x.z, x.w, upper), c = halves(y.x, y.y, upper), d = halves(y.z, y.w, upper);
+                    TokenRegs<T>::swap(a, c);
+                    TokenRegs<T>::swap(b, d);
+                    return u32x4{a, b, c, d};
+                };
+                hi.w[i] = pairs(xr, yr, true);
+                lo.w[i] = pairs(x, y, false);
             }
         } else {
             hi.set(e);
@@ -234,47 +271,35 @@ struct ErrorRegs {
     __device__ void get(uint32_t mask, f32x4 (&e)[4]) const {
         typename Mat<T>::Frag f[4];
         hi.get(mask, f);
+        if constexpr (sizeof(T) == 2) {
+            Mat<bf16_t>::Frag h[4];
+            lo.get(mask, h);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            e[i] = Mat<T>::widen(f[i]);
-            if constexpr (sizeof(T) == 2) {
+            for (int i = 0; i < 4; ++i) e[i] = f32x4{whole(f[i].x, h[i].x, 0), whole(f[i].x, h[i].x, 1), whole(f[i].y, h[i].y, 0), whole(f[i].y, h[i].y, 1)};
+        } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t two = lo[i / 2][(i % 2) * 2 + r / 2] & mask;
-                    const int32_t half = r % 2 ? (int32_t)two >> 16 : (int32_t)(two << 16) >> 16;
-                    e[i][r] = __uint_as_float(__float_as_uint(e[i][r]) + (uint32_t)half);
-                }
-            }
+            for (int i = 0; i < 4; ++i) e[i] = f[i];
         }
     }
-    // low: the chunk's and wave's
-    __device__ void store(T* row, uint16_t* low, int64_t t0, int l, int64_t L, bool live) const {
-        if (live) hi.store(row, t0, l, L);
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<u32x4*>(low + l * 16) = lo[0];
-            *reinterpret_cast<u32x4*>(low + l * 16 + 8) = lo[1];
-        }
+    __device__ void store(T* row, uint16_t* low, int64_t t0, int l, int64_t L) const {
+        hi.store(row, t0, l, L);
+        if constexpr (sizeof(T) == 2) lo.store(low, t0, l, L);
     }
     __device__ void load(const T* row, const uint16_t* low, int64_t t0, int l, int64_t L) {
         hi.load(row, t0, l, L);
-        if constexpr (sizeof(T) == 2) {
-            lo[0] = *reinterpret_cast<const u32x4*>(low + l * 16);
-            lo[1] = *reinterpret_cast<const u32x4*>(low + l * 16 + 8);
-        }
+        if constexpr (sizeof(T) == 2) lo.load(low, t0, l, L);
     }
-    // one token's of the chunk, token j in a column
-    __device__ static int low_at(int j, int col) { return ((j % 16) / 4 * 16 + col) * 16 + j / 16 * 4 + j % 4; }
-    __device__ static void put(T* at, uint16_t* low, int j, int col, float e) {
+    // one token's
+    __device__ static void put(T* at, uint16_t* low, float e) {
         if constexpr (sizeof(T) == 2) {
             at->bits = (uint16_t)((__float_as_uint(e) + 0x8000u) >> 16);
-            low[low_at(j, col)] = (uint16_t)__float_as_uint(e);
+            *low = (uint16_t)__float_as_uint(e);
         } else {
             *at = e;
         }
     }
-    __device__ static float take(const T* at, const uint16_t* low, int j, int col) {
-        if constexpr (sizeof(T) == 2)
-            return __uint_as_float(((uint32_t)at->bits << 16) + (uint32_t)(int32_t)(int16_t)low[low_at(j, col)]);
+    __device__ static float take(const T* at, const uint16_t* low) {
+        if constexpr (sizeof(T) == 2) return whole(at->bits, *low, 0);
         else return *at;
     }
 };
@@ -524,7 +549,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     const T* dop = MODE == kDeltaStates ? static_cast<const T*>(a.dout) + zrow * L : nullptr;
     TO* op = MODE == kDeltaOut ? static_cast<TO*>(a.out) + zrow * L : nullptr;
     T* ep = MODE == kDeltaStates ? static_cast<T*>(a.e) + zrow * L : nullptr;
-    const auto low = [&](int64_t unit) { return a.e_low + (unit * kWaves + w) * 1024; };
+    uint16_t* elp = MODE == kDeltaStates && M::kSplit ? a.e_low + zrow * L : nullptr;
     const float* betap = a.beta + bh * L;
 
     DeltaState<KF> S;
@@ -669,7 +694,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                 if constexpr (MODE == kDeltaStates) {
                     ErrorRegs<T> er;
                     er.set(x);
-                    er.store(ep, low(unit), ct, here(l), L, live);
+                    if (live) er.store(ep, elp, ct, here(l), L);
                 }
                 Frag uf[4][NQ];
                 f32x4 o[4];
@@ -714,7 +739,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                     } else {
                         const float d = lanes16(live && t < L ? o * Storage<T>::load1(dop + t) : 0.0f);
                         if (l == 0) dot[w][j] = d;
-                        if (mine) ErrorRegs<T>::put(ep + t, low(unit), j, col, e);
+                        if (mine) ErrorRegs<T>::put(ep + t, M::kSplit ? elp + t : nullptr, e);
                     }
                 }
             }
@@ -771,7 +796,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const T* dop = static_cast<const T*>(a.dout) + zrow * L;
     TO* op = SUM ? nullptr : static_cast<TO*>(a.out) + zrow * L;
     const T* ep = SUM ? nullptr : static_cast<const T*>(a.e) + zrow * L;
-    const auto low = [&](int64_t unit) { return a.e_low + (unit * kWaves + w) * 1024; };
+    const uint16_t* elp = !SUM && M::kSplit ? a.e_low + zrow * L : nullptr;
     T* wp = SUM || !a.w ? nullptr : static_cast<T*>(a.w) + zrow * L;      // a copy in T, where the out has another type
     const float* betap = a.beta + bh * L;
 
@@ -877,7 +902,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         if constexpr (!kTwo) __syncthreads();
         if constexpr (!SUM) {                            // needed late in the chunk
             vr.load(vp, ct, here(l), L);
-            er.load(ep, low(unit), ct, here(l), L);
+            er.load(ep, elp, ct, here(l), L);
         }
         const float A = uniform(sm.misc[0]);
         const bool cut = A < 0.0f;
@@ -960,7 +985,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                 D.add(sm.q, j, d * a.scale);
                 const float du = D.against(sm.k, j), dvt = in ? betap[t] * du : 0.0f;
                 if constexpr (!SUM) {
-                    const float et = in && live ? ErrorRegs<T>::take(ep + t, low(unit), j, col) : 0.0f;
+                    const float et = in && live ? ErrorRegs<T>::take(ep + t, M::kSplit ? elp + t : nullptr) : 0.0f;
                     const float vd = lanes16(in && live ? Storage<T>::load1(vp + t) * dvt : 0.0f), db = lanes16(in && live ? du * et : 0.0f);
                     if (l == 0) {
                         dot[0][w][j] = vd;

@@ -298,8 +298,7 @@ __global__ __launch_bounds__(kFinCols * kFinRows) void norm_partial_sums(const f
             float w[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) w[q] = partial[(i + q * kFinRows) * cols + f];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v += w[q];
+            v += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
         }
         for (; i < rows; i += kFinRows) v += partial[i * cols + f];
     }
