@@ -29,9 +29,9 @@ def compare(d, shape, dtype, case=""):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("L", [2, 3, 4, 5, 7, 8, 9, 12, 127, 128, 192, 193])
+@pytest.mark.parametrize("L", [2, 3, 4, 5, 7, 8, 9, 12, 127, 128, 192, 193, 255, 256, 257, 511, 512, 513, 769])
 def test_lengths(L, dtype):
-    """Rows shorter than a vector, of odd lengths, and ends inside and at a chunk."""
+    """Rows shorter than a vector, of odd lengths, and ends inside and at a chunk, and at a boundary of the decays' sums."""
     shape = (3, 4, 2, 20, 33, L)
     note(f"delta rule length {L} {dtype}")
     compare(make(shape, dtype, "token", True, 100 + L, mean=max(1, L // 3)), shape, dtype)
