@@ -165,6 +165,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     const int64_t b = bat, chunk = unit_id - row * (uint32_t)a.chunks, grp = bg - bat * (uint32_t)a.groups, t0 = chunk * kC;
     const int half = (int)(id % kHalves), part = (int)(row - bg * (uint32_t)parts);
     const int f0 = half * 64, frows = min(64, a.dk - f0);
+    const bool few_k = !M::kSplit && frows <= 32;       // in 32 bits, where matrix instructions are slow: tiles without features are left out
     const int vpad = a.dv <= 64 ? 64 : 128, vshift = a.dv <= 64 ? 0 : 1;
     const int h0 = (int)grp * rep + part * a.grad_per, h1 = min((int)(grp + 1) * rep, h0 + a.grad_per);
     const T* kp = static_cast<const T*>(a.k) + ((b * a.groups + grp) * a.dk + f0) * L;
@@ -210,6 +211,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     for (int step = 0; step < steps; ++step) {
         const bool first = (step & vshift) == 0, done = (step & vshift) == vshift;
         const int rows = min(64, a.dv - (step & vshift) * 64);
+        const bool few_v = !M::kSplit && rows <= 32;
         __syncthreads();
         dor.settle(tid, base(a.dout, step), rows, t0, L);
         er.settle(tid, base(a.e, step), rows, t0, L);
@@ -255,6 +257,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             if (i <= w) {
 #pragma unroll
                 for (int n = 0; n < 4; n += 2) {
+                    if (n >= 2 && few_v) break;
                     if constexpr (M::kSplit) {
                         const Frag y0 = tok(sm.low, n, i), y1 = tok(sm.low, n + 1, i);
                         mo[i] = M::mma(y0, y1, dw[n], dw[n + 1], mo[i]);
@@ -267,6 +270,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             } else {
 #pragma unroll
                 for (int n = 0; n < 4; n += 2) {
+                    if (n >= 2 && few_v) break;
                     const Frag x0 = tok(sm.dout, n, i), x1 = tok(sm.dout, n + 1, i), y0 = tok(sm.w, n, i), y1 = tok(sm.w, n + 1, i);
                     if constexpr (M::kSplit) {
                         mo[i] = M::mma(x0, x1, lw[n], lw[n + 1], mo[i]);
@@ -279,6 +283,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
         }
 #pragma unroll
         for (int n = 0; n < 4; n += 2) {
+            if (n >= 2 && few_v) break;
             if constexpr (M::kSplit) {
                 mo_d = M::mma(dw[n], dw[n + 1], lw[n], lw[n + 1], mo_d);
                 mv_d = M::mma(ww[n], ww[n + 1], lw[n], lw[n + 1], mv_d);
@@ -295,9 +300,11 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
             const auto states = [&](auto some) {
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
+                    if (f >= 2 && few_k) break;
                     f32x4 q = {0, 0, 0, 0}, g = q, x = q;
 #pragma unroll
                     for (int n = 0; n < 4; n += 2) {
+                        if (n >= 2 && few_v) break;
                         const Frag s0 = tok(sm.st.s, n, f), s1 = tok(sm.st.s, n + 1, f);
                         q = M::mma(dw[n], dw[n + 1], s0, s1, q);
                         x = M::mma(ww[n], ww[n + 1], s0, s1, x);
@@ -368,6 +375,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
                 rows_of(2 * p + 1, a1, b1, e1);
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
+                    if (f >= 2 && few_k) break;
                     const Frag k0 = M::direct(l, sm.k + f * 16 * kC, 2 * p), k1 = M::direct(l, sm.k + f * 16 * kC, 2 * p + 1);
                     const Frag q0 = M::direct(l, sm.q + f * 16 * kC, 2 * p), q1 = M::direct(l, sm.q + f * 16 * kC, 2 * p + 1);
 #pragma unroll

@@ -283,11 +283,9 @@ int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const 
     a.dk_out = pieces ? x.dk : dk;
     if (int e = launch_status(pm::launch_delta_grads(a, pieces || dtype != PACKMAMBA_BF16, s))) return e;
     if (pieces) {
-        const int32_t of = (int32_t)groups * p.grad_parts;
-        for (int i = 0; i < 2; ++i)
-            if (int e = launch_status(pm::launch_linear_group_sum(i ? x.dk : x.dq, i ? dk : dq, batch, of, (int32_t)groups,
-                                                                  dk_size * seqlen, dtype != PACKMAMBA_BF16, s)))
-                return e;
+        if (int e = launch_status(pm::launch_linear_group_sums(x.dq, dq, x.dk, dk, batch, (int32_t)groups * p.grad_parts, (int32_t)groups,
+                                                               dk_size * seqlen, dtype != PACKMAMBA_BF16, s)))
+            return e;
     }
     if (!ddecay) return PACKMAMBA_OK;
     pm::LinDecayArgs d{};

@@ -113,6 +113,7 @@ __global__ __launch_bounds__(256, 3) void delta_prep_kernel(DeltaArgs a) {
             if (i < w) continue;
 #pragma unroll
             for (int k = 0; k < KT; k += 2) {
+                if (!M::kSplit && KT == 4 && k >= 2 && a.dk <= 32) break;
                 const Frag k0 = M::transposed(l, sm.in.k + k * 16 * kC, i), k1 = M::transposed(l, sm.in.k + (k + 1) * 16 * kC, i);
                 const Frag q0 = M::transposed(l, sm.in.q + k * 16 * kC, i), q1 = M::transposed(l, sm.in.q + (k + 1) * 16 * kC, i);
                 kf[i] = M::mma(ks[k], ks[k + 1], k0, k1, kf[i]);

@@ -138,8 +138,12 @@ __global__ __launch_bounds__(64) void linear_ddecay_heads(const float* __restric
 // cache); 2 x 24 heads of 64 x 512, one group, 3.8 us, with one load at a time 8.7.
 constexpr int kSumAhead = 8;            // heads' loads on their way at a time
 template <typename TO>
-__global__ __launch_bounds__(256) void group_sum_kernel(const float* __restrict__ part, TO* __restrict__ out, int per,
-                                                        int64_t n) {
+__global__ __launch_bounds__(256) void group_sum_kernel(const float* __restrict__ part, TO* __restrict__ out, int per, int64_t n,
+                                                        const float* __restrict__ part1, TO* __restrict__ out1) {
+    if (blockIdx.y) {
+        part = part1;
+        out = out1;
+    }
     const int64_t blocks = (n + 1023) / 1024, bg = blockIdx.x / blocks;
     const int64_t i = (blockIdx.x - bg * blocks) * 1024 + threadIdx.x * 4;
     if (i >= n) return;
@@ -165,6 +169,19 @@ __global__ __launch_bounds__(256) void group_sum_kernel(const float* __restrict_
             Storage<TO>::store1(o + r, v);
         }
     }
+}
+
+// of one tensor, or of two in one launch
+hipError_t group_sums(const float* part, void* out, const float* part1, void* out1, int64_t batch, int32_t heads, int32_t groups,
+                      int64_t n, bool f32, hipStream_t s) {
+    const dim3 grid((unsigned)((n + 1023) / 1024 * batch * groups), part1 ? 2 : 1);
+    if (f32)
+        hipLaunchKernelGGL(group_sum_kernel<float>, grid, dim3(256), 0, s, part, static_cast<float*>(out), heads / groups, n, part1,
+                           static_cast<float*>(out1));
+    else
+        hipLaunchKernelGGL(group_sum_kernel<bf16_t>, grid, dim3(256), 0, s, part, static_cast<bf16_t*>(out), heads / groups, n, part1,
+                           static_cast<bf16_t*>(out1));
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -197,12 +214,12 @@ hipError_t launch_linear_ddecay(const LinDecayArgs& a, hipStream_t s) {
 
 hipError_t launch_linear_group_sum(const float* part, void* out, int64_t batch, int32_t heads, int32_t groups, int64_t n,
                                    bool f32, hipStream_t s) {
-    const dim3 grid((unsigned)((n + 1023) / 1024 * batch * groups));
-    if (f32)
-        hipLaunchKernelGGL(group_sum_kernel<float>, grid, dim3(256), 0, s, part, static_cast<float*>(out), heads / groups, n);
-    else
-        hipLaunchKernelGGL(group_sum_kernel<bf16_t>, grid, dim3(256), 0, s, part, static_cast<bf16_t*>(out), heads / groups, n);
-    return hipGetLastError();
+    return group_sums(part, out, nullptr, nullptr, batch, heads, groups, n, f32, s);
+}
+
+hipError_t launch_linear_group_sums(const float* part, void* out, const float* part1, void* out1, int64_t batch, int32_t heads,
+                                    int32_t groups, int64_t n, bool f32, hipStream_t s) {
+    return group_sums(part, out, part1, out1, batch, heads, groups, n, f32, s);
 }
 
 }  // namespace pm

@@ -127,6 +127,8 @@ hipError_t launch_linear_ddecay(const LinDecayArgs& a, hipStream_t s);
 // out[b, g, i] = sum over the heads of group g of part[b, h, i], i < n, in the heads' order
 hipError_t launch_linear_group_sum(const float* part, void* out, int64_t batch, int32_t heads, int32_t groups, int64_t n,
                                    bool f32, hipStream_t s);
+hipError_t launch_linear_group_sums(const float* part, void* out, const float* part1, void* out1, int64_t batch, int32_t heads,
+                                    int32_t groups, int64_t n, bool f32, hipStream_t s);     // two tensors'
 
 struct LinStepArgs {
     const void* q;

@@ -10,6 +10,9 @@ hipError_t launch_delta_states(const DeltaArgs&, hipStream_t) { return hipErrorI
 hipError_t launch_delta_rev(const DeltaArgs&, hipStream_t) { return hipErrorInvalidValue; }
 hipError_t launch_delta_segments(const DeltaArgs&, bool, hipStream_t) { return hipErrorInvalidValue; }
 hipError_t launch_delta_grads(const DeltaArgs&, bool, hipStream_t) { return hipErrorInvalidValue; }
+hipError_t launch_linear_group_sums(const float*, void*, const float*, void*, int64_t, int32_t, int32_t, int64_t, bool, hipStream_t) {
+    return hipErrorInvalidValue;
+}
 hipError_t launch_delta_step(const DeltaStepArgs&, hipStream_t) { return hipErrorInvalidValue; }
 hipError_t launch_layernorm_fwd(const NormArgs&, hipStream_t) { return hipErrorInvalidValue; }
 hipError_t launch_layernorm_bwd(const NormArgs&, hipStream_t) { return hipErrorInvalidValue; }
