@@ -53,11 +53,12 @@ struct DeltaTiles {
     __attribute__((aligned(16))) float coef[3][kC];
     __attribute__((aligned(16))) float misc[4];
 };
-// Two of them where a CU holds as many blocks all the same: the next chunk's are written during this one, with one barrier a
-// chunk and not two.
+// Two of them, the next chunk's written during this one with one barrier a chunk and not two, for blocks of four waves where a CU
+// holds two blocks all the same.  Us with one and with two: backward of 4 x 24 heads x 2048, 64 x 64, 371, 358; 30001 tokens
+// forward, 24 heads of 128 x 64, 695, 690; eight waves: 8 x 32 x 4096, 128 x 128, forward 515, 529, backward 2350, 2400.
 template <typename T, int KC, int VP, int NH, int NP, bool Q>
 constexpr int delta_buffers() {
-    return (int)sizeof(DeltaTiles<T, KC, NH, NP, Q>) * 2 <= (VP == 128 ? 156 : 78) * 1024 ? 2 : 1;
+    return VP == 64 && (int)sizeof(DeltaTiles<T, KC, NH, NP, Q>) * 2 <= 78 * 1024 ? 2 : 1;
 }
 template <typename T, int KC, int VP, int NH, int NP, bool Q, int DOTS>
 struct DeltaSmem {
