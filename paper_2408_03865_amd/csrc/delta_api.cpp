@@ -59,13 +59,16 @@ pm::NormArgs norm_args(const void* x, int64_t rows, int64_t dim, int64_t seqlen,
 // Split of the rows into segments of whole chunks, each walked by its own block.
 struct Plan {
     int64_t chunks, units;
-    int32_t nseg, seg_chunks, nb, heads_per, grad_per, grad_parts;
+    int32_t nseg, seg_chunks, bound, nb, heads_per, grad_per, grad_parts;
 };
 // Chunks between the boundaries at which the backward multiplies the two states.  A decay's gradient is a sum over the tokens up
-// to the next, of terms that cancel: its error grows with their number, and the boundaries' fp32 states move memory.  8 rows of
-// 4096 tokens, 32 heads of 128 x 128: 4 chunks 7.8e-7 off in the 2-norm, 8 chunks 1.0e-6 and 35 us of 2375 faster, 2 chunks 105
-// slower (the plain form in fp32: 5.6e-7).
-constexpr int32_t kBoundChunks = 4;
+// to the next, of terms that cancel: its error grows with their number, and the boundaries' fp32 states move memory.  With 1, 2, 4
+// and 8 chunks, us and errors in the 2-norm:
+//   8 x 32 heads x 4096 (16384 chunks of heads), 128 x 128, bf16    -, 2480, 2375, 2340; -, -, 7.8e-7, 1.0e-6 (the plain form 5.6e-7)
+//   4 x 24 x 2048 (3072), 64 x 64, bf16                             369, 361, 359, -
+//   1 x 2 x 256 (8), 24 x 32, fp32, decays of a head                91.6, 89.9, 89.8, -; 1.2e-4, 1.5e-4, 1.7e-4, - of sums near 200
+//                                                                   (the plain form 1.6e-4)
+int32_t bound_chunks(int64_t units) { return units <= 1024 ? 1 : units <= 4096 ? 2 : 4; }
 // Heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks.  Us with this rule, with
 // all heads of a group in a block and with one (batch x heads in groups x tokens, dk x dv; bf16):
 //   the preparation, forward    1 x 32 in 1 x 512, 128 x 128: 50, 183, 50    2 x 64 in 4 x 2048, 128 x 128: 192, 222, 192
@@ -118,7 +121,8 @@ Plan make_plan(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t
     p.units = rows * p.chunks;
     p.seg_chunks = (int32_t)per;
     p.nseg = (int32_t)((p.chunks + per - 1) / per);
-    p.nb = (int32_t)((p.chunks + kBoundChunks - 1) / kBoundChunks);
+    p.bound = bound_chunks(p.units);
+    p.nb = (int32_t)((p.chunks + p.bound - 1) / p.bound);
     const int64_t rep = heads / groups, blocks = batch * p.chunks * groups;
     p.heads_per = heads_for(blocks, rep, 1024);
     p.grad_per = heads_for(blocks * (dk <= 64 ? 1 : 2), rep, 256);
@@ -179,7 +183,7 @@ void set_plan(pm::DeltaArgs& a, const Plan& p) {
     a.chunks = (int32_t)p.chunks;
     a.nseg = p.nseg;
     a.seg_chunks = p.seg_chunks;
-    a.bound_chunks = kBoundChunks;
+    a.bound_chunks = p.bound;
     a.nb = p.nb;
     a.heads_per = p.heads_per;
     a.grad_per = p.grad_per;
@@ -291,7 +295,7 @@ int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const 
     pm::LinDecayArgs d{};
     d.rq = a.rq; d.rk = a.rk; d.dot = a.dot; d.decay = decay; d.pos = position_indices; d.ddecay = ddecay; d.partial = x.pieces;
     d.seqlen = seqlen; d.batch = a.batch; d.heads = a.heads; d.decay_mode = a.decay_mode;
-    d.bound_tokens = kBoundChunks * (int32_t)pm::kLinChunk; d.nb = p.nb; d.bound_end = a.bound_end;
+    d.bound_tokens = p.bound * (int32_t)pm::kLinChunk; d.nb = p.nb; d.bound_end = a.bound_end;
     return launch_status(pm::launch_linear_ddecay(d, s));
 }
 

@@ -42,7 +42,7 @@ def test_sizes():
     for shape in bad:
         assert fwd(*shape) == 0 and bwd(*shape, 1) == 0, shape
     assert fwd(1, 16, 16, 8, 8, 1 << 22) > 0 and fwd(1 << 20, 1, 1, 8, 8, 64) > 0       # the limits themselves
-    # linear in the chunks, whatever the split: products 22 KB, two states 128, errors 32, pieces of two gradients 64, a boundary 16,
+    # linear in the chunks, whatever the split: products 22 KB, two states 128, errors 32, pieces of two gradients 64, a boundary 64,
     # a segment of two chunks or more 128
     for shape in ((1, 1, 1, 128, 128, 1 << 22), (1, 16, 2, 128, 128, 1 << 22), (1 << 10, 64, 64, 128, 128, 1024), (3, 5, 5, 128, 128, 100)):
         units = shape[0] * shape[1] * -(-shape[5] // 64)
