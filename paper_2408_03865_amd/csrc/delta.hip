@@ -445,7 +445,11 @@ hipError_t chain_kc(const DeltaArgs& a, bool rev, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_delta_fwd(const DeltaArgs& a, bool exact, hipStream_t s) { return walk(a, exact ? kWalkOutExact : kWalkOut, s); }
+hipError_t launch_delta_fwd(const DeltaArgs& a, bool split, hipStream_t s) {
+    if (split)
+        if (hipError_t e = launch_delta_segments(a, false, s)) return e;
+    return walk(a, kWalkOut, s);
+}
 hipError_t launch_delta_states(const DeltaArgs& a, hipStream_t s) { return walk(a, kWalkStates, s); }
 hipError_t launch_delta_rev(const DeltaArgs& a, hipStream_t s) { return walk(a, kWalkRev, s); }
 

@@ -57,9 +57,8 @@ struct DeltaArgs {
 
 inline int32_t delta_pad(int32_t n) { return n <= 64 ? 64 : 128; }
 
-// exact: 32-bit accuracy of the states, else what a bf16 out shows of them
 hipError_t launch_delta_prep(const DeltaArgs& a, hipStream_t s);
-hipError_t launch_delta_fwd(const DeltaArgs& a, bool exact, hipStream_t s);
+hipError_t launch_delta_fwd(const DeltaArgs& a, bool split, hipStream_t s);     // split: the states that enter the segments first
 hipError_t launch_delta_states(const DeltaArgs& a, hipStream_t s);          // the backward's walk in time
 hipError_t launch_delta_rev(const DeltaArgs& a, hipStream_t s);
 hipError_t launch_delta_segments(const DeltaArgs& a, bool rev, hipStream_t s);

@@ -222,13 +222,10 @@ int packmamba_delta_rule_fwd(const void* q, const void* k, const void* v, const 
     a.dk = (int32_t)dk; a.dv = (int32_t)dv; a.dtype = dtype;
     a.decay_mode = decay ? (decay_per_token ? 2 : 1) : 0;
     set_plan(a, p);
-    const bool exact = final_state != nullptr;
     a.sum_segs = p.nseg - 1;
     const hipStream_t s = (hipStream_t)stream;
     if (int e = launch_status(pm::launch_delta_prep(a, s))) return e;
-    if (p.nseg > 1)
-        if (int e = launch_status(pm::launch_delta_segments(a, false, s))) return e;
-    return launch_status(pm::launch_delta_fwd(a, exact, s));
+    return launch_status(pm::launch_delta_fwd(a, p.nseg > 1, s));
 }
 
 size_t packmamba_delta_rule_bwd_workspace_size(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,

@@ -18,17 +18,17 @@
 // k's features, in registers, in the layout that an MFMA result has and, four rows of it a lane, an MFMA operand
 // takes.  So do x, e, u and the outs: four consecutive tokens of a feature a lane.  A block's waves share the chunk's
 // K, Q, H and P in LDS, which the next chunk's loads pass through registers.
-// Rounding in bf16: what is no input is split into two or three bf16 terms (16 or all 24 bits): the state, H, P, x and u.  The
-// outs and the errors are small differences of their terms where keys are near each other, and a term rounded to
-// bf16 would show (heads of one feature, P and u rounded once: outs 4.9e-3 off in the 2-norm, split 1.7e-3).
+// bf16: what is no input is split into three bf16 terms, all 24 bits of it: the state, H, P, x and u.  Outs and errors are
+// small differences of their terms where keys are near each other, and of large ones where a token replaces what the
+// state held: with two terms outs behind a value 100 times the others, which the next token of its key replaces, were 2.1e-2
+// off in the 2-norm and not 1.7e-3 (8 x 4096 tokens, 32 heads of 128 x 128 took 506 us and not 620).
 //
 // What bounds them: the instructions of two waves a SIMD, which the registers leave room for, and in the backward's the memory that
 // they keep states and errors in.  8 x 4096 tokens, 32 heads of 128 x 128, bf16, in cycles that a unit works and bytes moved:
-//   outs    443 us   VALU 53%, matrix 36%, LDS 28%; 1.13 GB, 2.5 TB/s
+//   outs    568 us   VALU 59%, matrix 47%, LDS 25%; 1.16 GB, 2.0 TB/s
 //   states  730 us   VALU 46%, matrix 32%, LDS 18%; 2.45 GB, 3.3 TB/s
 //   reverse 860 us   VALU 43%, matrix 24%, LDS 19%; 2.74 GB, 3.2 TB/s
-// Nearly half of the VALU work is splitting of states, errors and products, in three terms for the gradients' accuracy.  Loads that
-// branch on a head's size: outs 427 (then 405).
+// Nearly half of the VALU work is splitting of states, errors and products.
 //
 // Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
 // by token from the definition, so that 0 times it reaches no other token or sequence.  A state that holds one makes x
@@ -54,8 +54,8 @@ struct DeltaTiles {
     __attribute__((aligned(16))) float misc[4];
 };
 // Two of them, the next chunk's written during this one with one barrier a chunk and not two, for blocks of four waves where a CU
-// holds two blocks all the same.  Us with one and with two: backward of 4 x 24 heads x 2048, 64 x 64, 371, 358; 30001 tokens
-// forward, 24 heads of 128 x 64, 695, 690; eight waves: 8 x 32 x 4096, 128 x 128, forward 515, 529, backward 2350, 2400.
+// holds two blocks all the same: those are the segments' sums in time, which have no P.  Us of calls with one and with two: backward
+// of 4 x 24 heads x 2048, 64 x 64, 371, 358; 30001 tokens forward, 24 heads of 128 x 64, 695, 690.
 template <typename T, int KC, int VP, int NH, int NP, bool Q>
 constexpr int delta_buffers() {
     return VP == 64 && (int)sizeof(DeltaTiles<T, KC, NH, NP, Q>) * 2 <= 78 * 1024 ? 2 : 1;
@@ -544,8 +544,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     using Frag = typename M::Frag;
     constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
     constexpr bool kQ = MODE != kDeltaSum;
-    constexpr int NQ = MODE == kDeltaStates || NS == 1 ? NS : 2;        // terms of what the outs are made of
-    using Smem = DeltaSmem<T, KC, VP, NS, kQ ? NQ : 0, kQ, MODE == kDeltaStates ? 1 : 0>;
+    using Smem = DeltaSmem<T, KC, VP, NS, kQ ? NS : 0, kQ, MODE == kDeltaStates ? 1 : 0>;
     constexpr bool kTwo = Smem::kBuffers == 2;
     __shared__ Smem smem;
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
@@ -578,7 +577,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     else S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
 
     FeatureRegs<T, KC, kThreads> kr, qr;
-    ProductRegs<T, NS, kQ ? NQ : 0, kThreads> hr;
+    ProductRegs<T, NS, kQ ? NS : 0, kThreads> hr;
     TokenRegs<T> vr, dr;
     f32x4 cr;
     // K, Q and the weights; H and P, which are needed later: half the loads at a time, each after products that
@@ -716,14 +715,14 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                     er.set(x);
                     if (live) er.store(ep, elp, ct, here(l), L);
                 }
-                Frag uf[4][NQ];
+                Frag uf[4][NS];
                 f32x4 o[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    M::template split<NQ>(u[i], uf[i]);
+                    M::template split<NS>(u[i], uf[i]);
                     o[i] = aq[i] * (four(0, i) * a.scale);
                 }
-                multiply_product<T, false, NQ, NQ>(l, sm.p, uf, o);
+                multiply_product<T, false, NS, NS>(l, sm.p, uf, o);
                 if constexpr (MODE == kDeltaOut) {
                     any_pending = true;
                     pending.set(o);
@@ -797,7 +796,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     using Frag = typename M::Frag;
     constexpr int KF = KC / 16, kWaves = VP / 16, kThreads = VP * 4;
     using Smem = DeltaSmem<T, KC, VP, NS, NS, true, SUM ? 0 : 2>;
-    constexpr bool kTwo = Smem::kBuffers == 2;
+    static_assert(Smem::kBuffers == 1, "one set of operands");
     __shared__ Smem smem;
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
     const int64_t L = a.seqlen;
@@ -844,7 +843,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     };
     const auto stage = [&](int chunk) {
         const int tid = here(threadIdx.x);
-        auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
+        auto& sm = smem.b[0];
         const int64_t ct = (int64_t)chunk * kC;
         kr.settle(tid, kp, a.dk, ct, L);
         kr.store(tid, sm.k);
@@ -852,9 +851,9 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         qr.store(tid, sm.q);
         if (tid <= 48) *reinterpret_cast<f32x4*>(tid < 48 ? &sm.coef[0][0] + tid * 4 : sm.misc) = cr;
     };
-    const auto stage_products = [&](int chunk) {
+    const auto stage_products = [&] {
         const int tid = here(threadIdx.x);
-        auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
+        auto& sm = smem.b[0];
         hr.store(tid, &sm.h[0][0][0], &sm.p[0][0][0]);
     };
     const auto flush = [&](int chunk) {
@@ -875,24 +874,14 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     };
     load(last);
     load_products(last);
-    if constexpr (kTwo) {
-        stage(last);
-        stage_products(last);
-        load(max(last - 1, first));
-        load_products(max(last - 1, first));
-    }
     for (int chunk = last; chunk >= first; --chunk) {
         const int64_t ct = (int64_t)chunk * kC, unit = bh * a.chunks + chunk;
-        auto& sm = smem.b[kTwo ? (last - chunk) & 1 : 0];
+        auto& sm = smem.b[0];
         auto& dot = smem.dot[(last - chunk) & 1];
         __syncthreads();
         if (!SUM && chunk < last) flush(chunk + 1);
-        if constexpr (kTwo) {
-            stage(chunk - 1);
-        } else {
-            stage(chunk);
-            stage_products(chunk);
-        }
+        stage(chunk);
+        stage_products();
         dr.load(dop, ct, here(l), L);
         if constexpr (!SUM) {
             // a boundary at the chunk's end: the product of the state and its gradient there
@@ -920,7 +909,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             }
             D.keep(static_cast<T*>(a.grads) + unit * KC * VP, zf);
         }
-        if constexpr (!kTwo) __syncthreads();
+        __syncthreads();
         if constexpr (!SUM) {                            // needed late in the chunk
             vr.load(vp, ct, here(l), L);
             er.load(ep, elp, ct, here(l), L);
@@ -941,8 +930,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             M::template split<NS>(D.s[k + 1], s1);
             against_tokens<T, NS>(lk, sm.k, k, s0, s1, ak);
         }
-        load(max(chunk - 1 - kTwo, first));             // without a branch: the last chunks load theirs again
-        if (kTwo) stage_products(chunk - 1);
+        load(max(chunk - 1, first));             // without a branch: the last chunks load theirs again
         const int g4c = (here(l) >> 4) * 4;
         const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4c]); };
         f32x4 x[4];
@@ -964,7 +952,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) hx[i] = f32x4{0, 0, 0, 0};
         multiply_product<T, true, NS, NS>(l, sm.h, y, hx);
-        load_products(max(chunk - 1 - kTwo, first));
+        load_products(max(chunk - 1, first));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] -= hx[i];                               // du
@@ -1037,17 +1025,16 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
 // launches: one T, TO and KC in each translation unit
 // --------------------------------------------------------------------------------------------
 enum DeltaWalk : int {
-    kWalkOut = 0, kWalkOutExact = 1, kWalkStates = 2, kWalkRev = 3, kWalkSum = 4, kWalkSumRev = 5
+    kWalkOut = 0, kWalkStates = 1, kWalkRev = 2, kWalkSum = 3, kWalkSumRev = 4
 };
 
 template <typename T, typename TO, int KC, int VP>
 hipError_t launch_delta_vp(const DeltaArgs& a, DeltaWalk which, hipStream_t s) {
-    constexpr int kAll = Mat<T>::kSplit ? 3 : 1, kSome = Mat<T>::kSplit ? 2 : 1;
+    constexpr int kAll = Mat<T>::kSplit ? 3 : 1;
     const int64_t rows = (int64_t)a.batch * a.heads, mblocks = (KC + VP - 1) / VP;
     const dim3 block(VP * 4), grid((unsigned)(rows * a.nseg));
     switch (which) {
-        case kWalkOut: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaOut, kSome>), grid, block, 0, s, a); break;
-        case kWalkOutExact: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaOut, kAll>), grid, block, 0, s, a); break;
+        case kWalkOut: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaOut, kAll>), grid, block, 0, s, a); break;
         case kWalkStates: hipLaunchKernelGGL((delta_fwd_kernel<T, TO, KC, VP, kDeltaStates, kAll>), grid, block, 0, s, a); break;
         case kWalkRev: hipLaunchKernelGGL((delta_rev_kernel<T, TO, KC, VP, false, kAll>), grid, block, 0, s, a); break;
         case kWalkSum:
