@@ -29,11 +29,10 @@
  *   states    (batch, heads, dk, dv) float
  * dk, dv in [1, 128]; heads a multiple of groups; seqlen at most 2^22 and batch * heads * ceil(seqlen / 64)
  * at most 2^20.
- * Arithmetic: products accumulate in 32 bits and the state is held in 32 bits.  Out has 32-bit accuracy before its
- * last rounding, for all types, as have final states, dv, the initial state's gradient and those of beta and the decays
- * (a decay's gradient that of the sums of out . dout and v . dv that it is left of, over up to 256 tokens).  With bf16
- * inputs dq and dk have bf16's accuracy, also where PACKMAMBA_BF16_F32OUT returns 32 bits.  The same call gives the
- * same bits, and out the same with a final state and without.
+ * Arithmetic: products accumulate in 32 bits and the state is held in 32 bits.  All results have 32-bit accuracy, with
+ * bf16 inputs too, and out, dq, dk and dv are rounded to a bf16 output once (a decay's gradient has the accuracy of the
+ * sums of out . dout and v . dv that it is left of, over up to 256 tokens).  The same call gives the same bits, and out the
+ * same with a final state and without.
  * An infinity or NaN at token t reaches no other sequence and no other head (of q or k: no other group), and in
  * the forward no earlier token.  In the backward it may reach all gradients of its sequence and head (group).
  */

@@ -121,11 +121,12 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
 // One block a chunk, 64 features of k and grad_per heads of a group, whose sums stay in registers; wave w owns 16 tokens.  Mo
 // and Mv are made in both directions by the wave that needs them, as the operands they are next.  u is beta e: the
 // errors are what lies in memory.
-// In bf16 dv and the states are rounded once; e, Mo and Mv are split into two terms.
-// What bounds it: the waves' own work between two barriers a step, with two blocks a CU (67 KB of LDS) and all their registers:
-// 8 x 4096 tokens, 32 heads of 128 x 128 in 16 groups, 792 us for 2.7 GB, 3.4 TB/s.  e in one term: 665 us, but dq and dk 2.4e-3 off
-// and not 1.8e-3 (dk 3.0e-3 and not 2.5e-3 where a final state's gradient is large).  Masks of the weights where there are no
-// zeros and conditions as branches: 815 (then 692); all 128 features of k in a block of eight waves: 836 (then 755).
+// In bf16 all but the inputs is in three terms, as in the walks: what the state before the chunk holds and the chunk's tokens
+// replace cancels between (S dout) and Mo k, and between (S dv), (D u) and Mv.  32 features of v a step, so that two blocks of 70 KB of
+// LDS fit a CU.
+// What bounds it: VALU 59%, nearly a third of it splitting, and matrix 36% with two waves a SIMD (LDS 28%): 8 x 4096 tokens, 32 heads of
+// 128 x 128 in 16 groups, 1551 us for 4.1 GB, 2.6 TB/s.  States and dv rounded to bf16, e in two terms: 806 us, but dk as far off as it is
+// large where the gradient of the final state is 100 times dout's, and 1.8e-3 off and not 1.7e-3 elsewhere.
 // --------------------------------------------------------------------------------------------
 // 0 where the weight is, which an infinity or NaN must not pass
 __device__ __forceinline__ f32x4 masked(const f32x4& v, const f32x4& weight) {
@@ -137,25 +138,68 @@ __device__ __forceinline__ f32x4 masked(const f32x4& v, const f32x4& weight) {
 
 template <typename T>
 struct GradSmem {
+    static constexpr int kTerms = Mat<T>::kSplit ? 3 : 1, kRows = Mat<T>::kSplit ? 32 : 64;      // features of v a step
     __attribute__((aligned(16))) T k[64 * kC];
     __attribute__((aligned(16))) T q[64 * kC];
-    __attribute__((aligned(16))) T dout[64 * kC];
-    __attribute__((aligned(16))) T e[64 * kC];
-    __attribute__((aligned(16))) T low[Mat<T>::kSplit ? 64 * kC : 8];
-    __attribute__((aligned(16))) T w[64 * kC];
+    __attribute__((aligned(16))) T dout[kRows * kC];
+    __attribute__((aligned(16))) T e[kTerms][kRows * kC];
+    __attribute__((aligned(16))) T w[kTerms][kRows * kC];
     struct {
-        __attribute__((aligned(16))) T s[64 * 64];       // the state before, features of v by features of k
-        __attribute__((aligned(16))) T d[64 * 64];       // the gradient after
+        __attribute__((aligned(16))) T s[kTerms][kRows * 64];      // the state before, features of v by features of k
+        __attribute__((aligned(16))) T d[kTerms][kRows * 64];      // the gradient after
     } st;
     __attribute__((aligned(16))) float coef[kDeltaCoef];
 };
+
+// Values of 32 bits on their way into LDS as T's terms.
+template <int ROWS>
+__device__ __forceinline__ void store_terms(int tid, const TileRegs<float, ROWS, 256>& r, float (*tiles)[ROWS * 64]) {
+    r.store(tid, tiles[0]);
+}
+template <int ROWS>
+__device__ __forceinline__ void store_terms(int tid, const TileRegs<float, ROWS, 256>& r, bf16_t (*tiles)[ROWS * 64]) {
+    using Regs = TileRegs<float, ROWS, 256>;
+    const int row0 = tid / Regs::kLanes, c = tid % Regs::kLanes;                 // four values of a row, half a piece of 16 bytes
+    const int at = row0 * 64 + ((c >> 1) ^ Mat<bf16_t>::swz(row0)) * 8 + (c & 1) * 4;
+#pragma unroll
+    for (int i = 0; i < Regs::kPasses; ++i) {
+        u32x2 f[3];
+        Mat<bf16_t>::split<3>(__builtin_bit_cast(f32x4, r.w[i]), f);
+#pragma unroll
+        for (int n = 0; n < 3; ++n) *reinterpret_cast<u32x2*>(&tiles[n][at + i * Regs::kRowsPass * 64]) = f[n];
+    }
+}
+// The same of halves, upper ones rounded and lower (delta_walk.hpp); in 32 bits `hi` is all.
+template <typename T, int ROWS>
+__device__ __forceinline__ void store_halves(int tid, const TileRegs<T, ROWS, 256>& hi, const TileRegs<T, ROWS, 256>& lo, T (*tiles)[ROWS * kC]) {
+    if constexpr (Mat<T>::kSplit) {
+        TileRegs<T, ROWS, 256> f[3];
+#pragma unroll
+        for (int i = 0; i < TileRegs<T, ROWS, 256>::kPasses; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float a = whole(hi.w[i][r], lo.w[i][r], 0), b = whole(hi.w[i][r], lo.w[i][r], 1);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    f[n].w[i][r] = Mat<T>::high2(a, b);
+                    a -= Mat<T>::cut1(a);
+                    b -= Mat<T>::cut1(b);
+                }
+            }
+#pragma unroll
+        for (int n = 0; n < 3; ++n) f[n].store(tid, tiles[n]);
+    } else {
+        hi.store(tid, tiles[0]);
+    }
+}
 
 template <typename T, typename TO, int KC>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_kernel(DeltaArgs a) {
     using M = Mat<T>;
     using Frag = typename M::Frag;
-    using Regs = TileRegs<T, 64, 256>;
-    constexpr int NM = M::kSplit ? 2 : 1, kHalves = KC / 64;
+    constexpr int NM = GradSmem<T>::kTerms, VR = GradSmem<T>::kRows, NV = VR / 16, kHalves = KC / 64;
+    using Regs = TileRegs<T, VR, 256>;
+    using Wide = TileRegs<float, VR, 256>;
     __shared__ GradSmem<T> sm;
     const int l = lane_id(), w = wave_id(), col = l & 15, g4 = (l >> 4) * 4, tid = threadIdx.x;
     const int64_t L = a.seqlen;
@@ -166,39 +210,48 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     const int half = (int)(id % kHalves), part = (int)(row - bg * (uint32_t)parts);
     const int f0 = half * 64, frows = min(64, a.dk - f0);
     const bool few_k = !M::kSplit && frows <= 32;       // in 32 bits, where matrix instructions are slow: tiles without features are left out
-    const int vpad = a.dv <= 64 ? 64 : 128, vshift = a.dv <= 64 ? 0 : 1;
+    const int vpad = a.dv <= 64 ? 64 : 128, vsteps = (a.dv + VR - 1) / VR;
     const int h0 = (int)grp * rep + part * a.grad_per, h1 = min((int)(grp + 1) * rep, h0 + a.grad_per);
     const T* kp = static_cast<const T*>(a.k) + ((b * a.groups + grp) * a.dk + f0) * L;
     const T* qp = static_cast<const T*>(a.q) + ((b * a.groups + grp) * a.dk + f0) * L;
-    const uint32_t at = Regs::offset_of(tid, (int)t0, (int)L), sat = Regs::offset_of(tid, 0, KC);
+    const uint32_t at = Regs::offset_of(tid, (int)t0, (int)L), sat = Wide::offset_of(tid, 0, KC);
+    const int slots = delta_slots<T>(a.chunks);
 
     f32x4 dq[4], dk[4];
 #pragma unroll
     for (int f = 0; f < 4; ++f) dq[f] = dk[f] = f32x4{0, 0, 0, 0};
 
-    Regs dor, er, lr, wr, sr, gr;
+    Regs dor, er, lr, wr, xr;
+    Wide sr, gr;
     float cr[2];
-    const int steps = (h1 - h0) << vshift;
+    const int steps = (h1 - h0) * vsteps;
+    const auto rows_of_step = [&](int step) { return min(VR, a.dv - step % vsteps * VR); };
     const auto base = [&](const void* p, int step) {
-        const int h = h0 + (step >> vshift), v0 = (step & vshift) * 64;
+        const int h = h0 + step / vsteps, v0 = step % vsteps * VR;
         return static_cast<const T*>(p) + ((b * a.heads + h) * a.dv + v0) * L;
     };
     const auto load = [&](int step) {
-        const int h = h0 + (step >> vshift), v0 = (step & vshift) * 64, rows = min(64, a.dv - v0);
-        const int64_t unit = (b * a.heads + h) * a.chunks + chunk;
+        const int h = h0 + step / vsteps, v0 = step % vsteps * VR, rows = rows_of_step(step);
+        const int64_t bh = b * a.heads + h;
         dor.load(tid, at, base(a.dout, step), rows, (int)L);
         er.load(tid, at, base(a.e, step), rows, (int)L);
-        if constexpr (M::kSplit) lr.load(tid, at, base(a.e_low, step), rows, (int)L);
         wr.load(tid, at, base(a.w, step), rows, (int)L);
-        sr.load(tid, sat, static_cast<const T*>(a.states) + (unit * vpad + v0) * KC + f0, 64, KC);
-        gr.load(tid, sat, static_cast<const T*>(a.grads) + (unit * vpad + v0) * KC + f0, 64, KC);
-        cr[0] = a.coef[unit * kDeltaCoef + tid];
-        cr[1] = a.coef[unit * kDeltaCoef + min(tid + 256, kDeltaCoef - 1)];
+        if constexpr (M::kSplit) {
+            lr.load(tid, at, base(a.e_low, step), rows, (int)L);
+            xr.load(tid, at, base(a.w_low, step), rows, (int)L);
+        }
+        sr.load(tid, sat, a.states + ((bh * slots + chunk) * vpad + v0) * KC + f0, VR, KC);
+        gr.load(tid, sat, a.grads + ((bh * a.chunks + chunk) * vpad + v0) * KC + f0, VR, KC);
+        const float* cf = a.coef + (bh * a.chunks + chunk) * kDeltaCoef;
+        cr[0] = cf[tid];
+        cr[1] = cf[min(tid + 256, kDeltaCoef - 1)];
     };
     {
-        Regs kr, qr;
-        kr.load(tid, at, kp, frows, (int)L);
-        qr.load(tid, at, qp, frows, (int)L);
+        using Keys = TileRegs<T, 64, 256>;
+        Keys kr, qr;
+        const uint32_t kat = Keys::offset_of(tid, (int)t0, (int)L);
+        kr.load(tid, kat, kp, frows, (int)L);
+        qr.load(tid, kat, qp, frows, (int)L);
         load(0);                                        // blocks are short: all their first loads at once
         kr.settle(tid, kp, frows, t0, L);
         qr.settle(tid, qp, frows, t0, L);
@@ -209,29 +262,22 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
     // diagonal tile a second time for dk.  Mv's the same way.
     f32x4 mo[4], mv[4], mo_d, mv_d;
     for (int step = 0; step < steps; ++step) {
-        const bool first = (step & vshift) == 0, done = (step & vshift) == vshift;
-        const int rows = min(64, a.dv - (step & vshift) * 64);
+        const bool first = step % vsteps == 0, done = step % vsteps == vsteps - 1;
+        const int rows = rows_of_step(step);
         const bool few_v = !M::kSplit && rows <= 32;
         __syncthreads();
         dor.settle(tid, base(a.dout, step), rows, t0, L);
         er.settle(tid, base(a.e, step), rows, t0, L);
-        if constexpr (M::kSplit) {                      // what the rounding leaves of them
-            lr.settle(tid, base(a.e_low, step), rows, t0, L);
-#pragma unroll
-            for (int i = 0; i < Regs::kPasses; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t hi = er.w[i][r], lo = lr.w[i][r];
-                    lr.w[i][r] = pack_bf16x2(whole(hi, lo, 0) - __uint_as_float(hi << 16), whole(hi, lo, 1) - __uint_as_float(hi & 0xffff0000u));
-                }
-        }
         wr.settle(tid, base(a.w, step), rows, t0, L);
+        if constexpr (M::kSplit) {
+            lr.settle(tid, base(a.e_low, step), rows, t0, L);
+            xr.settle(tid, base(a.w_low, step), rows, t0, L);
+        }
         dor.store(tid, sm.dout);
-        er.store(tid, sm.e);
-        if constexpr (M::kSplit) lr.store(tid, sm.low);
-        wr.store(tid, sm.w);
-        sr.store(tid, sm.st.s);
-        gr.store(tid, sm.st.d);
+        store_halves<T, VR>(tid, er, lr, sm.e);
+        store_halves<T, VR>(tid, wr, xr, sm.w);
+        store_terms<VR>(tid, sr, sm.st.s);
+        store_terms<VR>(tid, gr, sm.st.d);
         sm.coef[tid] = cr[0];
         if (tid + 256 < kDeltaCoef) sm.coef[tid + 256] = cr[1];
         __syncthreads();
@@ -244,52 +290,55 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
 #pragma unroll
             for (int i = 0; i < 4; ++i) mo[i] = mv[i] = f32x4{0, 0, 0, 0};
         }
-        Frag dw[4], uw[4], lw[4], ww[4];
+        Frag dw[NV], uw[NM][NV], ww[NM][NV];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
+        for (int n = 0; n < NV; ++n) {
             dw[n] = tok(sm.dout, n, w);
-            uw[n] = tok(sm.e, n, w);
-            lw[n] = M::kSplit ? tok(sm.low, n, w) : Frag{};
-            ww[n] = tok(sm.w, n, w);
+#pragma unroll
+            for (int p = 0; p < NM; ++p) {
+                uw[p][n] = tok(sm.e[p], n, w);
+                ww[p][n] = tok(sm.w[p], n, w);
+            }
         }
+        // terms' products below the last term's size are left out, the small ones come first
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (i <= w) {
 #pragma unroll
-                for (int n = 0; n < 4; n += 2) {
+                for (int n = 0; n < NV; n += 2) {
                     if (n >= 2 && few_v) break;
-                    if constexpr (M::kSplit) {
-                        const Frag y0 = tok(sm.low, n, i), y1 = tok(sm.low, n + 1, i);
-                        mo[i] = M::mma(y0, y1, dw[n], dw[n + 1], mo[i]);
-                        mv[i] = M::mma(y0, y1, ww[n], ww[n + 1], mv[i]);
+#pragma unroll
+                    for (int p = NM - 1; p >= 0; --p) {
+                        const Frag x0 = tok(sm.e[p], n, i), x1 = tok(sm.e[p], n + 1, i);
+                        mo[i] = M::mma(x0, x1, dw[n], dw[n + 1], mo[i]);
+#pragma unroll
+                        for (int m = NM - 1 - p; m >= 0; --m) mv[i] = M::mma(x0, x1, ww[m][n], ww[m][n + 1], mv[i]);
                     }
-                    const Frag x0 = tok(sm.e, n, i), x1 = tok(sm.e, n + 1, i);
-                    mo[i] = M::mma(x0, x1, dw[n], dw[n + 1], mo[i]);
-                    mv[i] = M::mma(x0, x1, ww[n], ww[n + 1], mv[i]);
                 }
             } else {
 #pragma unroll
-                for (int n = 0; n < 4; n += 2) {
+                for (int n = 0; n < NV; n += 2) {
                     if (n >= 2 && few_v) break;
-                    const Frag x0 = tok(sm.dout, n, i), x1 = tok(sm.dout, n + 1, i), y0 = tok(sm.w, n, i), y1 = tok(sm.w, n + 1, i);
-                    if constexpr (M::kSplit) {
-                        mo[i] = M::mma(x0, x1, lw[n], lw[n + 1], mo[i]);
-                        mv[i] = M::mma(y0, y1, lw[n], lw[n + 1], mv[i]);
+                    const Frag x0 = tok(sm.dout, n, i), x1 = tok(sm.dout, n + 1, i);
+#pragma unroll
+                    for (int p = NM - 1; p >= 0; --p) {
+                        mo[i] = M::mma(x0, x1, uw[p][n], uw[p][n + 1], mo[i]);
+                        const Frag y0 = tok(sm.w[p], n, i), y1 = tok(sm.w[p], n + 1, i);
+#pragma unroll
+                        for (int m = NM - 1 - p; m >= 0; --m) mv[i] = M::mma(y0, y1, uw[m][n], uw[m][n + 1], mv[i]);
                     }
-                    mo[i] = M::mma(x0, x1, uw[n], uw[n + 1], mo[i]);
-                    mv[i] = M::mma(y0, y1, uw[n], uw[n + 1], mv[i]);
                 }
             }
         }
 #pragma unroll
-        for (int n = 0; n < 4; n += 2) {
+        for (int n = 0; n < NV; n += 2) {
             if (n >= 2 && few_v) break;
-            if constexpr (M::kSplit) {
-                mo_d = M::mma(dw[n], dw[n + 1], lw[n], lw[n + 1], mo_d);
-                mv_d = M::mma(ww[n], ww[n + 1], lw[n], lw[n + 1], mv_d);
+#pragma unroll
+            for (int p = NM - 1; p >= 0; --p) {
+                mo_d = M::mma(dw[n], dw[n + 1], uw[p][n], uw[p][n + 1], mo_d);
+#pragma unroll
+                for (int m = NM - 1 - p; m >= 0; --m) mv_d = M::mma(ww[p][n], ww[p][n + 1], uw[m][n], uw[m][n + 1], mv_d);
             }
-            mo_d = M::mma(dw[n], dw[n + 1], uw[n], uw[n + 1], mo_d);
-            mv_d = M::mma(ww[n], ww[n + 1], uw[n], uw[n + 1], mv_d);
         }
         {
             const f32x4 in = c4(kCoefIn, w), up = c4(kCoefUp, w) * c4(kCoefBeta, w), scaled = in * a.scale;
@@ -303,14 +352,19 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void delta_grads_ker
                     if (f >= 2 && few_k) break;
                     f32x4 q = {0, 0, 0, 0}, g = q, x = q;
 #pragma unroll
-                    for (int n = 0; n < 4; n += 2) {
+                    for (int n = 0; n < NV; n += 2) {
                         if (n >= 2 && few_v) break;
-                        const Frag s0 = tok(sm.st.s, n, f), s1 = tok(sm.st.s, n + 1, f);
-                        q = M::mma(dw[n], dw[n + 1], s0, s1, q);
-                        x = M::mma(ww[n], ww[n + 1], s0, s1, x);
-                        const Frag d0 = tok(sm.st.d, n, f), d1 = tok(sm.st.d, n + 1, f);
-                        if constexpr (M::kSplit) g = M::mma(lw[n], lw[n + 1], d0, d1, g);
-                        g = M::mma(uw[n], uw[n + 1], d0, d1, g);
+#pragma unroll
+                        for (int p = NM - 1; p >= 0; --p) {
+                            const Frag s0 = tok(sm.st.s[p], n, f), s1 = tok(sm.st.s[p], n + 1, f);
+                            const Frag d0 = tok(sm.st.d[p], n, f), d1 = tok(sm.st.d[p], n + 1, f);
+                            q = M::mma(dw[n], dw[n + 1], s0, s1, q);
+#pragma unroll
+                            for (int m = NM - 1 - p; m >= 0; --m) {
+                                x = M::mma(ww[m][n], ww[m][n + 1], s0, s1, x);
+                                g = M::mma(uw[m][n], uw[m][n + 1], d0, d1, g);
+                            }
+                        }
                     }
                     if constexpr (decltype(some)::value) {
                         q = masked(q, in);

@@ -31,14 +31,15 @@ struct DeltaArgs {
     float* seg;                 // the state that enters a segment (first what it adds), dk x dv
     float* seg_m;               // what it multiplies the state with, dk x dk padded to tiles
     int32_t* seg_cut;           // whether a sequence starts in it
-    // the backward's: per chunk the states before and the gradients after it, (dv, dk) in the inputs' type padded to tiles
-    void* states;
-    void* grads;
-    float* bound;               // the states at every bound_chunks chunks' end, in the threads' order
+    // the backward's: per chunk the states before and the gradients after it, (dv, dk) padded to tiles; bf16: also the row's last state
+    float* states;
+    float* grads;
+    float* bound;               // fp32: the states at every bound_chunks chunks' end again, in the threads' order
     float* dot;                 // their products with the gradients there, (batch, heads, nb + 1)
     void* e;                    // the errors, (batch, heads, dv, seqlen) in the inputs' type, rounded half up
     uint16_t* e_low;            // bf16: the lower halves of their fp32 patterns, as e
-    void* w;                    // dv, as e, where the out is of another type; else null
+    void* w;                    // dv, rounded, where the out is of another type; else null
+    uint16_t* w_low;            // bf16: what the rounding leaves of it, as e_low
     float* rq;                  // out . dout and -(v . dv) of every token
     float* rk;
     float* dbeta;

@@ -159,14 +159,18 @@ struct BwdExtra {
 BwdExtra take_bwd(Taker& t, pm::DeltaArgs& a, const Plan& p, int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv,
                   int64_t seqlen, int32_t dtype) {
     const int64_t rows = batch * heads, state = (int64_t)pm::delta_pad((int32_t)dk) * pm::delta_pad((int32_t)dv);
-    const size_t size = dtype == PACKMAMBA_F32 ? 4 : 2;
+    const bool f32 = dtype == PACKMAMBA_F32;
+    const size_t size = f32 ? 4 : 2;
     take_common(t, a, p, rows, dk, dv);
-    a.states = t.take(size * (size_t)(p.units * state));
-    a.grads = t.take(size * (size_t)(p.units * state));
-    a.bound = t.floats(rows * p.nb * state);
+    a.states = t.floats((f32 ? p.units : p.units + rows) * state);
+    a.grads = t.floats(p.units * state);
+    a.bound = f32 ? t.floats(rows * p.nb * state) : nullptr;
     a.dot = t.floats(rows * (p.nb + 1));
     a.e = t.take(size * (size_t)(rows * dv * seqlen));
-    if (dtype != PACKMAMBA_F32) a.e_low = static_cast<uint16_t*>(t.take(size * (size_t)(rows * dv * seqlen)));
+    if (!f32) {
+        a.e_low = static_cast<uint16_t*>(t.take(size * (size_t)(rows * dv * seqlen)));
+        a.w_low = static_cast<uint16_t*>(t.take(size * (size_t)(rows * dv * seqlen)));
+    }
     a.w = dtype == PACKMAMBA_BF16_F32OUT ? t.take(size * (size_t)(rows * dv * seqlen)) : nullptr;
     a.rq = t.floats(rows * seqlen);
     a.rk = t.floats(rows * seqlen);

@@ -26,8 +26,8 @@
 // What bounds them: the instructions of two waves a SIMD, which the registers leave room for, and in the backward's the memory that
 // they keep states and errors in.  8 x 4096 tokens, 32 heads of 128 x 128, bf16, in cycles that a unit works and bytes moved:
 //   outs    568 us   VALU 59%, matrix 47%, LDS 25%; 1.16 GB, 2.0 TB/s
-//   states  730 us   VALU 46%, matrix 32%, LDS 18%; 2.45 GB, 3.3 TB/s
-//   reverse 860 us   VALU 43%, matrix 24%, LDS 19%; 2.74 GB, 3.2 TB/s
+//   states  754 us   VALU 45%, matrix 32%, LDS 17%; 2.78 GB, 3.7 TB/s
+//   reverse 873 us   VALU 44%, matrix 24%, LDS 19%; 3.60 GB, 4.1 TB/s
 // Nearly half of the VALU work is splitting of states, errors and products.
 //
 // Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
@@ -207,6 +207,12 @@ struct TokenRegs {
     }
 };
 
+// What a value's pattern of 32 bits is over that of its bf16 rounding (as 32 bits): 16 bits, a signed number; where a tie went down
+// one less.
+__device__ __forceinline__ uint32_t rest_of(float v, uint32_t rounded) {
+    return (uint32_t)max(min((int32_t)(__float_as_uint(v) - rounded), 0x7fff), -0x8000) & 0xffffu;
+}
+
 // 16 bits a token that are no numbers, as TokenRegs has a row's bf16.
 struct HalfRegs : TokenRegs<bf16_t> {
     __device__ void load(const uint16_t* p, int64_t t0, int l, int64_t L) {
@@ -220,6 +226,19 @@ struct HalfRegs : TokenRegs<bf16_t> {
                     const int64_t t = t0 + at(l, i) + r;
                     w[i][r / 2] = (t < L ? p[t] : 0u) | (uint32_t)(t + 1 < L ? p[t + 1] : 0u) << 16;
                 }
+        }
+    }
+    // what TokenRegs<bf16_t>::set() leaves of the values
+    __device__ void set_rest(const f32x4 (&v)[4]) {
+        const auto pair = [](float x, float y, uint32_t rounded) { return rest_of(x, rounded << 16) | rest_of(y, rounded & 0xffff0000u) << 16; };
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x4 &x = v[2 * i], &y = v[2 * i + 1];
+            const u32x2 xr = Mat<bf16_t>::round(x), yr = Mat<bf16_t>::round(y);
+            uint32_t a = pair(x.x, x.y, xr.x), b = pair(x.z, x.w, xr.y), c = pair(y.x, y.y, yr.x), d = pair(y.z, y.w, yr.y);
+            swap(a, c);
+            swap(b, d);
+            w[i] = u32x4{a, b, c, d};
         }
     }
     __device__ void store(uint16_t* p, int64_t t0, int l, int64_t L) const {
@@ -318,6 +337,10 @@ __device__ __forceinline__ void store_tokens(TO* row, int64_t t, int64_t L, cons
     }
 }
 
+// States of a row that the backward keeps: those before its chunks, and in bf16 the last one, in place of `bound`.
+template <typename T>
+__host__ __device__ constexpr int delta_slots(int chunks) { return Mat<T>::kSplit ? chunks + 1 : chunks; }
+
 // The state: rows 16 k + 4 (lane / 16) .. + 3, column lane % 16 of the wave's 16.
 template <int KF>
 struct DeltaState {
@@ -357,14 +380,19 @@ struct DeltaState {
 #pragma unroll
         for (int k = 0; k < KF; ++k) s[k] = f32x4{0, 0, 0, 0};
     }
-    // transposed, rounded to T: column z is a row of KF * 16
-    template <typename T>
-    __device__ void keep(T* p, int zf) {
+    // transposed: column z is a row of KF * 16
+    __device__ void keep(float* p, int zf) {
+        each([&](int x, int z, f32x4& v) { *reinterpret_cast<f32x4*>(p + (zf + z) * (KF * 16) + x) = v; });
+    }
+    // the sum of the products with what keep() left
+    __device__ float dot_kept(const float* p, int zf) {
+        float d = 0.0f;
         each([&](int x, int z, f32x4& v) {
-            T* to = p + (int64_t)(zf + z) * (KF * 16) + x;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = Mat<T>::round(v);
-            else *reinterpret_cast<f32x4*>(to) = v;
+            const f32x4 o = *reinterpret_cast<const f32x4*>(p + (zf + z) * (KF * 16) + x);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d = fmaf(o[r], v[r], d);
         });
+        return d;
     }
     // one token, of which column f of a tile is the key's or query's: sum over the rows of it times the column
     template <typename T>
@@ -664,8 +692,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
         }
         const bool bad = __builtin_amdgcn_readfirstlane(__float_as_int(sm.misc[1])) != 0;
         if constexpr (MODE == kDeltaStates) {
-            S.keep(static_cast<T*>(a.states) + unit * KC * VP, zf);
-            if (chunk > 0 && chunk % a.bound_chunks == 0) {
+            S.keep(a.states + (bh * delta_slots<T>(a.chunks) + chunk) * KC * VP, zf);
+            if (!M::kSplit && chunk > 0 && chunk % a.bound_chunks == 0) {
                 float* p = a.bound + ((bh * a.nb + chunk / a.bound_chunks - 1) * KF * kThreads + tid) * 4;
 #pragma unroll
                 for (int k = 0; k < KF; ++k) *reinterpret_cast<f32x4*>(p + k * 4 * kThreads) = S.s[k];
@@ -768,7 +796,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     if constexpr (MODE == kDeltaStates) {
         __syncthreads();
         flush(last);
-        if (last == a.chunks - 1 && a.bound_end) {
+        if (M::kSplit && last == a.chunks - 1 && a.bound_end) S.keep(a.states + (bh * delta_slots<T>(a.chunks) + a.chunks) * KC * VP, zf);
+        if (!M::kSplit && last == a.chunks - 1 && a.bound_end) {
             float* p = a.bound + ((bh * a.nb + a.nb - 1) * KF * kThreads + tid) * 4;
 #pragma unroll
             for (int k = 0; k < KF; ++k) *reinterpret_cast<f32x4*>(p + k * 4 * kThreads) = S.s[k];
@@ -817,6 +846,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
     const T* ep = SUM ? nullptr : static_cast<const T*>(a.e) + zrow * L;
     const uint16_t* elp = !SUM && M::kSplit ? a.e_low + zrow * L : nullptr;
     T* wp = SUM || !a.w ? nullptr : static_cast<T*>(a.w) + zrow * L;      // a copy in T, where the out has another type
+    uint16_t* wlp = !SUM && M::kSplit ? a.w_low + zrow * L : nullptr;
     const float* betap = a.beta + bh * L;
     const bool few = KF == 4 && a.dk <= 32;              // half of the state's rows are none
 
@@ -888,13 +918,17 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             const int next = chunk + 1;
             if (next < a.chunks ? next % a.bound_chunks == 0 : a.bound_end != 0) {          // block-uniform
                 const int64_t n = (next + a.bound_chunks - 1) / a.bound_chunks;
-                const float* p = a.bound + ((bh * a.nb + n - 1) * KF * kThreads + tid) * 4;
                 float v = 0.0f;
+                if constexpr (M::kSplit) {
+                    v = D.dot_kept(a.states + (bh * delta_slots<T>(a.chunks) + next) * KC * VP, zf);
+                } else {
+                    const float* p = a.bound + ((bh * a.nb + n - 1) * KF * kThreads + tid) * 4;
 #pragma unroll
-                for (int k = 0; k < KF; ++k) {
-                    const f32x4 o = *reinterpret_cast<const f32x4*>(p + k * 4 * kThreads);
+                    for (int k = 0; k < KF; ++k) {
+                        const f32x4 o = *reinterpret_cast<const f32x4*>(p + k * 4 * kThreads);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v = fmaf(o[r], D.s[k][r], v);
+                        for (int r = 0; r < 4; ++r) v = fmaf(o[r], D.s[k][r], v);
+                    }
                 }
 #pragma unroll
                 for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
@@ -907,7 +941,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                     a.dot[bh * (a.nb + 1) + n] = v;
                 }
             }
-            D.keep(static_cast<T*>(a.grads) + unit * KC * VP, zf);
+            D.keep(a.grads + unit * KC * VP, zf);
         }
         __syncthreads();
         if constexpr (!SUM) {                            // needed late in the chunk
@@ -930,7 +964,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
             M::template split<NS>(D.s[k + 1], s1);
             against_tokens<T, NS>(lk, sm.k, k, s0, s1, ak);
         }
-        load(max(chunk - 1, first));             // without a branch: the last chunks load theirs again
+        load(max(chunk - 1, first));                    // without a branch: the last chunks load theirs again
         const int g4c = (here(l) >> 4) * 4;
         const auto four = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&sm.coef[which][i * 16 + g4c]); };
         f32x4 x[4];
@@ -968,6 +1002,11 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                     copy.set(dv);
                     if (live) copy.store(wp, ct, here(l), L);
                 }
+                if constexpr (M::kSplit) {
+                    HalfRegs low;
+                    low.set_rest(dv);
+                    if (live) low.store(wlp, ct, here(l), L);
+                }
                 Frag vf[4];
                 vr.get(mask, vf);
 #pragma unroll
@@ -1004,6 +1043,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                     if (g4 == 0 && live && in) {
                         Storage<TO>::store1(op + t, dvt);
                         if (wp) Storage<T>::store1(wp + t, dvt);
+                        if constexpr (M::kSplit) wlp[t] = (uint16_t)rest_of(dvt, Mat<T>::round(f32x4{dvt, 0, 0, 0}).x << 16);
                     }
                 }
                 D.add(sm.k, j, -dvt);
