@@ -365,11 +365,12 @@ struct DeltaState {
                 if (x + r < rows && zf + z < cols) p[(int64_t)(x + r) * stride + zf + z] = v[r];
         });
     }
-    // columns of the identity from zf on
-    __device__ void identity(int zf) {
+    // columns of the identity of `rows` from zf on: ones of rows that no key has would only be decayed, where decays are above 0 to
+    // infinities, whose products with the 0 that the state holds there are none
+    __device__ void identity(int zf, int rows) {
         each([&](int x, int z, f32x4& v) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = x + r == zf + z ? 1.0f : 0.0f;
+            for (int r = 0; r < 4; ++r) v[r] = x + r == zf + z && x + r < rows ? 1.0f : 0.0f;
         });
     }
     __device__ void decay(float a) {
@@ -601,7 +602,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
     DeltaState<KF> S;
     const int64_t sz = (int64_t)a.dk * a.dv;
     if (MODE == kDeltaSum && mb == 0) S.load(nullptr, 0, 0, 0, 0);
-    else if (MODE == kDeltaSum) S.identity((int)(mb - 1) * VP + zf);
+    else if (MODE == kDeltaSum) S.identity((int)(mb - 1) * VP + zf, a.dk);
     else S.load(a.nseg > 1 ? a.seg + (bh * a.nseg + seg) * sz : a.entry ? a.entry + bh * sz : nullptr, a.dk, a.dv, zf, a.dv);
 
     FeatureRegs<T, KC, kThreads> kr, qr;

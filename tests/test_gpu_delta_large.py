@@ -48,7 +48,8 @@ def near(got, ref, tokens, size, dk, rounded, name):
     rel = ((got - ref)[..., tokens].norm() / ref[..., tokens].norm()).item()
     tol = (4e-6 + dk * 2.0 ** -24) * max(C, 1) + (HALF / 3 ** 0.5 if rounded else 0)
     note(f"  {name} {rel:.2g} off of {tol:.2g}, terms {C:.2g} times the results")
-    assert bool(got.isfinite().all()) and rel <= tol, f"{name}: {rel:.2g} off, {tol:.2g} allowed"
+    finite = bool(got.isfinite().all())
+    assert finite and rel <= tol, f"{name}: {rel:.2g} off, {tol:.2g} allowed"
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
