@@ -26,6 +26,9 @@
  *   decay     log decays, float: (batch, heads, seqlen) if decay_per_token, else (heads); NULL: 0.
  *             A value of -104 or less (exp of it is 0 in 32 bits; -infinity too) cuts as a start
  *             does.
+ *             Values above 0 are taken as they are; where those of a sequence's tokens in a row sum to more
+ *             than 88 over 64 tokens or fewer, their exponentials' products are infinite in 32 bits, and what
+ *             they meet may become infinite or NaN though the state itself is not.
  *   states    (batch, heads, dk, dv) float
  * dk, dv in [1, 128]; heads a multiple of groups; seqlen at most 2^22 and batch * heads * ceil(seqlen / 64)
  * at most 2^20.

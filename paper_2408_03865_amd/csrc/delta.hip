@@ -30,7 +30,7 @@ hipError_t walk(const DeltaArgs& a, DeltaWalk which, hipStream_t s) {
 // the segment), in place of what is added; backwards with M's transpose.  A block takes 16 columns of the state of one
 // row and head, its waves 16 rows each; products in 32 bits.
 // What bounds it: a step's way through LDS, 32 matrix instructions in 32 bits (16 with keys of 64) and a block's 64 KB of M, on their
-// way for one step: 24 heads of 128 x 64 in 18 segments 51 us (the sums one after the other, M loaded after the products: 66),
+// way for one step: 24 heads of 128 x 64 in 18 segments 54 us (the sums one after the other, M loaded after the products: 66),
 // 96 of 64 x 64 in four 8.6.
 // --------------------------------------------------------------------------------------------
 template <int KC, bool REV>
@@ -93,13 +93,31 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
         for (int j = 0; j < KF; ++j) c[j] = cur[i][j][l];
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = f32x4{0, 0, 0, 0};
-        if (!cut[i]) {                                  // the sums in turns: a matrix instruction waits for the one whose result it takes
+        if (!cut[i]) {
+            f32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < KF; j += 4)
+            for (int j = 0; j < KF; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) zero[e] = fmaf(m[i][j][e], 0.0f, zero[e]);
+            if (__ballot(!((zero.x + zero.y) + (zero.z + zero.w) == 0.0f)) == 0) {       // the sums in turns: a matrix instruction waits for the one whose result it takes
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) sum[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i][j + q][e], c[j + q][e], sum[q], 0, 0, 0);
+                for (int j = 0; j < KF; j += 4)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) sum[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i][j + q][e], c[j + q][e], sum[q], 0, 0, 0);
+            } else {                                    // decays above 0, or k is not finite: what is 0 stays 0 whatever it is multiplied with
+                const float* M = a.seg_m + seg(min(n, a.nseg - 2)) * KC * KC;
+#pragma unroll 1
+                for (int x = 0; x < KC; ++x) {
+                    const float v = reinterpret_cast<const float*>(&cur[i][x >> 4][((x >> 2) & 3) * 16 + col])[x & 3];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int y = w * 16 + g4 + r;
+                        sum[0][r] += v == 0.0f ? 0.0f : (REV ? M[x * KC + y] : M[y * KC + x]) * v;
+                    }
+                }
+            }
         }
         own = lives(added[i]) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
         float* p = a.seg + seg(n) * sz;

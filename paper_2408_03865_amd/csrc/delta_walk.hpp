@@ -395,15 +395,19 @@ struct DeltaState {
         });
         return d;
     }
-    // one token, of which column f of a tile is the key's or query's: sum over the rows of it times the column
+    // one token, of which column j of a tile is the key's or query's: sum over the rows of it times the column.  absent: a row that it
+    // has 0 of is not met, also where the state is infinite there
     template <typename T>
-    __device__ float against(const T* tile, int j) {
+    __device__ float against(const T* tile, int j, bool absent = false) {
         const int l = here(lane_id());
         float v = 0.0f;
 #pragma unroll
         for (int k = 0; k < KF; ++k) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v = fmaf(tile_value(tile + k * 16 * kC, (l >> 4) * 4 + r, j), s[k][r], v);
+            for (int r = 0; r < 4; ++r) {
+                const float x = tile_value(tile + k * 16 * kC, (l >> 4) * 4 + r, j);
+                v = absent && x == 0.0f ? v : fmaf(x, s[k][r], v);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         v += __shfl_xor(v, 16);
@@ -776,7 +780,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_fwd_kernel(DeltaArgs a) {
                 if (start) S.clear();
                 else S.decay(mult);
                 const float beta = t < L ? betap[t] : 0.0f;
-                const float e = (live && t < L ? Storage<T>::load1(vp + t) : 0.0f) - S.against(sm.k, j);
+                const float e = (live && t < L ? Storage<T>::load1(vp + t) : 0.0f) - S.against(sm.k, j, mb > 0);
                 const float ut = t < L ? beta * e : 0.0f;
                 S.add(sm.k, j, ut);
                 if constexpr (kQ) {

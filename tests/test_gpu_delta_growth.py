@@ -54,3 +54,53 @@ def test_decays_above_zero(shape, g, states, dtype):
     for name in NAMES:
         if got[name] is not None:
             near(got[name], ref[name], name, g, dtype)
+
+
+LONG = (1, 128, 32, 3, 8, 9200)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nothing_grows_to_nothing(dtype):
+    """States of 0 that are only decayed, by more than 32 bits hold over a segment, stay 0: a row whose first 5000 tokens write
+    nothing, and heads that write and ask for nothing at all."""
+    g, quiet = 0.042, 5000
+    note(f"delta rule, decays of {g} over empty states, {dtype}")
+    d = growing(LONG, dtype, g, False)
+    d["beta"][..., :quiet] = 0.0
+    ref, _ = reference(d, back=False)
+    out, fin = forward(cuda(d))
+    near(out, ref["out"], "out", g, dtype)
+    near(fin, ref["final_state"], "final_state", g, dtype)
+    assert not bool(out[..., :quiet].any())
+    d = growing(LONG, dtype, g, False)
+    d["beta"][:, :8] = 0.0
+    d["dout"][:, :8] = 0.0
+    ref, _ = reference(d)
+    c = cuda(d)
+    out, _ = forward(c)
+    near(out, ref["out"], "out", g, dtype)
+    got = backward(c)
+    for name in ("dq", "dk", "dv", "dbeta", "ddecay"):
+        near(got[name], ref[name], name, g, dtype)
+        quiet_part = got[name][:, :8 // (4 if name in ("dq", "dk") else 1)]
+        assert not bool(quiet_part.any()), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_features_of_zeros(dtype):
+    """Heads filled up with features that no key and no query has: what they would hold is only decayed, and stays 0."""
+    import torch
+    g, shape = 0.042, (1, 128, 32, 5, 8, 9200)
+    note(f"delta rule, decays of {g} over empty features, {dtype}")
+    d = growing(shape, dtype, g, False)
+    three = growing(LONG, dtype, g, False)
+    for n in "qk":
+        d[n] = torch.cat([three[n], torch.zeros_like(three[n][:, :, :2])], 2).contiguous()
+    ref, _ = reference(d)
+    c = cuda(d)
+    out, fin = forward(c)
+    near(out, ref["out"], "out", g, dtype)
+    near(fin, ref["final_state"], "final_state", g, dtype)
+    got = backward(c)
+    for name in ("dq", "dk", "dv", "dbeta", "ddecay"):
+        near(got[name], ref[name], name, g, dtype)
