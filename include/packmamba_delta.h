@@ -73,7 +73,7 @@ size_t packmamba_delta_rule_bwd_workspace_size(int64_t batch, int64_t heads, int
 /*
  * Backward: gradients of sum(dout * out) + sum(dfinal_state * final_state), from the inputs alone.
  *   dq, dk (batch, groups, dk, seqlen) and dv (batch, heads, dv, seqlen) in the dtype's output type; dq
- *   and dk are summed over the heads of a group in 32 bits, in the heads' order.
+ *   and dk are summed over the heads of a group in 32 bits, in an order that the call's sizes fix.
  *   dbeta (batch, heads, seqlen) float.
  *   ddecay: NULL, or decay's shape, float; 0 at a start (a cut multiplier is a constant).  It must
  *   be NULL where decay is.  dinitial_state: NULL iff initial_state is; it may be dfinal_state's

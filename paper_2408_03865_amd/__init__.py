@@ -24,15 +24,16 @@ final-state gradients (dfinal_x, dfinal_state).
 Linear attention with a decay for each head over the same packed rows, its single-token form and the gated
 RMSNorm (``include/packmamba_linear.h``) are in ``linear.py``:
     out, state = linear_attention_fwd(q, k, v, decay, position_indices, return_final=True)
-    out = linear_attention_step(q, k, v, decay, state)
-    y, rstd = gated_rmsnorm_fwd(out, z, weight, groups=heads)
+    y, rstd = gated_rmsnorm_fwd(out.flatten(1, 2), z, weight, groups=heads)     # (batch, heads * dv, seqlen)
+    out = linear_attention_step(q1, k1, v1, decay1, state)                      # one token
 
 The gated delta rule over packed rows, its single-token form (``delta.py``), the norm of its keys and queries and the layer
 norm (``norms.py``; all in ``include/packmamba_delta.h``):
-    k, rnorm = head_l2norm_fwd(k, groups=heads)
+    h, mean, rstd = layernorm_fwd(x, weight, bias)
+    k, rnorm = head_l2norm_fwd(k, groups=groups)                                # (batch, groups * dk, seqlen)
+    k = k.unflatten(1, (groups, -1))                                            # (batch, groups, dk, seqlen), as q
     out, state = delta_rule_fwd(q, k, v, beta, decay, position_indices, return_final=True)
-    out = delta_rule_step(q, k, v, beta, decay, state)
-    y, mean, rstd = layernorm_fwd(x, weight, bias)
+    out = delta_rule_step(q1, k1, v1, beta1, decay1, state)                     # one token
 """
 from __future__ import annotations
 

@@ -11,8 +11,10 @@
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int64_t kMaxSeqlen = (int64_t)1 << 22;    // 64 rows of it in fp32 are an offset of 32 bits in the walks
-constexpr int64_t kMaxUnits = (int64_t)1 << 20;     // chunks of all rows and heads: up to 340 KB of workspace each
+constexpr int64_t kMaxSeqlen = (int64_t)1 << 22;    // 128 rows of it in fp32 are an offset of 32 bits in the walks
+// Chunks of all rows and heads: up to 382 KB of workspace each in a backward of two heads that share keys, some hundred tokens and
+// segments of two chunks, 215 KB in the largest calls.
+constexpr int64_t kMaxUnits = (int64_t)1 << 20;
 
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 inline size_t floats(int64_t n) { return align_up(sizeof(float) * (size_t)n); }
