@@ -34,7 +34,7 @@
  * at most 2^20.
  * Arithmetic: products accumulate in 32 bits and the state is held in 32 bits.  All results have 32-bit accuracy, with
  * bf16 inputs too, and out, dq, dk and dv are rounded to a bf16 output once (a decay's gradient has the accuracy of the
- * sums of out . dout and v . dv that it is left of, over up to 256 tokens).  The same call gives the same bits, and out the
+ * sums of out . dout and v . dv that it is left of, over up to 64 tokens, or 256 in fp32).  The same call gives the same bits, and out the
  * same with a final state and without.
  * An infinity or NaN at token t reaches no other sequence and no other head (of q or k: no other group), and in
  * the forward no earlier token.  In the backward it may reach all gradients of its sequence and head (group).

@@ -64,13 +64,14 @@ struct Plan {
     int32_t nseg, seg_chunks, bound, nb, heads_per, grad_per, grad_parts;
 };
 // Chunks between the boundaries at which the backward multiplies the two states.  A decay's gradient is a sum over the tokens up
-// to the next, of terms that cancel: its error grows with their number, and the boundaries' fp32 states move memory.  With 1, 2, 4
-// and 8 chunks, us and errors in the 2-norm:
-//   8 x 32 heads x 4096 (16384 chunks of heads), 128 x 128, bf16    -, 2480, 2375, 2340; -, -, 7.8e-7, 1.0e-6 (the plain form 5.6e-7)
-//   4 x 24 x 2048 (3072), 64 x 64, bf16                             369, 361, 359, -
-//   1 x 2 x 256 (8), 24 x 32, fp32, decays of a head                91.6, 89.9, 89.8, -; 1.2e-4, 1.5e-4, 1.7e-4, - of sums near 200
-//                                                                   (the plain form 1.6e-4)
-int32_t bound_chunks(int64_t units) { return units <= 1024 ? 1 : units <= 4096 ? 2 : 4; }
+// to the next, of terms that cancel: its error grows with their number.  In bf16 every chunk ends at one, whose state the gradients
+// keep anyway; in fp32 boundaries have a copy of it, which moves memory.  Us with 1, 2 and 4 chunks by the chunks of all heads:
+//   fp32   512 (64 x 64) 221, 217, 216    1024 283, 279, 278    2048 480, 471, 470    3072 752, 740, 735    4096 888, 868, 865, of
+//          128 x 128 2445, 2367, 2328    8192 (64 x 64) 1413, 1363, 1338    16384 (128 x 128) 6950, 6750, 6670: 1 costs 2% to 1024, 2 1% or
+//          less to 4096 but for 128 x 128; errors in the 2-norm 5.0e-7 to 5.8e-7, 6.1e-7 to 8.1e-7, 8.0e-7 to 1.1e-6
+//   bf16   3072 397, 391, 393    4096 (128 x 128) 1119, 1091, 1080    16384 (128 x 128) 3328, 3241, 3209; errors of the last 4.5e-7, 6.0e-7,
+//          7.9e-7 (the plain form 5.6e-7)
+int32_t bound_chunks(int64_t units, bool f32) { return !f32 || units <= 1024 ? 1 : units <= 4096 ? 2 : 4; }
 // Heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks.  Us with this rule, with
 // all heads of a group in a block and with one (batch x heads in groups x tokens, dk x dv; bf16):
 //   the preparation, forward    1 x 32 in 1 x 512, 128 x 128: 50, 183, 50    2 x 64 in 4 x 2048, 128 x 128: 192, 222, 192
@@ -116,14 +117,14 @@ int64_t segment_chunks(int64_t rows, int64_t dk, int64_t dv, int64_t chunks, boo
     return best;
 }
 
-Plan make_plan(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv, int64_t seqlen, bool backward) {
+Plan make_plan(int64_t batch, int64_t heads, int64_t groups, int64_t dk, int64_t dv, int64_t seqlen, bool backward, bool f32 = false) {
     Plan p;
     p.chunks = (seqlen + pm::kLinChunk - 1) / pm::kLinChunk;
     const int64_t rows = batch * heads, per = segment_chunks(rows, dk, dv, p.chunks, backward);
     p.units = rows * p.chunks;
     p.seg_chunks = (int32_t)per;
     p.nseg = (int32_t)((p.chunks + per - 1) / per);
-    p.bound = bound_chunks(p.units);
+    p.bound = bound_chunks(p.units, f32);
     p.nb = (int32_t)((p.chunks + p.bound - 1) / p.bound);
     const int64_t rep = heads / groups, blocks = batch * p.chunks * groups;
     p.heads_per = heads_for(blocks, rep, 1024);
@@ -239,7 +240,7 @@ size_t packmamba_delta_rule_bwd_workspace_size(int64_t batch, int64_t heads, int
     if (check_heads(batch, heads, groups, dk, dv, seqlen) || check_dtype(dtype)) return 0;
     Taker t{nullptr};
     pm::DeltaArgs a{};
-    take_bwd(t, a, make_plan(batch, heads, groups, dk, dv, seqlen, true), batch, heads, groups, dk, dv, seqlen, dtype);
+    take_bwd(t, a, make_plan(batch, heads, groups, dk, dv, seqlen, true, dtype == PACKMAMBA_F32), batch, heads, groups, dk, dv, seqlen, dtype);
     return t.at;
 }
 
@@ -257,7 +258,7 @@ int packmamba_delta_rule_bwd(const void* q, const void* k, const void* v, const 
     if (!aligned16(q, k, v, beta, decay, position_indices, initial_state, dout, dfinal_state) ||
         !aligned16(dq, dk, dv, dbeta, ddecay, dinitial_state, workspace))
         return PACKMAMBA_ERR_ALIGN;
-    const Plan p = make_plan(batch, heads, groups, dk_size, dv_size, seqlen, true);
+    const Plan p = make_plan(batch, heads, groups, dk_size, dv_size, seqlen, true, dtype == PACKMAMBA_F32);
     Taker t{static_cast<char*>(workspace)};
     pm::DeltaArgs a{};
     const BwdExtra x = take_bwd(t, a, p, batch, heads, groups, dk_size, dv_size, seqlen, dtype);

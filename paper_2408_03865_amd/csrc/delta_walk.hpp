@@ -65,7 +65,7 @@ struct DeltaSmem {
     static constexpr int kBuffers = delta_buffers<T, KC, VP, NH, NP, Q>();
     DeltaTiles<T, KC, NH, NP, Q> b[kBuffers];
     __attribute__((aligned(16))) float dot[2][DOTS ? DOTS : 1][VP / 16][kC];
-    float xdot[VP / 16];
+    float xdot[2][VP / 16];
 };
 
 __host__ __device__ constexpr int delta_tile(int i, int j) { return i * (i + 1) / 2 + j; }
@@ -891,6 +891,8 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         auto& sm = smem.b[0];
         hr.store(tid, &sm.h[0][0][0], &sm.p[0][0][0]);
     };
+    const auto bounded = [&](int chunk) { return chunk + 1 < a.chunks ? (chunk + 1) % a.bound_chunks == 0 : a.bound_end != 0; };
+    const auto bound_of = [&](int next) { return (next + a.bound_chunks - 1) / a.bound_chunks; };
     const auto flush = [&](int chunk) {
         if constexpr (!SUM) {
             const auto& dot = smem.dot[(last - chunk) & 1];
@@ -904,6 +906,13 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                 }
                 a.rk[bh * L + t] = -v;
                 a.dbeta[bh * L + t] = d;
+            }
+            if (tid == kC && bounded(chunk)) {
+                const float* x = smem.xdot[(last - chunk) & 1];
+                float v = x[0];
+#pragma unroll
+                for (int n = 1; n < kWaves; ++n) v += x[n];
+                a.dot[bh * (a.nb + 1) + bound_of(chunk + 1)] = v;
             }
         }
     };
@@ -920,14 +929,13 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
         dr.load(dop, ct, here(l), L);
         if constexpr (!SUM) {
             // a boundary at the chunk's end: the product of the state and its gradient there
-            const int next = chunk + 1;
-            if (next < a.chunks ? next % a.bound_chunks == 0 : a.bound_end != 0) {          // block-uniform
-                const int64_t n = (next + a.bound_chunks - 1) / a.bound_chunks;
+            if (bounded(chunk)) {                            // block-uniform
+                const int next = chunk + 1;
                 float v = 0.0f;
                 if constexpr (M::kSplit) {
                     v = D.dot_kept(a.states + (bh * delta_slots<T>(a.chunks) + next) * KC * VP, zf);
                 } else {
-                    const float* p = a.bound + ((bh * a.nb + n - 1) * KF * kThreads + tid) * 4;
+                    const float* p = a.bound + ((bh * a.nb + bound_of(next) - 1) * KF * kThreads + tid) * 4;
 #pragma unroll
                     for (int k = 0; k < KF; ++k) {
                         const f32x4 o = *reinterpret_cast<const f32x4*>(p + k * 4 * kThreads);
@@ -937,14 +945,7 @@ __global__ __launch_bounds__(VP * 4, 2) void delta_rev_kernel(DeltaArgs a) {
                 }
 #pragma unroll
                 for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
-                if (l == 0) smem.xdot[w] = v;
-                __syncthreads();
-                if (tid == 0) {
-                    v = smem.xdot[0];
-#pragma unroll
-                    for (int i = 1; i < kWaves; ++i) v += smem.xdot[i];
-                    a.dot[bh * (a.nb + 1) + n] = v;
-                }
+                if (l == 0) smem.xdot[(last - chunk) & 1][w] = v;
             }
             D.keep(a.grads + unit * KC * VP, zf);
         }

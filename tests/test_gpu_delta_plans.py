@@ -1,5 +1,5 @@
 """GPU: the gated delta rule in calls large enough that a block takes several heads of a group and the decays' boundaries lie two and
-four chunks apart, against the rule in 64 bits.  Small heads keep the reference cheap.  What the rules of delta_api.cpp give:
+four chunks apart in fp32, against the rule in 64 bits.  Small heads keep the reference cheap.  What the rules of delta_api.cpp give:
 heads a block of the preparation and of the gradients of q and k, chunks between boundaries.  Bounds as in test_gpu_delta; results
 in bf16 are held to one rounding, 2^-8 / sqrt 3 in the 2-norm."""
 import numpy as np
@@ -11,7 +11,7 @@ from test_gpu_delta import NAMES, backward, bound_of, check, cuda, forward, make
 
 pytestmark = pytest.mark.gpu
 
-# (batch, heads, groups, dk, dv, tokens), starts              preparation, gradients, boundaries
+# (batch, heads, groups, dk, dv, tokens), starts              preparation, gradients, fp32's boundaries
 SHAPES = [((4, 40, 8, 8, 12, 320), 0),                      # 1, 3 of 5 (two parts), 1
           ((9, 40, 8, 8, 12, 257), 128),                    # 2 of 5 (three parts), 5, 2
           ((16, 40, 8, 8, 12, 127), 0),                     # 1, 5, 2
