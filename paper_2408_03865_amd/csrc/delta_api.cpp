@@ -74,32 +74,36 @@ struct Plan {
 int32_t bound_chunks(int64_t units, bool f32) { return !f32 || units <= 1024 ? 1 : units <= 4096 ? 2 : 4; }
 // Heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks.  Us with this rule, with
 // all heads of a group in a block and with one (batch x heads in groups x tokens, dk x dv; bf16):
-//   the preparation, forward    1 x 32 in 1 x 512, 128 x 128: 50, 183, 50    2 x 64 in 4 x 2048, 128 x 128: 192, 222, 192
-//                               8 x 32 in 16 x 4096, 128 x 128: 524, 524, 560    1 x 24 in 8 x 30001, 128 x 64: 620, 619, 649
-//   gradients of q, k, backward 1 x 32 in 1 x 512, 128 x 128: 165, 319    1 x 16 in 1 x 4096, 64 x 64: 192, 225
+//   the preparation, forward    1 x 32 in 1 x 512, 128 x 128: 63, 175, 63    2 x 64 in 4 x 2048, 128 x 128: 245, 270, 246
+//                               8 x 32 in 16 x 4096, 128 x 128: 610, 610, 637    1 x 24 in 8 x 30001, 128 x 64: 597, 597, 629
+//   gradients of q, k, backward 1 x 32 in 1 x 512, 128 x 128: 165, 579, 157    1 x 16 in 1 x 4096, 64 x 64: 196, 286, 194
+//                               8 x 32 in 16 x 4096, 128 x 128: 3018, 3018, 3330    4 x 24 in 8 x 2048, 64 x 64: 368, 368, 405
 int32_t heads_for(int64_t blocks, int64_t rep, int64_t target) {
     int64_t per = rep;
     while (per > 1 && blocks * ((rep + per - 1) / per) < target) per = (per + 1) / 2;
     return (int32_t)per;
 }
 
-// The cheapest split, in units of a chunk walked alone on a CU (with these, the figures below to within 10%):
+// The cheapest split, in units of a chunk walked alone on a CU (4.4 us forward, 3.5 in one of the backward's walks; with these, the
+// figures below to within 10%):
 //   - a CU holds two blocks of heads with up to 64 features of v, one with more; a chunk in company takes 1.35, and
 //     blocks beyond a round add to it, in the walks that end a call with a quarter of a block's wait besides;
-//   - a sum walk takes 0.7 of one in time (0.3 backwards) and needs a block more for every 64 or 128 columns of the
-//     multiplier; the chain of the segments' states 0.5 a segment;
-//   - a block costs a chunk besides its own, the launches two.
+//   - a sum walk takes 0.55 of one forward and 0.7 in the backward (0.3 backwards) and needs a block more for every 64 or 128
+//     columns of the multiplier; the chain of the segments' states 0.4 (0.5) a segment;
+//   - a block costs a chunk besides its own, the launches 1.6 (2).
 // Us of a bf16 call by chunks a segment (batch x heads x tokens, dk x dv):
-//   forward   1 x 24 x 30001, 128 x 64: unsplit 2690, 20 815, 22 805, 27 736, 36 765    1 x 8 x 16384, 64 x 64: 687, 4 172, 8 132, 16 144
-//             1 x 64 x 8192, 128 x 128: 686, 16 579, 32 542, 64 667    2 x 24 x 4096, 64 x 64: 214, 4 146, 8 132, 16 153
-//             1 x 4 x 1024, 64 x 64: 56, 2 42, 4 46, 8 63    1 x 4 x 512: 35, 2 35, 4 43    4 x 32 x 4096, 128 x 128: 400, 16 507, 32 403
-//   backward  4 x 24 x 2048, 64 x 64: 483, 4 402, 8 384, 16 460    1 x 32 x 4096, 128 x 128: 1289, 4 616, 8 533, 16 660
-//             1 x 4 x 1024, 64 x 64: 191, 2 101, 4 122, 8 180    4 x 32 x 4096, 128 x 128: 1714, 16 1766, 32 1652
+//   forward   1 x 24 x 30001, 128 x 64: unsplit 2535, 20 757, 22 742, 27 689, 36 736    1 x 8 x 16384, 64 x 64: 1004, 4 143, 8 121, 16 152
+//             1 x 64 x 8192, 128 x 128: 888, 16 656, 32 593, 43 577, 64 775    2 x 24 x 4096, 64 x 64: 279, 4 133, 8 127, 16 161
+//             1 x 4 x 1024, 64 x 64: 72, 2 37, 4 46, 8 70    1 x 4 x 512: 41, 2 34, 4 44    4 x 32 x 4096, 128 x 128: 498, 16 580, 32 466
+//             2 x 64 x 4096, 64 x 64: 338, 8 294, 16 261, 32 311
+//   backward  4 x 24 x 2048, 64 x 64: 497, 4 411, 8 397, 16 473    1 x 32 x 4096, 128 x 128: 1439, 4 678, 8 613, 16 759
+//             1 x 4 x 1024, 64 x 64: 199, 2 94, 4 121, 8 183    4 x 32 x 4096, 128 x 128: 2149, 16 2185, 32 2092
+//             1 x 24 x 30001, 128 x 64: 8781, 20 2427, 27 2234, 36 2455
 int64_t segment_chunks(int64_t rows, int64_t dk, int64_t dv, int64_t chunks, bool backward) {
     const double slots = dv <= 64 ? 512 : 256, company = dv <= 64 ? 1.35 : 1.0;
     const int64_t columns = 1 + ((dk <= 64 ? 64 : 128) + (dv <= 64 ? 64 : 128) - 1) / (dv <= 64 ? 64 : 128);
     const auto load = [&](int64_t n) { return n <= 256 ? 1.0 : (double)n <= slots ? company : company * (double)n / slots; };
-    const double walks = backward ? 2.0 : 1.0, chain = 0.5;
+    const double walks = backward ? 2.0 : 1.0, sums = backward ? 0.7 : 0.55, chain = backward ? 0.5 : 0.4, launches = backward ? 2.0 : 1.6;
     int64_t best = chunks;
     double least = walks * load(rows) * (double)(chunks + 1);
     if (rows > 256) return best;
@@ -107,8 +111,8 @@ int64_t segment_chunks(int64_t rows, int64_t dk, int64_t dv, int64_t chunks, boo
         const int64_t nseg = (chunks + per - 1) / per;
         const double block = (double)(per + 1);
         const double walk = load(rows * nseg) + ((double)(rows * nseg) > slots ? 0.25 : 0.0);
-        double cost = walks * block * walk + 0.7 * block * load(rows * (backward ? nseg : nseg - 1) * columns) + chain * (double)nseg + 2.0;
-        if (backward) cost += 0.3 * block * load(rows * (nseg - 1)) + chain * (double)nseg + 2.0;
+        double cost = walks * block * walk + sums * block * load(rows * (backward ? nseg : nseg - 1) * columns) + chain * (double)nseg + launches;
+        if (backward) cost += 0.3 * block * load(rows * (nseg - 1)) + chain * (double)nseg + launches;
         if (cost < least) {
             least = cost;
             best = per;
