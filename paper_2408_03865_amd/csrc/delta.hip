@@ -143,7 +143,7 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
 // replace cancels between (S dout) and Mo k, and between (S dv), (D u) and Mv.  32 features of v a step, so that two blocks of 70 KB of
 // LDS fit a CU.
 // What bounds it: VALU 59%, nearly a third of it splitting, and matrix 36% with two waves a SIMD (LDS 28%): 8 x 4096 tokens, 32 heads of
-// 128 x 128 in 16 groups, 1551 us for 4.1 GB, 2.6 TB/s.  States and dv rounded to bf16, e in two terms: 806 us, but dk as far off as it is
+// 128 x 128 in 16 groups, 1521 us for 4.1 GB, 2.7 TB/s.  States and dv rounded to bf16, e in two terms: 806 us, but dk as far off as it is
 // large where the gradient of the final state is 100 times dout's, and 1.8e-3 off and not 1.7e-3 elsewhere.
 // --------------------------------------------------------------------------------------------
 // 0 where the weight is, which an infinity or NaN must not pass

@@ -23,11 +23,12 @@
 // state held: with two terms outs behind a value 100 times the others, which the next token of its key replaces, were 2.1e-2
 // off in the 2-norm and not 1.7e-3 (8 x 4096 tokens, 32 heads of 128 x 128 took 506 us and not 620).
 //
-// What bounds them: the instructions of two waves a SIMD, which the registers leave room for, and in the backward's the memory that
-// they keep states and errors in.  8 x 4096 tokens, 32 heads of 128 x 128, bf16, in cycles that a unit works and bytes moved:
-//   outs    568 us   VALU 59%, matrix 47%, LDS 25%; 1.16 GB, 2.0 TB/s
-//   states  754 us   VALU 45%, matrix 32%, LDS 17%; 2.78 GB, 3.7 TB/s
-//   reverse 873 us   VALU 44%, matrix 24%, LDS 19%; 3.60 GB, 4.1 TB/s
+// What bounds them: the instructions of two waves a SIMD.  8 x 32 rows of 128 features are 2048 waves, two for each of 1024 SIMDs; with
+// more rows the registers, 190 to 245 a wave, would leave room for no more.  In the backward also the memory that they keep states and
+// errors in.  8 x 4096 tokens, 32 heads of 128 x 128, bf16, in cycles that a unit works and bytes moved:
+//   outs    570 us   VALU 59%, matrix 47%, LDS 25%; 1.16 GB, 2.0 TB/s
+//   states  745 us   VALU 45%, matrix 32%, LDS 17%; 2.79 GB, 3.7 TB/s
+//   reverse 967 us   VALU 41%, matrix 21%, LDS 17%; 4.40 GB, 4.6 TB/s
 // Nearly half of the VALU work is splitting of states, errors and products.
 //
 // Infinities and NaN: a chunk whose k or q holds one, or whose u (du) a wave finds one in, is walked by that wave token
