@@ -452,7 +452,7 @@ __global__ void conv1d_bwd_finalize(const float* __restrict__ partial, float* __
 
 // bf16 rows that a block each walks.  Us, one wave per tile against a block per row:
 // 2 x 6208 x 5120 52, 43; 1 x 7872 x 5120 34, 27; 2 x 16192 x 2048 53, 43; 1 x 21704 x 1536 29,
-// 24; 4 x 3072 x 2048 22, 19; 5 x 7104 x 192 9.4, 7.3; 8 x 4096 x 4096 103, 95.  Beyond the limits, the second measured
+// 24; 5 x 7104 x 192 9.4, 7.3; 8 x 4096 x 4096 103, 95.  Beyond the limits, the second measured
 // with row ends looked for: 12 x 1088 x 5120 62, 68 (a block's 2048 tokens are half empty);
 // 1 x 32768 x 5120 141, 190 and 2 x 65536 x 1024 95, 123; 1 x 16384 x 256 5.1, 7.3 (too few
 // rows); unaligned rows, 8 x 4095 x 4096 119, 121, 2 x 12289 x 2048 43, 46.  In fp32 a lane's 8
@@ -523,7 +523,7 @@ hipError_t conv_fwd_t(const ConvArgs& a, hipStream_t s) {
 // places at once, which costs where blocks queue, the more so where they load its four SIMDs
 // unevenly or leave many places empty (12), and its waves read batch rows far apart.  Us, a wave per block against gathered, bf16
 // rows of 500 tokens (fp32 and 64 tokens lie within a few percent):
-//   4 waves x 3072 channels 19.9, 17.9; x 5120 28, 27;  5 x 1024 11.5, 10.9; x 1536 14.6, 15.3
+//   4 waves x 5120 channels 28, 27;  5 x 1024 11.5, 10.9; x 1536 14.6, 15.3
 //   6 x 1024 13.3, 12.2; x 1536 16.2, 17.5;  8 x 1024 15.7, 12.7; x 2048 26, 25; x 5120 51, 57
 //   9 x 512 12.2, 11.4; x 1024 16.7, 21.4;  12 x 512 14.6, 12; x 1024 21.8, 23.1
 //   16 x 512 17.4, 13.2; x 1024 28, 27; x 2048 45, 52;  9 x 704 x 5120: 61, 111; 12, 4 x 7488 x 403

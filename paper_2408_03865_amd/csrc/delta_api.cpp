@@ -65,12 +65,14 @@ struct Plan {
 };
 // Chunks between the boundaries at which the backward multiplies the two states.  A decay's gradient is a sum over the tokens up
 // to the next, of terms that cancel: its error grows with their number.  In bf16 every chunk ends at one, whose state the gradients
-// keep anyway; in fp32 boundaries have a copy of it, which moves memory.  Us with 1, 2 and 4 chunks by the chunks of all heads:
-//   fp32   512 (64 x 64) 221, 217, 216    1024 283, 279, 278    2048 480, 471, 470    3072 752, 740, 735    4096 888, 868, 865, of
-//          128 x 128 2445, 2367, 2328    8192 (64 x 64) 1413, 1363, 1338    16384 (128 x 128) 6950, 6750, 6670: 1 costs 2% to 1024, 2 1% or
-//          less to 4096 but for 128 x 128; errors in the 2-norm 5.0e-7 to 5.8e-7, 6.1e-7 to 8.1e-7, 8.0e-7 to 1.1e-6
-//   bf16   3072 397, 391, 393    4096 (128 x 128) 1119, 1091, 1080    16384 (128 x 128) 3328, 3241, 3209; errors of the last 4.5e-7, 6.0e-7,
-//          7.9e-7 (the plain form 5.6e-7)
+// keep anyway; in fp32 boundaries have a copy of it, which moves memory.  Us with 1, 2 and 4 chunks (batch x heads x tokens, dk x dv;
+// the chunks of all heads):
+//   fp32   1 x 16 x 2048, 64 x 64 (512) 221, 217, 216    2 x 16 x 2048 (1024) 283, 279, 278    4 x 16 x 2048 (2048) 480, 471, 470
+//          8 x 16 x 2048 (4096) 888, 868, 865, of 128 x 128 2445, 2367, 2328    16 x 16 x 2048, 64 x 64 (8192) 1413, 1363, 1338
+//          8 x 32 x 4096, 128 x 128 (16384) 6950, 6750, 6670: 1 costs 2% to 1024 chunks, 2 1% or less to 4096 but for 128 x 128.  Errors in the
+//          2-norm 5.0e-7 to 5.8e-7, 6.1e-7 to 8.1e-7, 8.0e-7 to 1.1e-6
+//   bf16   4 x 24 x 2048, 64 x 64 397, 391, 393    8 x 16 x 2048, 128 x 128 1119, 1091, 1080    8 x 32 x 4096 3328, 3241, 3209; errors of the
+//          last 4.5e-7, 6.0e-7, 7.9e-7 (the plain form 5.6e-7)
 int32_t bound_chunks(int64_t units, bool f32) { return !f32 || units <= 1024 ? 1 : units <= 4096 ? 2 : 4; }
 // Heads of a group that one block takes: all, or fewer where that leaves the GPU's CUs without blocks.  Us with this rule, with
 // all heads of a group in a block and with one (batch x heads in groups x tokens, dk x dv; bf16):
