@@ -99,7 +99,8 @@ __global__ __launch_bounds__(KC * 4) void delta_chain(DeltaArgs a) {
             for (int j = 0; j < KF; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) zero[e] = fmaf(m[i][j][e], 0.0f, zero[e]);
-            if (__ballot(!((zero.x + zero.y) + (zero.z + zero.w) == 0.0f)) == 0) {       // the sums in turns: a matrix instruction waits for the one whose result it takes
+            // the sums in turns: a matrix instruction waits for the one whose result it takes
+            if (__ballot(!((zero.x + zero.y) + (zero.z + zero.w) == 0.0f)) == 0) {
 #pragma unroll
                 for (int j = 0; j < KF; j += 4)
 #pragma unroll

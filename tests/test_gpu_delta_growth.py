@@ -40,8 +40,8 @@ def near(got, ref, name, g, dtype):
 
 # the last one in segments of 36 chunks, over each of which the decays sum to more than what 32 bits hold, e^88.7
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("shape,g,states", [((2, 3, 1, 7, 16, 333), 0.03, False), ((1, 2, 2, 65, 70, 200), 0.01, True), ((1, 2, 1, 3, 5, 1500), 0.05, True),
-                                            ((1, 128, 32, 3, 8, 9200), 0.042, True)], ids=lambda s: str(s))
+@pytest.mark.parametrize("shape,g,states", [((2, 3, 1, 7, 16, 333), 0.03, False), ((1, 2, 2, 65, 70, 200), 0.01, True),
+                                            ((1, 2, 1, 3, 5, 1500), 0.05, True), ((1, 128, 32, 3, 8, 9200), 0.042, True)], ids=lambda s: str(s))
 def test_decays_above_zero(shape, g, states, dtype):
     note(f"delta rule, decays of {g}, {shape} states={states} {dtype}")
     d = growing(shape, dtype, g, states)

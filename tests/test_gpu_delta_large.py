@@ -2,16 +2,16 @@
 which the next token of the same key replaces.  Its terms cancel in the outs and gradients of the tokens behind it, so that
 what is rounded of them shows there, and not what is rounded of the results.
 
-Tolerances, in the 2-norm over those tokens.  With C the size of the terms that cancel over the compared results' (by length): a
-sum of up to dk + 192 terms, each rounded to 32 bits by at most u = 2^-24 and apart from each other, is off by about sqrt(320) u of
-its terms, 1.1e-6; e comes of two such sums and a result of one more: 4e-6 C.  But k.k is one sum for all pairs of tokens, whose
-error, at most dk u, is the same in all of them: e sums to x / (1 + dk u) where it should to x, which shows as dk u C.  The terms' size follows from beta |k|^2 = 1 with one
-key and no decay: S_t holds v_t along the key and D_t what makes dv_t, so that with |q| = |k| = 1 the terms of out are as large
-as the largest |v|, of dq (S dout, dout's elements of size 1) scale |v|, of dv |dv|, of dk (S dv and D u, whose sums over v's
-features have random signs) |v| |dv| / sqrt(dv) and |dv| |u| / sqrt(dv), the largest of the row times the compared tokens'.  The
-result's own length is no measure: that of the large token alone is a product of two vectors that may be small by chance.
-bf16 results are rounded once: 2^-8 of themselves at
-most, spread evenly, 2^-8 / sqrt 3."""
+Tolerances, in the 2-norm over those tokens. With C the size of the terms that cancel over the compared results' (by length): a
+sum of up to dk + 192 terms, each rounded to 32 bits by at most u = 2^-24 and apart from each other, is off by about sqrt(320) u
+of its terms, 1.1e-6; e comes of two such sums and a result of one more: 4e-6 C. But k.k is one sum for all pairs of tokens,
+whose error, at most dk u, is the same in all of them: e sums to x / (1 + dk u) where it should to x, which shows as dk u C. The
+terms' size follows from beta |k|^2 = 1 with one key and no decay: S_t holds v_t along the key and D_t what makes dv_t, so that
+with |q| = |k| = 1 the terms of out are as large as the largest |v|, of dq (S dout, dout's elements of size 1) scale |v|, of dv
+|dv|, of dk (S dv and D u, whose sums over v's features have random signs) |v| |dv| / sqrt(dv) and |dv| |u| / sqrt(dv), the
+largest of the row times the compared tokens'. The result's own length is no measure: that of the large token alone is a product
+of two vectors that may be small by chance. bf16 results are rounded once: 2^-8 of themselves at most, spread evenly, 2^-8 /
+sqrt 3."""
 import pytest
 
 from gpu_common import note
